@@ -58,7 +58,8 @@ enum {
     HT_STATUS_BAD_PATH = 3,      /* accepted path not increasing / out of range */
     HT_STATUS_PATH_TOO_LONG = 4, /* the accepted path has more than max_path nodes */
     HT_STATUS_BAD_PAGE = 5,      /* paged cache: a block-table entry the sequence needs is outside the pool */
-    HT_STATUS_TIMEOUT = 6
+    HT_STATUS_TIMEOUT = 6,
+    HT_STATUS_BAD_PARAM = 7      /* sampling: a parameter or a uniform number of the sequence is out of range */
 };
 
 /* ht_attn_desc.flags */
@@ -352,6 +353,98 @@ int ht_draft_tree(const void *logits, int dtype, int B, int rows, int V, int fir
 int ht_rope_kv_append(const ht_attn_desc *desc /* host */, const void *q_in, const void *k_in, const void *v_in,
                       const int32_t *pos, const int32_t *kv_len, float rope_base, void *q_out, void *k_cache,
                       void *v_cache, int32_t *status, void *stream);
+
+/*
+ * Norm of each head, rotary embedding and placement of the rows' K / V behind the context, in one pass: the step ahead
+ * of ht_tree_attention for models that normalise their query and key heads, rotate a part of each head only, pair
+ * neighbouring features, or scale the rotation for contexts longer than the trained one.  (Section "Tree attention":
+ * the flattened tree keeps the tokens' positional indices; the paper's own models take ht_rope_kv_append.)
+ * For each query and key head x of D features (the norm where `norm` asks for it):
+ *     y = x * rsqrt(mean(x^2) + eps) * (weight + weight_offset)
+ * then the first rot_dim features of y are rotated in pairs (a, b) by pos * f_i:  a' = a cos - b sin, b' = b cos + a sin,
+ * with cosine and sine times `magnitude`.
+ *   rot_dim       0..D, even; half-split pairing: a multiple of 16 (8 for fp32)
+ *   interleaved   0: pair i = features (i, i + rot_dim/2); else features (2i, 2i + 1)
+ *   scaling       HT_ROPE_PLAIN     f_i = rope_base^(-2i/rot_dim)
+ *                 HT_ROPE_LINEAR    f_i / factor
+ *                 HT_ROPE_BY_PARTS  turns = orig_len * f_i / (2 pi), keep = clamp((turns - low) / (high - low), 0, 1):
+ *                                   f_i * (keep + (1 - keep) / factor)
+ *   magnitude     0 selects 1
+ *   q_stride, k_stride, v_stride   elements between consecutive rows of q_in / k_in / v_in (row r of sequence b is row
+ *                 b*N + r); 0 = Hq*D / Hkv*D.  The heads of a row are D apart: a fused projection's output is passed by
+ *                 three pointers into it and one stride.
+ */
+#define HT_HEAD_NORM_Q 1
+#define HT_HEAD_NORM_K 2
+enum { HT_ROPE_PLAIN = 0, HT_ROPE_LINEAR = 1, HT_ROPE_BY_PARTS = 2 };
+typedef struct {
+    int32_t norm;                  /* HT_HEAD_NORM_Q | HT_HEAD_NORM_K */
+    int32_t rot_dim, interleaved, scaling;
+    float eps, weight_offset, rope_base, factor, low, high, orig_len, magnitude;
+    int64_t q_stride, k_stride, v_stride;
+} ht_head_desc;
+
+/*
+ *   desc     B, N, Hq, Hkv, D, cap, dtype and the cache strides are used (scale, num_splits, flags are not)
+ *   q_in [B, N, Hq, D], k_in, v_in [B, N, Hkv, D] (rows strided, see above), q_weight, k_weight [D] of `dtype` or NULL
+ *            (ones, without weight_offset)
+ *   pos [B, N] int32, kv_len [B] int32
+ *   q_out    [B, N, Hq, D] dense; may be q_in itself where q_in is dense, and must not overlap the inputs otherwise
+ *   k_cache, v_cache [B, Hkv, cap, D]: row kv_len[b] + r receives the key row / v_in[b, r] as is
+ *   status   [B] out: HT_STATUS_BAD_LEN sequences are skipped (nothing of theirs is written)
+ * The paged form takes pools, block table and descriptor as ht_rope_kv_append_paged does; a row whose page entry lies
+ * outside the pool is not stored (its q row is still written) and marks the sequence HT_STATUS_BAD_PAGE.
+ * Angles are formed in 64 bits, the norm, products and sums in fp32, one rounding to `dtype`.  D in {64, 128}.
+ */
+int ht_norm_rope_kv_append(const ht_attn_desc *desc /* host */, const ht_head_desc *head /* host */, const void *q_in,
+                           const void *k_in, const void *v_in, const void *q_weight, const void *k_weight,
+                           const int32_t *pos, const int32_t *kv_len, void *q_out, void *k_cache, void *v_cache,
+                           int32_t *status, void *stream);
+int ht_norm_rope_kv_append_paged(const ht_attn_desc *desc /* host */, const ht_head_desc *head /* host */,
+                                 const ht_paged_desc *pages /* host */, const void *q_in, const void *k_in,
+                                 const void *v_in, const void *q_weight, const void *k_weight, const int32_t *pos,
+                                 const int32_t *kv_len, const int32_t *block_table, void *q_out, void *k_pages,
+                                 void *v_pages, int32_t *status, void *stream);
+
+/*
+ * Tokens drawn from filtered distributions with given uniform numbers.  (The paper verifies greedily; with sampled tokens
+ * in the argmax's place the emitted text is distributed as, and for the same uniform numbers equal to, what sampling one
+ * token at a time gives.)  For a row of logits x with largest value m:
+ *     w_i = exp((x_i - m) / temperature), 0 where that is below 2^-1000; larger x comes first in the order, the lower
+ *     index among equals.  Kept are the first top_k of the order; of those, the ones before which less than
+ *     top_p * (weight of the first top_k) has come; of those, the ones with w_i >= min_p.  The token is the first kept
+ *     one, in index order, at which the running kept weight exceeds uniform * (kept weight); the last one with a
+ *     weight where none does (uniform = 1).
+ *   logits       [B, N, V] of `dtype`; NaN counts as -inf.  A row without anything above -inf gives its first -inf, a row
+ *                of NaNs 0; where +inf occurs, those tokens share the weight.
+ *   uniform      [B, N] float, in [0, 1]
+ *   temperature  [B] float or NULL (1); 0: the argmax, lowest index among equals
+ *   top_k        [B] int32 or NULL; <= 0 or >= V: off
+ *   top_p        [B] float or NULL; >= 1: off; <= 0: the first of the order
+ *   min_p        [B] float or NULL; <= 0: off
+ *   token        [B, N] int32 out
+ *   status       [B] out: HT_STATUS_BAD_PARAM where the temperature is negative, infinite or NaN, top_p or min_p NaN, min_p
+ *                above 1 or a uniform number outside [0, 1]; the sequence's tokens are then -1.
+ * Weights and their sums are held in 64 bits.  N is the rows per sequence (1 for plain decoding); V <= 2^30.
+ */
+int ht_sample(const void *logits, int dtype, int B, int N, int V, const float *uniform, const float *temperature,
+              const int32_t *top_k, const float *top_p, const float *min_p, int32_t *token, int32_t *status,
+              void *stream);
+
+/*
+ * Sampled verification -- ht_verify_greedy with each tree row's token drawn as ht_sample draws it instead of its argmax:
+ * a node is accepted where its draft token is the token drawn at its parent (top level: root_pred, the token drawn last).
+ *   logits [B, N, V], uniform [B, N]: the T tree rows are used, 1 <= T <= N
+ *   pred [B, N] out: the drawn tokens; -1 for the rows behind the tree
+ *   tokens, parent, root_pred, accept_len (also on entry: [0, 255]), accept_path, next_token: as in ht_verify_greedy
+ *   status [B] out: as ht_verify_greedy, and HT_STATUS_BAD_PARAM as ht_sample, which looks at the uniform numbers of the T
+ *            tree rows (pred -1, accept_len 0, accept_path and next_token -1)
+ */
+int ht_verify_sampled(const void *logits, int dtype, const float *uniform, const float *temperature,
+                      const int32_t *top_k, const float *top_p, const float *min_p, const int32_t *tokens,
+                      const int32_t *parent, const int32_t *root_pred, int B, int N, int T, int V, int max_path,
+                      int32_t *pred, int32_t *accept_len, int32_t *accept_path, int32_t *next_token, int32_t *status,
+                      void *stream);
 
 /*
  * Tree attention without a caller-provided workspace.  (The paper has no counterpart: this

@@ -24,12 +24,14 @@ HT_ATTN_FORCE_SIMT = 1
 HT_ATTN_WORKSPACE_CLEAN = 2
 HT_ATTN_CONTEXT_FINAL = 4
 HT_ATTN_TEST_SHORT_WAITS = 0x80000000
-HT_STATUS_BAD_PAGE, HT_STATUS_TIMEOUT = 5, 6
+HT_STATUS_BAD_PAGE, HT_STATUS_TIMEOUT, HT_STATUS_BAD_PARAM = 5, 6, 7
+HT_HEAD_NORM_Q, HT_HEAD_NORM_K = 1, 2
+HT_ROPE_PLAIN, HT_ROPE_LINEAR, HT_ROPE_BY_PARTS = range(3)
 
 EXPORTS = ("ht_version", "ht_last_error_string", "ht_transfer", "ht_tree_attention_workspace",
            "ht_tree_attention", "ht_verify_greedy", "ht_kv_compact", "ht_draft_tree", "ht_rope_kv_append", "ht_tree_attention_static",
            "ht_tree_attention_paged", "ht_rope_kv_append_paged", "ht_kv_compact_paged", "ht_tree_attention_launches",
-           "ht_verify_greedy_compact")
+           "ht_verify_greedy_compact", "ht_norm_rope_kv_append", "ht_norm_rope_kv_append_paged", "ht_sample", "ht_verify_sampled")
 HT_STATIC_SCRATCH_BYTES = 16 << 20
 
 _DTYPES = {torch.float32: HT_F32, torch.float16: HT_F16, torch.bfloat16: HT_BF16}
@@ -53,6 +55,14 @@ class CacheDesc(ctypes.Structure):
                 ("cap", ctypes.c_int32), ("D", ctypes.c_int32), ("dtype", ctypes.c_int32),
                 ("N", ctypes.c_int32), ("stride_layer", ctypes.c_int64),
                 ("stride_b", ctypes.c_int64), ("stride_h", ctypes.c_int64)]
+
+
+class HeadDesc(ctypes.Structure):
+    _fields_ = [("norm", ctypes.c_int32), ("rot_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32),
+                ("scaling", ctypes.c_int32), ("eps", ctypes.c_float), ("weight_offset", ctypes.c_float),
+                ("rope_base", ctypes.c_float), ("factor", ctypes.c_float), ("low", ctypes.c_float), ("high", ctypes.c_float),
+                ("orig_len", ctypes.c_float), ("magnitude", ctypes.c_float), ("q_stride", ctypes.c_int64),
+                ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64)]
 
 
 class HtError(RuntimeError):
@@ -105,6 +115,16 @@ def load() -> ctypes.CDLL:
         lib.ht_draft_tree.argtypes = [vp, i32, i32, i32, i32, i32, i32, i32, vp, vp, i32, vp, vp, vp, vp, vp, vp, vp]
         lib.ht_rope_kv_append.restype = i32
         lib.ht_rope_kv_append.argtypes = [ctypes.POINTER(AttnDesc), vp, vp, vp, vp, vp, ctypes.c_float, vp, vp, vp, vp, vp]
+        place = [vp] * 10
+        lib.ht_norm_rope_kv_append.restype = i32
+        lib.ht_norm_rope_kv_append.argtypes = [ctypes.POINTER(AttnDesc), ctypes.POINTER(HeadDesc), *place, vp, vp]
+        lib.ht_norm_rope_kv_append_paged.restype = i32
+        lib.ht_norm_rope_kv_append_paged.argtypes = [ctypes.POINTER(AttnDesc), ctypes.POINTER(HeadDesc), ctypes.POINTER(PagedDesc),
+                                                     *place, vp, vp, vp]
+        lib.ht_sample.restype = i32
+        lib.ht_sample.argtypes = [vp, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp]
+        lib.ht_verify_sampled.restype = i32
+        lib.ht_verify_sampled.argtypes = [vp, i32, vp, vp, vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp]
         _lib = lib
     return _lib
 
@@ -442,3 +462,165 @@ def kv_compact_paged(k_pages, v_pages, block_table, n_rows: int, kv_len, accept_
                                       _ptr(block_table), _ptr(kv_len), _ptr(accept_len), _ptr(accept_path), max_path,
                                       _ptr(new_kv_len), _ptr(status), _stream()))
     return new_kv_len, status
+
+
+def make_head_desc(D: int, norm: int = HT_HEAD_NORM_Q | HT_HEAD_NORM_K, eps: float = 1e-6, weight_offset: float = 0.0,
+                   rot_dim: Optional[int] = None, interleaved: bool = False, rope_base: float = 10000.0,
+                   scaling: int = HT_ROPE_PLAIN, factor: float = 1.0, low: float = 1.0, high: float = 4.0,
+                   orig_len: float = 0.0, magnitude: float = 1.0) -> HeadDesc:
+    """What ``norm_rope_kv_append`` does to each head of ``D`` features (``rot_dim`` None: all of them are rotated).
+    The calls fill in the row strides of their tensors."""
+    return HeadDesc(norm, D if rot_dim is None else rot_dim, int(interleaved), scaling, eps, weight_offset, rope_base, factor, low,
+                    high, orig_len, magnitude, 0, 0, 0)
+
+
+def _one_device(first: torch.Tensor, *others) -> None:
+    """All tensors on the current device, whose stream the work goes to."""
+    dev = first.device
+    for t in others:
+        if t is not None and t.device != dev:
+            raise ValueError("tensors on different devices")
+    if dev.index != torch.cuda.current_device():
+        raise ValueError("the tensors' device is not the current one")
+
+
+def _row_stride(t: torch.Tensor, name: str) -> int:
+    """Elements between the rows of t [B, N, H, D], whose heads must be dense and whose rows evenly spaced."""
+    B, N, H, D = t.shape
+    sb, sn, sh, sd = t.stride()
+    if sd != 1 or (sh != D and H > 1) or (B > 1 and N > 1 and sb != N * sn):
+        raise ValueError("%s: heads must be contiguous and D apart, rows evenly spaced over [B, N]" % name)
+    return sn if N > 1 else (sb if B > 1 else H * D)
+
+
+def _place_args(q_in, k_in, v_in, pos, kv_len, head, q_weight, k_weight, q_out):
+    B, N, Hq, D = q_in.shape
+    for t, name in ((q_in, "q_in"), (k_in, "k_in"), (v_in, "v_in")):
+        if not t.is_cuda or t.dtype != q_in.dtype:
+            raise ValueError("%s must be a CUDA tensor of q_in's dtype (this library has no CPU path)" % name)
+    if k_in.shape != v_in.shape or k_in.shape[:2] != (B, N) or k_in.shape[3] != D:
+        raise ValueError("k_in and v_in must be [B, N, Hkv, D]")
+    _need(pos, torch.int32, "pos")
+    _need(kv_len, torch.int32, "kv_len")
+    if tuple(pos.shape) != (B, N) or tuple(kv_len.shape) != (B,):
+        raise ValueError("pos must be [B, N] and kv_len [B]")
+    for w, name in ((q_weight, "q_weight"), (k_weight, "k_weight")):
+        if w is not None:
+            _need(w, q_in.dtype, name)
+            if tuple(w.shape) != (D,):
+                raise ValueError("%s must be [D]" % name)
+    if q_out is None:
+        q_out = torch.empty((B, N, Hq, D), dtype=q_in.dtype, device=q_in.device)
+    _need(q_out, q_in.dtype, "q_out")
+    if q_out.shape != q_in.shape:
+        raise ValueError("q_out must be [B, N, Hq, D]")
+    _one_device(q_in, k_in, v_in, pos, kv_len, q_weight, k_weight, q_out)
+    head = HeadDesc.from_buffer_copy(head)               # the caller's is left as it is
+    head.q_stride, head.k_stride, head.v_stride = _row_stride(q_in, "q_in"), _row_stride(k_in, "k_in"), _row_stride(v_in, "v_in")
+    return head, q_out, torch.empty(B, dtype=torch.int32, device=q_in.device)
+
+
+def norm_rope_kv_append(q_in, k_in, v_in, pos, kv_len, k_cache, v_cache, head: HeadDesc, q_weight=None, k_weight=None, q_out=None):
+    """Norm and rotation of the query and key heads as ``head`` (``make_head_desc``) says, K and V into the caches.
+    q_in [B, N, Hq, D], k_in, v_in [B, N, Hkv, D] (rows may be strided: slices of a fused projection); pos [B, N] int32;
+    kv_len [B] int32; caches [B, Hkv, cap, D] (written in place at rows kv_len[b] + r).  Returns (q_out, status)."""
+    head, q_out, status = _place_args(q_in, k_in, v_in, pos, kv_len, head, q_weight, k_weight, q_out)
+    if not (k_cache.is_cuda and v_cache.is_cuda) or k_cache.dtype != q_in.dtype or v_cache.dtype != q_in.dtype:
+        raise ValueError("caches must be CUDA tensors of q_in's dtype")
+    if k_cache.stride() != v_cache.stride() or k_cache.shape != v_cache.shape or k_cache.shape[1] != k_in.shape[2]:
+        raise ValueError("k_cache and v_cache must share shape and strides and hold k_in's heads")
+    _one_device(q_in, k_cache, v_cache)
+    desc = make_attn_desc(q_in, k_cache)
+    _check(load().ht_norm_rope_kv_append(ctypes.byref(desc), ctypes.byref(head), _ptr(q_in), _ptr(k_in), _ptr(v_in), _ptr(q_weight),
+                                         _ptr(k_weight), _ptr(pos), _ptr(kv_len), _ptr(q_out), _ptr(k_cache), _ptr(v_cache),
+                                         _ptr(status), _stream()))
+    return q_out, status
+
+
+def norm_rope_kv_append_paged(q_in, k_in, v_in, pos, kv_len, block_table, k_pages, v_pages, head: HeadDesc, q_weight=None,
+                              k_weight=None, q_out=None):
+    """As ``norm_rope_kv_append`` with the caches as page pools [n_pages, Hkv, page_size, D] (written in place at the
+    logical rows kv_len[b] + r through block_table [B, max_pages]).  Returns (q_out, status)."""
+    head, q_out, status = _place_args(q_in, k_in, v_in, pos, kv_len, head, q_weight, k_weight, q_out)
+    _need(block_table, torch.int32, "block_table")
+    B, N, Hq, D = q_in.shape
+    n_pages, Hkv, page_size, Dp = k_pages.shape
+    if not (k_pages.is_cuda and v_pages.is_cuda) or k_pages.dtype != q_in.dtype or v_pages.dtype != q_in.dtype:
+        raise ValueError("page pools must be CUDA tensors of q_in's dtype")
+    if Dp != D or Hkv != k_in.shape[2] or k_pages.stride(3) != 1 or k_pages.stride(2) != D or k_pages.stride() != v_pages.stride() \
+            or k_pages.shape != v_pages.shape:
+        raise ValueError("page rows must be contiguous and D apart, K and V pools alike and of k_in's heads")
+    if block_table.dim() != 2 or block_table.shape[0] != B:
+        raise ValueError("block_table must be [B, max_pages]")
+    _one_device(q_in, k_pages, v_pages, block_table)
+    max_pages = block_table.shape[1]
+    desc = AttnDesc(B, N, Hq, Hkv, D, max_pages * page_size, _DTYPES[q_in.dtype], 0.0, 0, 0, 0, 0)
+    pages = PagedDesc(page_size, max_pages, n_pages, k_pages.stride(0), k_pages.stride(1))
+    _check(load().ht_norm_rope_kv_append_paged(ctypes.byref(desc), ctypes.byref(head), ctypes.byref(pages), _ptr(q_in), _ptr(k_in),
+                                               _ptr(v_in), _ptr(q_weight), _ptr(k_weight), _ptr(pos), _ptr(kv_len), _ptr(block_table),
+                                               _ptr(q_out), _ptr(k_pages), _ptr(v_pages), _ptr(status), _stream()))
+    return q_out, status
+
+
+def _sample_args(logits, uniform, temperature, top_k, top_p, min_p):
+    _need(logits, name="logits")
+    _need(uniform, torch.float32, "uniform")
+    B, N, V = logits.shape
+    if tuple(uniform.shape) != (B, N):
+        raise ValueError("uniform must be [B, N]")
+    for t, dtype, name in ((temperature, torch.float32, "temperature"), (top_k, torch.int32, "top_k"),
+                           (top_p, torch.float32, "top_p"), (min_p, torch.float32, "min_p")):
+        if t is not None:
+            _need(t, dtype, name)
+            if tuple(t.shape) != (B,):
+                raise ValueError("%s must be [B]" % name)
+    _one_device(logits, uniform, temperature, top_k, top_p, min_p)
+    return B, N, V
+
+
+def sample(logits, uniform, temperature=None, top_k=None, top_p=None, min_p=None, token=None):
+    """Tokens drawn from the filtered distributions of logits [B, N, V] with uniform [B, N] float32 numbers in [0, 1];
+    temperature, top_p, min_p [B] float32 and top_k [B] int32, or None.  Returns (token [B, N], status [B])."""
+    B, N, V = _sample_args(logits, uniform, temperature, top_k, top_p, min_p)
+    if token is None:
+        token = torch.empty((B, N), dtype=torch.int32, device=logits.device)
+    _need(token, torch.int32, "token")
+    if tuple(token.shape) != (B, N):
+        raise ValueError("token must be [B, N]")
+    _one_device(logits, token)
+    status = torch.empty(B, dtype=torch.int32, device=logits.device)
+    _check(load().ht_sample(_ptr(logits), _DTYPES[logits.dtype], B, N, V, _ptr(uniform), _ptr(temperature), _ptr(top_k), _ptr(top_p),
+                            _ptr(min_p), _ptr(token), _ptr(status), _stream()))
+    return token, status
+
+
+def verify_sampled(logits, uniform, tokens, parent, root_pred=None, temperature=None, top_k=None, top_p=None, min_p=None,
+                   max_path: int = 8, accept_len=None):
+    """``verify_greedy`` with the tree rows' tokens drawn as ``sample`` draws them.  logits [B, N, V], uniform [B, N];
+    tokens [B, T], parent [B, N] int32, root_pred [B] int32 or None; ``accept_len`` as in ``verify_greedy``.
+    Returns (pred [B, N], accept_len [B], accept_path [B, max_path], next_token [B], status [B])."""
+    B, N, V = _sample_args(logits, uniform, temperature, top_k, top_p, min_p)
+    _need(tokens, torch.int32, "tokens")
+    _need(parent, torch.int32, "parent")
+    if tuple(parent.shape) != (B, N) or tokens.dim() != 2 or tokens.shape[0] != B:
+        raise ValueError("parent must be [B, N] and tokens [B, T]")
+    if root_pred is not None:
+        _need(root_pred, torch.int32, "root_pred")
+        if tuple(root_pred.shape) != (B,):
+            raise ValueError("root_pred must be [B]")
+    dev = logits.device
+    if accept_len is None:
+        accept_len = torch.zeros(B, dtype=torch.int32, device=dev)
+    else:
+        _need(accept_len, torch.int32, "accept_len")
+        if tuple(accept_len.shape) != (B,):
+            raise ValueError("accept_len must be [B]")
+    _one_device(logits, tokens, parent, root_pred, accept_len)
+    pred = torch.empty((B, N), dtype=torch.int32, device=dev)
+    accept_path = torch.empty((B, max_path), dtype=torch.int32, device=dev)
+    next_token = torch.empty(B, dtype=torch.int32, device=dev)
+    status = torch.empty(B, dtype=torch.int32, device=dev)
+    _check(load().ht_verify_sampled(_ptr(logits), _DTYPES[logits.dtype], _ptr(uniform), _ptr(temperature), _ptr(top_k), _ptr(top_p),
+                                    _ptr(min_p), _ptr(tokens), _ptr(parent), _ptr(root_pred), B, N, tokens.shape[1], V, max_path,
+                                    _ptr(pred), _ptr(accept_len), _ptr(accept_path), _ptr(next_token), _ptr(status), _stream()))
+    return pred, accept_len, accept_path, next_token, status

@@ -416,4 +416,132 @@ int ht_kv_compact_paged(void *k_pages, void *v_pages, const ht_cache_desc *desc,
                           static_cast<cudaStream_t>(stream), make_page_map(pages, block_table, d.Hkv, d.D));
 }
 
+// [a, a + an) and [b, b + bn) share a byte?
+static bool overlap_bytes(const void *a, unsigned long long an, const void *b, unsigned long long bn) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return x < y + bn && y < x + an;
+}
+
+static int check_head_desc(const ht_head_desc *h, const ht_attn_desc &d) {
+    if (!h) return fail(HT_ERR_INVALID_ARG, "head descriptor is NULL");
+    if (h->norm & ~(HT_HEAD_NORM_Q | HT_HEAD_NORM_K)) return fail(HT_ERR_INVALID_ARG, "unknown bits in norm");
+    if (h->rot_dim < 0 || h->rot_dim > d.D || h->rot_dim % 2) return fail(HT_ERR_INVALID_ARG, "rot_dim = %d must be even and in [0, D]", h->rot_dim);
+    const int ve = 16 / elem_bytes(d.dtype);
+    if (!h->interleaved && h->rot_dim % (2 * ve)) return fail(HT_ERR_UNSUPPORTED, "half-split rot_dim = %d must be a multiple of %d for this dtype", h->rot_dim, 2 * ve);
+    if (!(h->eps >= 0.f)) return fail(HT_ERR_INVALID_ARG, "eps must not be negative");
+    if (h->rot_dim > 0) {
+        if (!(h->rope_base > 1.f)) return fail(HT_ERR_INVALID_ARG, "rope_base must exceed 1");
+        if (h->scaling < HT_ROPE_PLAIN || h->scaling > HT_ROPE_BY_PARTS) return fail(HT_ERR_INVALID_ARG, "unknown scaling %d", h->scaling);
+        if (h->scaling != HT_ROPE_PLAIN && !(h->factor > 0.f)) return fail(HT_ERR_INVALID_ARG, "factor must be positive");
+        if (h->scaling == HT_ROPE_BY_PARTS && (!(h->high > h->low) || !(h->orig_len > 0.f)))
+            return fail(HT_ERR_INVALID_ARG, "by parts: high must exceed low and orig_len be positive");
+    }
+    const long long qs = h->q_stride ? h->q_stride : (long long)d.Hq * d.D;
+    const long long ks = h->k_stride ? h->k_stride : (long long)d.Hkv * d.D, vs = h->v_stride ? h->v_stride : (long long)d.Hkv * d.D;
+    if (qs < (long long)d.Hq * d.D || ks < (long long)d.Hkv * d.D || vs < (long long)d.Hkv * d.D)
+        return fail(HT_ERR_INVALID_ARG, "row strides smaller than a row");
+    if (qs % ve || ks % ve || vs % ve) return fail(HT_ERR_INVALID_ARG, "row strides must be multiples of 16 bytes");
+    return HT_OK;
+}
+
+static int norm_rope(const ht_attn_desc &d, const ht_head_desc *head, const void *q_in, const void *k_in, const void *v_in,
+                     const void *q_weight, const void *k_weight, const int32_t *pos, const int32_t *kv_len, void *q_out, void *kc,
+                     void *vc, int32_t *status, void *stream, const PageMap &pm) {
+    int rc = check_head_desc(head, d);
+    if (rc != HT_OK) return rc;
+    if (d.B == 0 || d.N == 0) return HT_OK;
+    if (!q_in || !k_in || !v_in || !pos || !kv_len || !q_out || !kc || !vc || !status) return fail(HT_ERR_INVALID_ARG, "NULL pointer");
+    if (!aligned16(q_in) || !aligned16(k_in) || !aligned16(v_in) || !aligned16(q_out) || !aligned16(kc) || !aligned16(vc) ||
+        !aligned16(q_weight) || !aligned16(k_weight))
+        return fail(HT_ERR_INVALID_ARG, "pointers must be 16-byte aligned");
+    const unsigned long long rows = (unsigned long long)d.B * d.N, e = elem_bytes(d.dtype);
+    if (rows > 0x7fffffffULL) return fail(HT_ERR_UNSUPPORTED, "B*N too large");
+    const unsigned long long qrow = (unsigned long long)d.Hq * d.D, krow = (unsigned long long)d.Hkv * d.D;
+    const unsigned long long qs = head->q_stride ? head->q_stride : qrow, ks = head->k_stride ? head->k_stride : krow,
+                             vs = head->v_stride ? head->v_stride : krow;
+    const unsigned long long out_bytes = rows * qrow * e;
+    const bool in_place = q_out == q_in && qs == qrow;
+    if ((!in_place && overlap_bytes(q_out, out_bytes, q_in, ((rows - 1) * qs + qrow) * e)) ||
+        overlap_bytes(q_out, out_bytes, k_in, ((rows - 1) * ks + krow) * e) || overlap_bytes(q_out, out_bytes, v_in, ((rows - 1) * vs + krow) * e))
+        return fail(HT_ERR_INVALID_ARG, "q_out overlaps an input (it may be q_in itself where q_in is dense)");
+    return launch_norm_rope(d, *head, q_in, k_in, v_in, q_weight, k_weight, pos, kv_len, q_out, kc, vc, status,
+                            static_cast<cudaStream_t>(stream), pm);
+}
+
+int ht_norm_rope_kv_append(const ht_attn_desc *desc, const ht_head_desc *head, const void *q_in, const void *k_in, const void *v_in,
+                           const void *q_weight, const void *k_weight, const int32_t *pos, const int32_t *kv_len, void *q_out,
+                           void *k_cache, void *v_cache, int32_t *status, void *stream) {
+    Range range("ht_norm_rope_kv_append");
+    if (desc && head) trace("ht_norm_rope_kv_append B=%d N=%d Hq=%d Hkv=%d D=%d dtype=%d norm=%d rot_dim=%d interleaved=%d scaling=%d", desc->B, desc->N, desc->Hq, desc->Hkv, desc->D, desc->dtype, head->norm, head->rot_dim, head->interleaved, head->scaling);
+    int rc = check_attn_desc(desc);
+    if (rc != HT_OK) return rc;
+    return norm_rope(*desc, head, q_in, k_in, v_in, q_weight, k_weight, pos, kv_len, q_out, k_cache, v_cache, status, stream, PageMap{});
+}
+
+int ht_norm_rope_kv_append_paged(const ht_attn_desc *desc, const ht_head_desc *head, const ht_paged_desc *pages, const void *q_in,
+                                 const void *k_in, const void *v_in, const void *q_weight, const void *k_weight,
+                                 const int32_t *pos, const int32_t *kv_len, const int32_t *block_table, void *q_out, void *k_pages,
+                                 void *v_pages, int32_t *status, void *stream) {
+    Range range("ht_norm_rope_kv_append_paged");
+    if (desc && head && pages) trace("ht_norm_rope_kv_append_paged B=%d N=%d Hq=%d Hkv=%d D=%d page_size=%d dtype=%d norm=%d rot_dim=%d interleaved=%d scaling=%d", desc->B, desc->N, desc->Hq, desc->Hkv, desc->D, pages->page_size, desc->dtype, head->norm, head->rot_dim, head->interleaved, head->scaling);
+    if (!desc) return fail(HT_ERR_INVALID_ARG, "NULL descriptor");
+    int rc = check_paged_desc(pages, desc->Hkv, desc->D);
+    if (rc != HT_OK) return rc;
+    ht_attn_desc d = *desc;
+    d.cap = pages->max_pages * pages->page_size;
+    d.kv_stride_b = 0;
+    d.kv_stride_h = 0;
+    rc = check_attn_desc(&d);
+    if (rc != HT_OK) return rc;
+    if (d.B > 0 && d.N > 0 && !block_table) return fail(HT_ERR_INVALID_ARG, "NULL pointer");
+    return norm_rope(d, head, q_in, k_in, v_in, q_weight, k_weight, pos, kv_len, q_out, k_pages, v_pages, status, stream,
+                     make_page_map(pages, block_table, d.Hkv, d.D));
+}
+
+static int check_sample(const void *logits, int dtype, int B, int N, int V) {
+    if (B < 0 || N < 0) return fail(HT_ERR_INVALID_ARG, "negative size");
+    if (!valid_dtype(dtype)) return fail(HT_ERR_INVALID_ARG, "unknown dtype %d", dtype);
+    if (V <= 0) return fail(HT_ERR_INVALID_ARG, "V must be positive");
+    if (V > 1 << 30) return fail(HT_ERR_UNSUPPORTED, "V = %d exceeds 2^30", V);
+    if (!aligned16(logits)) return fail(HT_ERR_INVALID_ARG, "logits must be 16-byte aligned");
+    if ((long long)B * N > 0x0fffffffLL) return fail(HT_ERR_UNSUPPORTED, "B*N too large");
+    return HT_OK;
+}
+
+int ht_sample(const void *logits, int dtype, int B, int N, int V, const float *uniform, const float *temperature,
+              const int32_t *top_k, const float *top_p, const float *min_p, int32_t *token, int32_t *status, void *stream) {
+    Range range("ht_sample");
+    trace("ht_sample B=%d N=%d V=%d dtype=%d temperature=%d top_k=%d top_p=%d min_p=%d", B, N, V, dtype, temperature != nullptr, top_k != nullptr, top_p != nullptr, min_p != nullptr);
+    int rc = check_sample(logits, dtype, B, N, V);
+    if (rc != HT_OK) return rc;
+    if (B == 0 || N == 0) return HT_OK;
+    if (!logits || !uniform || !token || !status) return fail(HT_ERR_INVALID_ARG, "NULL pointer");
+    SampleArgs a{};
+    a.logits = logits; a.uniform = uniform; a.temperature = temperature; a.top_k = top_k; a.top_p = top_p; a.min_p = min_p;
+    a.B = B; a.N = N; a.R = N; a.V = V; a.token = token; a.status = status;
+    return launch_sample(a, dtype, "ht_sample", static_cast<cudaStream_t>(stream));
+}
+
+int ht_verify_sampled(const void *logits, int dtype, const float *uniform, const float *temperature, const int32_t *top_k,
+                      const float *top_p, const float *min_p, const int32_t *tokens, const int32_t *parent,
+                      const int32_t *root_pred, int B, int N, int T, int V, int max_path, int32_t *pred, int32_t *accept_len,
+                      int32_t *accept_path, int32_t *next_token, int32_t *status, void *stream) {
+    Range range("ht_verify_sampled");
+    trace("ht_verify_sampled B=%d N=%d T=%d V=%d max_path=%d dtype=%d root_pred=%s", B, N, T, V, max_path, dtype, root_pred ? "given" : "none");
+    int rc = check_sample(logits, dtype, B, N, V);
+    if (rc != HT_OK) return rc;
+    if (B == 0) return HT_OK;
+    if (T < 1 || T > N) return fail(HT_ERR_INVALID_ARG, "need 1 <= T <= N");
+    if (max_path <= 0 || max_path > 255) return fail(HT_ERR_INVALID_ARG, "max_path must be in 1..255");
+    if (!logits || !uniform || !tokens || !parent || !pred || !accept_len || !accept_path || !next_token || !status)
+        return fail(HT_ERR_INVALID_ARG, "NULL pointer");
+    if (T >= 1 << 23) return fail(HT_ERR_UNSUPPORTED, "T too large");     // arrivals are counted above accept_len's low eight bits
+    SampleArgs a{};
+    a.logits = logits; a.uniform = uniform; a.temperature = temperature; a.top_k = top_k; a.top_p = top_p; a.min_p = min_p;
+    a.B = B; a.N = N; a.R = T; a.V = V; a.token = pred; a.status = status;
+    a.tokens = tokens; a.parent = parent; a.root_pred = root_pred; a.T = T; a.max_path = max_path;
+    a.accept_len = accept_len; a.accept_path = accept_path; a.next_token = next_token;
+    return launch_sample(a, dtype, "ht_verify_sampled", static_cast<cudaStream_t>(stream));
+}
+
 }  // extern "C"

@@ -130,6 +130,22 @@ int launch_draft(const void *logits, int dtype, int B, int rows, int V, int firs
 int launch_rope(const ht_attn_desc &d, const void *q_in, const void *k_in, const void *v_in, const int32_t *pos,
                 const int32_t *kv_len, float base, void *q_out, void *kc, void *vc, int32_t *status, cudaStream_t s,
                 const PageMap &pm = PageMap{});
+struct SampleArgs {
+    const void *logits;
+    const float *uniform, *temperature, *top_p, *min_p;
+    const int32_t *top_k;
+    int B, N, R, V;                       // R rows of each sequence's N are sampled
+    int32_t *token, *status;              // token [B, N]
+    // verification (tokens == nullptr: sampling alone)
+    const int32_t *tokens, *parent, *root_pred;
+    int T, max_path;
+    int32_t *accept_len, *accept_path, *next_token;
+};
+// `what`: the entry point, for messages.  tokens == nullptr: no verification.
+int launch_sample(const SampleArgs &a, int dtype, const char *what, cudaStream_t s);
+int launch_norm_rope(const ht_attn_desc &d, const ht_head_desc &h, const void *q_in, const void *k_in, const void *v_in,
+                     const void *q_weight, const void *k_weight, const int32_t *pos, const int32_t *kv_len, void *q_out,
+                     void *kc, void *vc, int32_t *status, cudaStream_t s, const PageMap &pm = PageMap{});
 int launch_compact(void *kc, void *vc, const ht_cache_desc &d, const int32_t *kv_len,
                    const int32_t *accept_len, const int32_t *accept_path, int max_path,
                    int32_t *new_kv_len, int32_t *status, cudaStream_t s, const PageMap &pm = PageMap{});

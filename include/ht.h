@@ -210,6 +210,33 @@ int ht_tree_attention_paged(const ht_attn_desc *desc /* host */, const ht_paged_
                             void *stream);
 
 /*
+ * Tree attention with shaped scores: ht_tree_attention / ht_tree_attention_paged (Section "Tree attention") for models
+ * that cap their attention scores or give them a bias by distance in place of a rotary embedding.  With
+ * s = scale * q[b,r,h] . k the raw score of a visible key, the softmax is over
+ *     cap > 0       s := cap * tanh(s / cap)                (cap 0: none)
+ *     slopes given  s := s - slopes[h] * (pos[b,r] - position of the key)
+ * where the position of context row j is j and that of tree row c is pos[b,c].
+ *   slopes   [Hq] float or NULL; any sign, 0 for a head without a bias
+ *   pos      [B, N] int32 position ids of the query rows (ht_draft_tree's `pos`, followed by the pseudo rows'); needed with
+ *            slopes.  HT_ATTN_CONTEXT_FINAL says nothing about slopes and pos: the kernel ahead may write them.
+ * All other arguments, the workspace, flags, statuses and supported shapes are those of the two entry points; a NULL
+ * descriptor or one that asks for nothing is the plain call.
+ */
+typedef struct {
+    float cap;
+    const float *slopes;  /* device */
+    const int32_t *pos;   /* device */
+} ht_score_desc;
+int ht_tree_attention_scored(const ht_attn_desc *desc /* host */, const ht_score_desc *score /* host */, const void *q,
+                             const void *k_cache, const void *v_cache, const int32_t *kv_len, const int32_t *parent,
+                             void *out, void *workspace, size_t workspace_bytes, int32_t *status, void *stream);
+int ht_tree_attention_scored_paged(const ht_attn_desc *desc /* host */, const ht_paged_desc *pages /* host */,
+                                   const ht_score_desc *score /* host */, const void *q, const void *k_pages,
+                                   const void *v_pages, const int32_t *block_table, const int32_t *kv_len,
+                                   const int32_t *parent, void *out, void *workspace, size_t workspace_bytes,
+                                   int32_t *status, void *stream);
+
+/*
  * The two row-moving steps on a paged cache (same pools, block table and descriptor as
  * ht_tree_attention_paged; one block table serves all layers):
  *   ht_rope_kv_append_paged  as ht_rope_kv_append, the rows of sequence b landing at logical cache rows

@@ -31,7 +31,8 @@ HT_ROPE_PLAIN, HT_ROPE_LINEAR, HT_ROPE_BY_PARTS = range(3)
 EXPORTS = ("ht_version", "ht_last_error_string", "ht_transfer", "ht_tree_attention_workspace",
            "ht_tree_attention", "ht_verify_greedy", "ht_kv_compact", "ht_draft_tree", "ht_rope_kv_append", "ht_tree_attention_static",
            "ht_tree_attention_paged", "ht_rope_kv_append_paged", "ht_kv_compact_paged", "ht_tree_attention_launches",
-           "ht_verify_greedy_compact", "ht_norm_rope_kv_append", "ht_norm_rope_kv_append_paged", "ht_sample", "ht_verify_sampled")
+           "ht_verify_greedy_compact", "ht_norm_rope_kv_append", "ht_norm_rope_kv_append_paged", "ht_sample", "ht_verify_sampled",
+           "ht_tree_attention_scored", "ht_tree_attention_scored_paged")
 HT_STATIC_SCRATCH_BYTES = 16 << 20
 
 _DTYPES = {torch.float32: HT_F32, torch.float16: HT_F16, torch.bfloat16: HT_BF16}
@@ -55,6 +56,10 @@ class CacheDesc(ctypes.Structure):
                 ("cap", ctypes.c_int32), ("D", ctypes.c_int32), ("dtype", ctypes.c_int32),
                 ("N", ctypes.c_int32), ("stride_layer", ctypes.c_int64),
                 ("stride_b", ctypes.c_int64), ("stride_h", ctypes.c_int64)]
+
+
+class ScoreDesc(ctypes.Structure):
+    _fields_ = [("cap", ctypes.c_float), ("slopes", ctypes.c_void_p), ("pos", ctypes.c_void_p)]
 
 
 class HeadDesc(ctypes.Structure):
@@ -115,6 +120,11 @@ def load() -> ctypes.CDLL:
         lib.ht_draft_tree.argtypes = [vp, i32, i32, i32, i32, i32, i32, i32, vp, vp, i32, vp, vp, vp, vp, vp, vp, vp]
         lib.ht_rope_kv_append.restype = i32
         lib.ht_rope_kv_append.argtypes = [ctypes.POINTER(AttnDesc), vp, vp, vp, vp, vp, ctypes.c_float, vp, vp, vp, vp, vp]
+        lib.ht_tree_attention_scored.restype = i32
+        lib.ht_tree_attention_scored.argtypes = [ctypes.POINTER(AttnDesc), ctypes.POINTER(ScoreDesc), *lib.ht_tree_attention.argtypes[1:]]
+        lib.ht_tree_attention_scored_paged.restype = i32
+        lib.ht_tree_attention_scored_paged.argtypes = [ctypes.POINTER(AttnDesc), ctypes.POINTER(PagedDesc), ctypes.POINTER(ScoreDesc),
+                                                       *lib.ht_tree_attention_paged.argtypes[2:]]
         place = [vp] * 10
         lib.ht_norm_rope_kv_append.restype = i32
         lib.ht_norm_rope_kv_append.argtypes = [ctypes.POINTER(AttnDesc), ctypes.POINTER(HeadDesc), *place, vp, vp]
@@ -624,3 +634,84 @@ def verify_sampled(logits, uniform, tokens, parent, root_pred=None, temperature=
                                     _ptr(min_p), _ptr(tokens), _ptr(parent), _ptr(root_pred), B, N, tokens.shape[1], V, max_path,
                                     _ptr(pred), _ptr(accept_len), _ptr(accept_path), _ptr(next_token), _ptr(status), _stream()))
     return pred, accept_len, accept_path, next_token, status
+
+
+def _score_desc(q, cap, slopes, pos) -> ScoreDesc:
+    B, N, Hq, _ = q.shape
+    if slopes is not None:
+        _need(slopes, torch.float32, "slopes")
+        if pos is None:
+            raise ValueError("slopes need pos")
+        _need(pos, torch.int32, "pos")
+        if tuple(slopes.shape) != (Hq,) or tuple(pos.shape) != (B, N):
+            raise ValueError("slopes must be [Hq] and pos [B, N]")
+        _one_device(q, slopes, pos)
+    return ScoreDesc(float(cap), _ptr(slopes), None if slopes is None else _ptr(pos))
+
+
+def _attn_buffers(q, desc, out, workspace):
+    if out is None:
+        out = torch.empty_like(q)
+    _need(out, q.dtype, "out")
+    if out.shape != q.shape:
+        raise ValueError("out must have q's shape")
+    need = tree_attention_workspace(desc)
+    if workspace is None and need:
+        workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+    return out, workspace, 0 if workspace is None else workspace.numel() * workspace.element_size()
+
+
+def tree_attention_scored(q, k_cache, v_cache, kv_len, parent, cap: float = 0.0, slopes=None, pos=None, out=None, workspace=None,
+                          status=None, scale: float = 0.0, num_splits: int = 0, flags: int = 0):
+    """``tree_attention`` with the scores capped (cap * tanh(s / cap), 0: not) and biased by distance (slopes [Hq] float32
+    with pos [B, N] int32, or None).  Returns (out, status)."""
+    _need(q, name="q")
+    _need(kv_len, torch.int32, "kv_len")
+    _need(parent, torch.int32, "parent")
+    if not (k_cache.is_cuda and v_cache.is_cuda) or k_cache.dtype != q.dtype or v_cache.dtype != q.dtype:
+        raise ValueError("caches must be CUDA tensors of q's dtype")
+    if k_cache.stride() != v_cache.stride() or k_cache.shape != v_cache.shape:
+        raise ValueError("k_cache and v_cache must share shape and strides")
+    _one_device(q, k_cache, v_cache, kv_len, parent, out, workspace, status)
+    score = _score_desc(q, cap, slopes, pos)
+    desc = make_attn_desc(q, k_cache, scale, num_splits, flags)
+    B, N = desc.B, desc.N
+    if tuple(parent.shape) != (B, N) or tuple(kv_len.shape) != (B,):
+        raise ValueError("parent must be [B, N] and kv_len [B]")
+    out, workspace, ws_bytes = _attn_buffers(q, desc, out, workspace)
+    if status is None:
+        status = torch.empty(B, dtype=torch.int32, device=q.device)
+    _check(load().ht_tree_attention_scored(ctypes.byref(desc), ctypes.byref(score), _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(kv_len),
+                                           _ptr(parent), _ptr(out), _ptr(workspace), ws_bytes, _ptr(status), _stream()))
+    return out, status
+
+
+def tree_attention_scored_paged(q, k_pages, v_pages, block_table, kv_len, parent, cap: float = 0.0, slopes=None, pos=None, out=None,
+                                workspace=None, status=None, scale: float = 0.0, flags: int = 0):
+    """``tree_attention_paged`` with the scores shaped as in ``tree_attention_scored``.  Returns (out, status)."""
+    _need(q, name="q")
+    _need(block_table, torch.int32, "block_table")
+    _need(kv_len, torch.int32, "kv_len")
+    _need(parent, torch.int32, "parent")
+    if not (k_pages.is_cuda and v_pages.is_cuda) or k_pages.dtype != q.dtype or v_pages.dtype != q.dtype:
+        raise ValueError("page pools must be CUDA tensors of q's dtype")
+    if k_pages.stride() != v_pages.stride() or k_pages.shape != v_pages.shape:
+        raise ValueError("k_pages and v_pages must share shape and strides")
+    _one_device(q, k_pages, v_pages, block_table, kv_len, parent, out, workspace, status)
+    B, N, Hq, D = q.shape
+    n_pages, Hkv, page_size, Dp = k_pages.shape
+    if Dp != D or k_pages.stride(3) != 1 or k_pages.stride(2) != D:
+        raise ValueError("page rows must be contiguous and D apart")
+    if block_table.dim() != 2 or block_table.shape[0] != B or tuple(parent.shape) != (B, N) or tuple(kv_len.shape) != (B,):
+        raise ValueError("block_table must be [B, max_pages], parent [B, N], kv_len [B]")
+    score = _score_desc(q, cap, slopes, pos)
+    max_pages = block_table.shape[1]
+    desc = AttnDesc(B, N, Hq, Hkv, D, max_pages * page_size, _DTYPES[q.dtype], scale, 0, 0, 0, flags)
+    pages = PagedDesc(page_size, max_pages, n_pages, k_pages.stride(0), k_pages.stride(1))
+    out, workspace, ws_bytes = _attn_buffers(q, desc, out, workspace)
+    if status is None:
+        status = torch.empty(B, dtype=torch.int32, device=q.device)
+    _check(load().ht_tree_attention_scored_paged(ctypes.byref(desc), ctypes.byref(pages), ctypes.byref(score), _ptr(q), _ptr(k_pages),
+                                                 _ptr(v_pages), _ptr(block_table), _ptr(kv_len), _ptr(parent), _ptr(out),
+                                                 _ptr(workspace), ws_bytes, _ptr(status), _stream()))
+    return out, status

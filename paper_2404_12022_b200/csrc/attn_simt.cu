@@ -31,9 +31,14 @@ struct SimtParams {
     int B, N, Hq, Hkv, D, cap, splits;
     long long stride_b, stride_h; // elements
     float scale_log2;
+    // the scored instantiations only
+    float scale, score_cap;       // score_cap 0: none
+    const float *slopes;          // [Hq] or null
+    const int32_t *pos;           // [B, N], with slopes
 };
 
-template <typename T, int D>
+// kScored: s -> cap tanh(s / cap), then - slope * (position of the row - of the key), in natural units.
+template <typename T, int D, bool kScored>
 __global__ void __launch_bounds__(kRows * 32)
 attn_simt_kernel(SimtParams p) {
     constexpr int DPL = D / 32;                       // output features per lane
@@ -114,7 +119,17 @@ attn_simt_kernel(SimtParams p) {
         float s = 0.f;
 #pragma unroll 8
         for (int x = 0; x < D; ++x) s = fmaf(Qs[warp][x], Ks[lane][x], s);
-        s *= p.scale_log2;
+        if constexpr (kScored) {
+            s *= p.scale;
+            if (p.score_cap > 0.f) s = p.score_cap * tanhf(s / p.score_cap);
+            if (p.slopes) {
+                const int at = key < L ? key : p.pos[(size_t)b * N + min(key - L, N - 1)];
+                s = fmaf(p.slopes[h], (float)(at - p.pos[(size_t)b * N + r]), s);
+            }
+            s *= kLog2e;
+        } else {
+            s *= p.scale_log2;
+        }
         bool visible = key < k_end;
         if (visible && key >= L) {
             const int c = key - L;
@@ -210,7 +225,8 @@ size_t attn_simt_workspace(const ht_attn_desc &d, int *splits_out) {
 template <typename T, int D>
 static int launch_typed(const SimtParams &p, cudaStream_t s) {
     dim3 grid((p.N + kRows - 1) / kRows, p.Hq, p.B * p.splits);
-    attn_simt_kernel<T, D><<<grid, kRows * 32, 0, s>>>(p);
+    if (p.score_cap > 0.f || p.slopes) attn_simt_kernel<T, D, true><<<grid, kRows * 32, 0, s>>>(p);
+    else attn_simt_kernel<T, D, false><<<grid, kRows * 32, 0, s>>>(p);
     int rc = check_launch("ht_tree_attention (simt)");
     if (rc != HT_OK || p.splits == 1) return rc;
     const long long items = (long long)p.B * p.N * p.Hq;
@@ -220,7 +236,7 @@ static int launch_typed(const SimtParams &p, cudaStream_t s) {
 
 int launch_attn_simt(const ht_attn_desc &d, const void *q, const void *kc, const void *vc,
                      const int32_t *kv_len, const int32_t *parent, void *out, void *ws, size_t ws_bytes,
-                     int32_t *status, cudaStream_t s) {
+                     int32_t *status, cudaStream_t s, const ht_score_desc *score) {
     SimtParams p;
     int splits;
     const size_t need = attn_simt_workspace(d, &splits);
@@ -233,6 +249,10 @@ int launch_attn_simt(const ht_attn_desc &d, const void *q, const void *kc, const
     p.stride_b = d.kv_stride_b ? d.kv_stride_b : (long long)d.Hkv * d.cap * d.D;
     const float scale = d.scale > 0.f ? d.scale : 1.f / sqrtf((float)d.D);
     p.scale_log2 = scale * kLog2e;
+    p.scale = scale;
+    p.score_cap = score ? score->cap : 0.f;
+    p.slopes = score ? score->slopes : nullptr;
+    p.pos = score ? score->pos : nullptr;
 #define HT_DISPATCH(T)                                          \
     (d.D == 64 ? launch_typed<T, 64>(p, s) : launch_typed<T, 128>(p, s))
     switch (d.dtype) {

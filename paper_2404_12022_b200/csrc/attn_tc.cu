@@ -116,7 +116,8 @@ __device__ __forceinline__ void fetch_q_tile(Smem &sm, const CUtensorMap &tm_q, 
 
 // kPaged: the cache is a pool of pages (separate instantiations, so that the contiguous kernels carry none of that code).
 // kClustered: launched as clusters (p.cluster_k > 1); a template parameter so that the persistent form carries no cluster code.
-template <bool kBf16, bool kPaged, bool kClustered>
+// kScored: scores capped or biased by distance before the softmax (shape_scores).
+template <bool kBf16, bool kPaged, bool kClustered, bool kScored = false>
 __global__ void __launch_bounds__(kThreads, 1)
 attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
                const __grid_constant__ CUtensorMap tm_v, const Params p, const PagedParams pp) {
@@ -333,7 +334,7 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
                     advance(k_slot, k_ph, j == 0 ? 1 : 2);                    // K entries: 0, 1, 3, 5, ...
                     if (j > 0) issue_pv(j - 1, prev_first, prev_tree);
                     prev_first = i < 2;
-                    prev_tree = (sg.kt0 + i + 1) * kTile > L;
+                    prev_tree = (sg.kt0 + i + 1) * kTile > L - (kScored ? p.near_keys : 0);
                     ++j;
                 }
                 t += sg.len;
@@ -416,6 +417,8 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
                 cu.cta_mul = 1; cu.cta_add = 0;
             }
 
+            RowShape shape{0.f, 0};
+            if constexpr (kScored) shape = row_shape(p, real, sg.b, node, sg.hk * p.g + row % p.g);
             float m_ref = -INFINITY, l_sum = 0.f;
 #pragma unroll 1
             for (int i = 0; i < sg.len; ++i) {
@@ -432,46 +435,77 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
                 const int tile_lo = kt * kTile;
                 float *const xa = xa_e, *const xb = xb_e;
                 if (warp_real) {
-                if (tile_lo + kTile > L) {
-                    // The tile reaches into the tree rows / the tail: overwrite the scores of keys this
-                    // row must not see with -inf, in place, so that the two passes below need no mask.
-                    // Context keys are visible, tree key c iff bit c of the row's ancestor words, the
-                    // tail never (whatever those cache rows hold, NaN included).
-#pragma unroll 1
-                    for (int w = 0; w < 4; ++w) {
-                        const int cc0 = tile_lo + 32 * w - L;           // tree index of the word's first key
-                        if (cc0 <= -32) continue;
-                        const int wi = cc0 >> 5, sh = cc0 & 31;         // arithmetic shift: -1 for cc0 in (-32, 0)
-                        const uint32_t lo = wi < 0 ? 0xFFFFFFFFu : (wi < words ? sm.anc[wi][row] : 0u);
-                        const uint32_t hi = (wi + 1 >= 0 && wi + 1 < words) ? sm.anc[wi + 1][row] : 0u;
-                        const uint32_t vis = __funnelshift_r(lo, hi, sh);
-                        tmem_ld32(s_addr + w * 32, xa);
-                        tmem_ld_wait();
+                float mx0 = -INFINITY, mx1 = -INFINITY;
+                if constexpr (kScored) {
+                    // --- shape, mask and row maximum in one sweep; the scores go back to TMEM in log2 units ---
+                    const RowShape rs = shape;
+                    auto sweep = [&](float *x, int w) {
+                        const int key0 = tile_lo + 32 * w;
+                        shape_scores(p, x, key0, L, sg.b, rs);
+                        mask_scores(x, key0, L, &sm.anc[0][row], kRows, words);
                         uint32_t r[32];
 #pragma unroll
-                        for (int c = 0; c < 32; ++c) r[c] = ((vis >> c) & 1u) ? __float_as_uint(xa[c]) : 0xFF800000u;
+                        for (int c = 0; c < 32; c += 4) {
+                            mx0 = max3(mx0, x[c], x[c + 1]);
+                            mx1 = max3(mx1, x[c + 2], x[c + 3]);
+                        }
+#pragma unroll
+                        for (int c = 0; c < 32; ++c) r[c] = __float_as_uint(x[c]);
                         tmem_st32(s_addr + w * 32, r);
+                    };
+                    tmem_ld32(s_addr, xa);
+#pragma unroll 1
+                    for (int h = 0; h < 2; ++h) {
+                        tmem_ld_wait();
+                        tmem_ld32(s_addr + (2 * h + 1) * 32, xb);
+                        sweep(xa, 2 * h);
+                        tmem_ld_wait();
+                        if (h == 0) tmem_ld32(s_addr + 2 * 32, xa);
+                        sweep(xb, 2 * h + 1);
                     }
                     tmem_st_wait();
-                }
-                // --- pass 1: row maximum, 32 scores at a time, the next chunk in flight meanwhile ---
-                float mx0 = -INFINITY, mx1 = -INFINITY;
-                tmem_ld32(s_addr, xa);
+                    tmem_ld32(s_addr, xa);                       // chunk 0 again, for pass 2
+                } else {
+                    if (tile_lo + kTile > L) {
+                        // The tile reaches into the tree rows / the tail: overwrite the scores of keys this
+                        // row must not see with -inf, in place, so that the two passes below need no mask.
+                        // Context keys are visible, tree key c iff bit c of the row's ancestor words, the
+                        // tail never (whatever those cache rows hold, NaN included).
 #pragma unroll 1
-                for (int h = 0; h < 2; ++h) {
-                    tmem_ld_wait();
-                    tmem_ld32(s_addr + (2 * h + 1) * 32, xb);
+                        for (int w = 0; w < 4; ++w) {
+                            const int cc0 = tile_lo + 32 * w - L;           // tree index of the word's first key
+                            if (cc0 <= -32) continue;
+                            const int wi = cc0 >> 5, sh = cc0 & 31;         // arithmetic shift: -1 for cc0 in (-32, 0)
+                            const uint32_t lo = wi < 0 ? 0xFFFFFFFFu : (wi < words ? sm.anc[wi][row] : 0u);
+                            const uint32_t hi = (wi + 1 >= 0 && wi + 1 < words) ? sm.anc[wi + 1][row] : 0u;
+                            const uint32_t vis = __funnelshift_r(lo, hi, sh);
+                            tmem_ld32(s_addr + w * 32, xa);
+                            tmem_ld_wait();
+                            uint32_t r[32];
 #pragma unroll
-                    for (int c = 0; c < 32; c += 4) {
-                        mx0 = max3(mx0, xa[c], xa[c + 1]);
-                        mx1 = max3(mx1, xa[c + 2], xa[c + 3]);
+                            for (int c = 0; c < 32; ++c) r[c] = ((vis >> c) & 1u) ? __float_as_uint(xa[c]) : 0xFF800000u;
+                            tmem_st32(s_addr + w * 32, r);
+                        }
+                        tmem_st_wait();
                     }
-                    tmem_ld_wait();
-                    tmem_ld32(s_addr + ((2 * h + 2) & 3) * 32, xa);   // after the last chunk: chunk 0 again, for pass 2
+                    // --- pass 1: row maximum, 32 scores at a time, the next chunk in flight meanwhile ---
+                    tmem_ld32(s_addr, xa);
+#pragma unroll 1
+                    for (int h = 0; h < 2; ++h) {
+                        tmem_ld_wait();
+                        tmem_ld32(s_addr + (2 * h + 1) * 32, xb);
 #pragma unroll
-                    for (int c = 0; c < 32; c += 4) {
-                        mx0 = max3(mx0, xb[c], xb[c + 1]);
-                        mx1 = max3(mx1, xb[c + 2], xb[c + 3]);
+                        for (int c = 0; c < 32; c += 4) {
+                            mx0 = max3(mx0, xa[c], xa[c + 1]);
+                            mx1 = max3(mx1, xa[c + 2], xa[c + 3]);
+                        }
+                        tmem_ld_wait();
+                        tmem_ld32(s_addr + ((2 * h + 2) & 3) * 32, xa);   // after the last chunk: chunk 0 again, for pass 2
+#pragma unroll
+                        for (int c = 0; c < 32; c += 4) {
+                            mx0 = max3(mx0, xb[c], xb[c + 1]);
+                            mx1 = max3(mx1, xb[c + 2], xb[c + 3]);
+                        }
                     }
                 }
                 const float mx = fmaxf(mx0, mx1) * p.scale_log2;   // scale > 0: max commutes with scaling
@@ -503,7 +537,7 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
                 // in columns [16 c, 16 c + 16), which hold scores already consumed. ---
                 const unsigned long long nbase2 = pack_f32x2(-base, -base);
                 unsigned long long acc2 = pack_f32x2(0.f, 0.f);
-                if (tile_lo + kTile > L) softmax_pass2<kBf16, true>(s_addr, xa, xb, scale2, nbase2, acc2);
+                if (tile_lo + kTile > L - (kScored ? p.near_keys : 0)) softmax_pass2<kBf16, true>(s_addr, xa, xb, scale2, nbase2, acc2);
                 else softmax_pass2<kBf16, false>(s_addr, xa, xb, scale2, nbase2, acc2);
                 {
                     float a0, a1;
@@ -835,12 +869,16 @@ size_t attn_tc_workspace(const ht_attn_desc &d) {
 }
 
 typedef void (*AttnKernelFn)(const CUtensorMap, const CUtensorMap, const CUtensorMap, const tc::Params, const tc::PagedParams);
-static AttnKernelFn attn_tc_fn(bool bf16, bool paged, bool clustered) {
-    static const AttnKernelFn fns[8] = {
+static AttnKernelFn attn_tc_fn(bool bf16, bool paged, bool clustered, bool scored = false) {
+    static const AttnKernelFn fns[16] = {
         tc::attn_tc_kernel<false, false, false>, tc::attn_tc_kernel<true, false, false>, tc::attn_tc_kernel<false, true, false>,
         tc::attn_tc_kernel<true, true, false>,   tc::attn_tc_kernel<false, false, true>, tc::attn_tc_kernel<true, false, true>,
-        tc::attn_tc_kernel<false, true, true>,   tc::attn_tc_kernel<true, true, true>};
-    return fns[(bf16 ? 1 : 0) + (paged ? 2 : 0) + (clustered ? 4 : 0)];
+        tc::attn_tc_kernel<false, true, true>,   tc::attn_tc_kernel<true, true, true>,
+        tc::attn_tc_kernel<false, false, false, true>, tc::attn_tc_kernel<true, false, false, true>,
+        tc::attn_tc_kernel<false, true, false, true>,  tc::attn_tc_kernel<true, true, false, true>,
+        tc::attn_tc_kernel<false, false, true, true>,  tc::attn_tc_kernel<true, false, true, true>,
+        tc::attn_tc_kernel<false, true, true, true>,   tc::attn_tc_kernel<true, true, true, true>};
+    return fns[(bf16 ? 1 : 0) + (paged ? 2 : 0) + (clustered ? 4 : 0) + (scored ? 8 : 0)];
 }
 
 // Kernels per call: the attention kernel, and ahead of it the one that zeroes the arrival counters where it is needed.
@@ -853,11 +891,12 @@ static cudaError_t ensure_smem_attr(size_t smem) {
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
     if (dev >= 0 && dev < 64 && done[dev]) return cudaSuccess;
-    for (int i = 0; i < 8; ++i) {
-        e = cudaFuncSetAttribute(attn_tc_fn(i & 1, (i >> 1) & 1, i >> 2), cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    for (int i = 0; i < 16; ++i) {
+        const AttnKernelFn fn = attn_tc_fn(i & 1, (i >> 1) & 1, (i >> 2) & 1, i >> 3);
+        e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
         if (e != cudaSuccess) return e;
-        if (i >> 2) {                        // the cluster form may be launched in clusters of 16
-            e = cudaFuncSetAttribute(attn_tc_fn(i & 1, (i >> 1) & 1, 1), cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+        if ((i >> 2) & 1) {                  // the cluster form may be launched in clusters of 16
+            e = cudaFuncSetAttribute(fn, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
             if (e != cudaSuccess) return e;
         }
     }
@@ -914,11 +953,11 @@ static int make_map(CUtensorMap *map, const void *base, int dtype, const cuuint6
 
 
 int launch_attn_tc_pair_kernel(const CUtensorMap &tm_q, const CUtensorMap &tm_k, const CUtensorMap &tm_v, const tc::Params &p,
-                               const tc::PagedParams &pp, bool bf16, bool paged, cudaStream_t s);
+                               const tc::PagedParams &pp, bool bf16, bool paged, bool scored, cudaStream_t s);
 
 int launch_attn_tc(const ht_attn_desc &d, const void *q, const void *kc, const void *vc, const int32_t *kv_len,
                    const int32_t *parent, void *out, void *ws, size_t ws_bytes, int32_t *status, cudaStream_t s,
-                   const ht_paged_desc *pages, const int32_t *block_table) {
+                   const ht_paged_desc *pages, const int32_t *block_table, const ht_score_desc *score) {
     if (ws_bytes < attn_tc_workspace(d) || !ws)
         return fail(HT_ERR_WORKSPACE, "workspace holds %zu bytes, %zu needed", ws ? ws_bytes : 0, attn_tc_workspace(d));
     const int g = d.Hq / d.Hkv;
@@ -961,6 +1000,17 @@ int launch_attn_tc(const ht_attn_desc &d, const void *q, const void *kc, const v
     p.n_rt = units_per_head(d);
     const float scale = d.scale > 0.f ? d.scale : 1.f / sqrtf((float)d.D);
     p.scale_log2 = scale * 1.4426950408889634f;
+    p.score_mul = 0.f; p.cap_log2 = 0.f; p.slopes = nullptr; p.pos = nullptr; p.near_keys = 0;
+    if (score) {
+        p.score_mul = score->cap > 0.f ? (float)fmin((double)scale / score->cap, 1e30) : p.scale_log2;
+        p.cap_log2 = score->cap * 1.4426950408889634f;
+        p.slopes = score->slopes;
+        p.pos = score->pos;
+        // A steep slope leaves a row a handful of keys: the tree's and the context rows right ahead of it.  The rounding of
+        // their weights to 16 bits does not average away, as on tiles with tree keys.
+        p.near_keys = score->slopes ? tc::kTile : 0;
+        p.scale_log2 = 1.f;
+    }
     p.is_bf16 = d.dtype == HT_BF16;
     p.grid = sm_count();
     p.cluster_k = 0;
@@ -1010,7 +1060,7 @@ int launch_attn_tc(const ht_attn_desc &d, const void *q, const void *kc, const v
     trace("ht_tree_attention -> %s kernel, %s, %d CTAs%s%s", pair_mode(d) ? "tile-pair" : "one-tile",
           k > 1 ? (k == 16 ? "clusters of 16" : (k == 8 ? (split == 2 ? "two clusters of 8 per unit" : "clusters of 8") : (k == 4 ? (split == 4 ? "four clusters of 4 per unit" : "clusters of 4") : "clusters of 2"))) : "persistent",
           p.grid, p.early ? ", early start" : "", needs_prepare(d, pages != nullptr) ? ", counters cleared by a kernel" : "");
-    if (pair_mode(d)) return launch_attn_tc_pair_kernel(tm_q, tm_k, tm_v, p, pp, d.dtype == HT_BF16, pages != nullptr, s);
+    if (pair_mode(d)) return launch_attn_tc_pair_kernel(tm_q, tm_k, tm_v, p, pp, d.dtype == HT_BF16, pages != nullptr, score != nullptr, s);
     e = ensure_smem_attr(sizeof(tc::Smem) + 1024);
     if (e != cudaSuccess) return fail(HT_ERR_CUDA, "cudaFuncSetAttribute: %s", cudaGetErrorString(e));
     // Few (sequence, KV head) units: one cluster of 16, 8, 4 or 2 CTAs per unit, parts reduced through
@@ -1030,7 +1080,7 @@ int launch_attn_tc(const ht_attn_desc &d, const void *q, const void *kc, const v
     attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = k > 1 ? 2 : 1;
-    e = cudaLaunchKernelEx(&cfg, attn_tc_fn(d.dtype == HT_BF16, pages != nullptr, k > 1), tm_q, tm_k, tm_v, p, pp);
+    e = cudaLaunchKernelEx(&cfg, attn_tc_fn(d.dtype == HT_BF16, pages != nullptr, k > 1, score != nullptr), tm_q, tm_k, tm_v, p, pp);
     if (e != cudaSuccess) {
         cudaGetLastError();
         return fail(HT_ERR_CUDA, "ht_tree_attention (tcgen05, clusters of %d): %s", k > 1 ? k : 1, cudaGetErrorString(e));

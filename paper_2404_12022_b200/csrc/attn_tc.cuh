@@ -40,6 +40,12 @@ struct Params {
     int cluster_split;     // clusters per unit: 1, or 2 (each reduces its half of the keys; the two results meet in the workspace)
     int wait_kcycles;      // how long a wait on an mbarrier may last, in units of 1024 clock cycles
     int early;             // HT_ATTN_CONTEXT_FINAL: lengths, trees and context rows may be read while the kernel ahead still runs
+    // The scored instantiations only (scale_log2 is 1 there: their scores are shaped into log2 units before the softmax):
+    float score_mul;       // with a cap: scale / cap; without: scale * log2(e)
+    float cap_log2;        // cap * log2(e); 0: no cap
+    const float *slopes;   // [Hq] or null: distance bias
+    const int32_t *pos;    // [B, N] position ids of the query rows (with slopes)
+    int near_keys;         // tiles reaching past context row kv_len - near_keys send P as a hi + lo pair
 };
 // The launch is serialized programmatically behind the kernel before it in the stream: a thread passes this point once
 // that kernel has completed and what it wrote is visible, and only then lets this kernel's own dependents be set up.
@@ -292,6 +298,98 @@ __device__ __forceinline__ unsigned long long add_f32x2(unsigned long long a, un
     unsigned long long d;
     asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
     return d;
+}
+
+// --- shaped scores (the scored instantiations): cap tanh(s / cap), then slope * (position of the key - of the row) ---
+// What a row's thread knows about its row.
+struct RowShape {
+    float slope;           // in log2 units; 0 without a distance bias
+    int pos;
+};
+__device__ __forceinline__ RowShape row_shape(const Params &p, bool real, int b, int node, int head) {
+    RowShape r{0.f, 0};
+    if (p.slopes && real) {
+        r.slope = p.slopes[head] * 1.4426950408889634f;
+        r.pos = p.pos[(size_t)b * p.N + node];
+    }
+    return r;
+}
+__device__ __forceinline__ float rcp(float x) {
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+// 32 raw products q . k of keys key0, ... of a sequence with L context rows -> scores in log2 units.
+// tanh t by its series to t^11 while all 32 x 32 values of the warp stay within 1/2 (the next term: 4e-7): seven fp32
+// operations, paired, against two of the special-function unit (each worth eight) for 1 - 2 / (1 + e^2t) -- which in
+// turn loses all digits at small t, so that a lane takes the series' result there as well.
+__device__ __forceinline__ void shape_scores(const Params &p, float *x, int key0, int L, int b, const RowShape row) {
+    if (p.cap_log2 > 0.f) {
+        const float mul = p.score_mul, cap = p.cap_log2;
+        float mx = 0.f;
+#pragma unroll
+        for (int c = 0; c < 32; c += 2) mx = max3(mx, fabsf(x[c]), fabsf(x[c + 1]));
+        const bool small = mx * mul <= 0.5f;                 // (false for NaN in a masked place: that lane's values take the general form)
+        const unsigned long long mul2 = pack_f32x2(mul, mul), cap2 = pack_f32x2(cap, cap), zero = pack_f32x2(0.f, 0.f);
+        const unsigned long long a11 = pack_f32x2(-1382.f / 155925.f, -1382.f / 155925.f), a9 = pack_f32x2(62.f / 2835.f, 62.f / 2835.f),
+                                 a7 = pack_f32x2(-17.f / 315.f, -17.f / 315.f), a5 = pack_f32x2(2.f / 15.f, 2.f / 15.f),
+                                 a3 = pack_f32x2(-1.f / 3.f, -1.f / 3.f);
+        auto series = [&](unsigned long long t) {            // cap * tanh t
+            const unsigned long long u = fma_f32x2(t, t, zero);
+            unsigned long long q = fma_f32x2(u, a11, a9);
+            q = fma_f32x2(q, u, a7);
+            q = fma_f32x2(q, u, a5);
+            q = fma_f32x2(q, u, a3);
+            const unsigned long long ct = fma_f32x2(t, cap2, zero);
+            return fma_f32x2(fma_f32x2(q, u, zero), ct, ct);
+        };
+        if (__all_sync(0xffffffffu, small)) {
+#pragma unroll
+            for (int c = 0; c < 32; c += 2) unpack_f32x2(series(fma_f32x2(pack_f32x2(x[c], x[c + 1]), mul2, zero)), x[c], x[c + 1]);
+        } else {
+#pragma unroll
+            for (int c = 0; c < 32; c += 2) {
+                const float t0 = x[c] * mul, t1 = x[c + 1] * mul;
+                float s0, s1;
+                unpack_f32x2(series(pack_f32x2(t0, t1)), s0, s1);
+                const float g0 = fmaf(-2.f * cap, rcp(1.f + ex2(t0 * 2.8853900817779268f)), cap);
+                const float g1 = fmaf(-2.f * cap, rcp(1.f + ex2(t1 * 2.8853900817779268f)), cap);
+                x[c] = fabsf(t0) <= 0.5f ? s0 : g0;
+                x[c + 1] = fabsf(t1) <= 0.5f ? s1 : g1;
+            }
+        }
+    } else {
+        const unsigned long long mul2 = pack_f32x2(p.score_mul, p.score_mul), zero = pack_f32x2(0.f, 0.f);
+#pragma unroll
+        for (int c = 0; c < 32; c += 2) unpack_f32x2(fma_f32x2(pack_f32x2(x[c], x[c + 1]), mul2, zero), x[c], x[c + 1]);
+    }
+    if (p.slopes) {
+        if (key0 + 32 <= L) {                                // context keys: position = row
+            const float first = row.slope * (float)(key0 - row.pos);
+#pragma unroll
+            for (int c = 0; c < 32; ++c) x[c] += fmaf(row.slope, (float)c, first);
+        } else {
+            const int32_t *pos = p.pos + (size_t)b * p.N;
+#pragma unroll
+            for (int c = 0; c < 32; ++c) {
+                const int cc = key0 + c - L;
+                const int at = cc < 0 ? key0 + c : (cc < p.N ? pos[cc] : row.pos);
+                x[c] = fmaf(row.slope, (float)(at - row.pos), x[c]);
+            }
+        }
+    }
+}
+// Scores of tree keys the row must not see, and of the tail, become -inf (context visible; `anc`: the row's ancestor
+// words, `stride` apart).
+__device__ __forceinline__ void mask_scores(float *x, int key0, int L, const uint32_t *anc, int stride, int words) {
+    const int cc0 = key0 - L;
+    if (cc0 <= -32) return;
+    const int wi = cc0 >> 5, sh = cc0 & 31;                  // arithmetic shift: -1 for cc0 in (-32, 0)
+    const uint32_t lo = wi < 0 ? 0xFFFFFFFFu : (wi < words ? anc[wi * stride] : 0u);
+    const uint32_t hi = (wi + 1 >= 0 && wi + 1 < words) ? anc[(wi + 1) * stride] : 0u;
+    const uint32_t vis = __funnelshift_r(lo, hi, sh);
+#pragma unroll
+    for (int c = 0; c < 32; ++c) x[c] = ((vis >> c) & 1u) ? x[c] : -INFINITY;
 }
 
 __device__ __forceinline__ void softmax_groups_sync() {   // the 256 softmax threads

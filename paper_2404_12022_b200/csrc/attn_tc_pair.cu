@@ -137,7 +137,8 @@ __device__ __noinline__ void cluster_merge_pair(const Params &p, const unsigned 
 }
 
 
-template <bool kBf16, bool kPaged, bool kSplit>
+// kScored: scores capped or biased by distance before the softmax (shape_scores).
+template <bool kBf16, bool kPaged, bool kSplit, bool kScored = false>
 __global__ void __launch_bounds__(kPThreads, 1)
 attn_tc_pair_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
                     const __grid_constant__ CUtensorMap tm_v, const Params p, const PagedParams pp) {
@@ -404,7 +405,7 @@ attn_tc_pair_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                         if (pend) issue_pv();
                         pend = true;
                         pend_first = (i == 0 && h == 0);
-                        pend_tree = key_hi + h * kHalf > L;
+                        pend_tree = key_hi + h * kHalf > L - (kScored ? p.near_keys : 0);
                         pend_h = h;
                         pend_slot = v_slot;
                         pend_ph = v_ph;
@@ -486,6 +487,8 @@ attn_tc_pair_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                 cu.c_hi = (cu.t0 + sg.nkt - 1) / per;
             }
 
+            RowShape shape{0.f, 0};
+            if constexpr (kScored) shape = row_shape(p, real, sg.b, node, sg.hk * p.g + row % p.g);
             float m_ref = -INFINITY, l_sum = 0.f;
             int last_h = -1;                            // score buffer of this stream's latest P V in this segment
             if (active) {
@@ -503,7 +506,7 @@ attn_tc_pair_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                     const uint32_t s_addr = tmem + lane_base + s * 128 + h * kHalf;
                     const int key_lo = kt * kTile + h * kHalf;
                     if (warp_real) {
-                    if (key_lo + kHalf > L) {
+                    if (!kScored && key_lo + kHalf > L) {
                         // Reaches into the tree rows / the tail: scores of keys this row must not see
                         // become -inf in place (context visible, tree key c iff ancestor bit c, tail never).
 #pragma unroll 1
@@ -528,6 +531,12 @@ attn_tc_pair_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                     tmem_ld32(s_addr, xa);
                     tmem_ld32(s_addr + 32, xb);
                     tmem_ld_wait();
+                    if constexpr (kScored) {                // shaped and masked in registers
+                        shape_scores(p, xa, key_lo, L, sg.b, shape);
+                        mask_scores(xa, key_lo, L, &sm.anc[s * words * kRows + row], kRows, words);
+                        shape_scores(p, xb, key_lo + 32, L, sg.b, shape);
+                        mask_scores(xb, key_lo + 32, L, &sm.anc[s * words * kRows + row], kRows, words);
+                    }
 #pragma unroll
                     for (int c = 0; c < 32; c += 4) {
                         mx0 = max3(mx0, xa[c], xa[c + 1]);
@@ -574,7 +583,7 @@ attn_tc_pair_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                     // to the tensor pipe as a pair hi + lo of 16-bit values: a second sweep forms the same exponentials
                     // again and stores what the rounding took away 32 columns further (all 64 scores are in registers,
                     // so the buffer's upper half is free), and P V is issued for both.
-                    const bool hi_lo = key_lo + kHalf > L;
+                    const bool hi_lo = key_lo + kHalf > L - (kScored ? p.near_keys : 0);
                     auto chunk = [&](const float *x, uint32_t col) {
                         uint32_t r[16];
 #pragma unroll
@@ -807,13 +816,17 @@ attn_tc_pair_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
 
 // Raises the kernels' dynamic shared memory limit (once per device) and launches.
 int launch_attn_tc_pair_kernel(const CUtensorMap &tm_q, const CUtensorMap &tm_k, const CUtensorMap &tm_v, const tc::Params &p,
-                               const tc::PagedParams &pp, bool bf16, bool paged, cudaStream_t s) {
+                               const tc::PagedParams &pp, bool bf16, bool paged, bool scored, cudaStream_t s) {
     typedef void (*Fn)(const CUtensorMap, const CUtensorMap, const CUtensorMap, const tc::Params, const tc::PagedParams);
-    const Fn fns[8] = {tc::attn_tc_pair_kernel<false, false, false>, tc::attn_tc_pair_kernel<true, false, false>,
+    const Fn fns[16] = {tc::attn_tc_pair_kernel<false, false, false>, tc::attn_tc_pair_kernel<true, false, false>,
                        tc::attn_tc_pair_kernel<false, true, false>,  tc::attn_tc_pair_kernel<true, true, false>,
                        tc::attn_tc_pair_kernel<false, false, true>,  tc::attn_tc_pair_kernel<true, false, true>,
-                       tc::attn_tc_pair_kernel<false, true, true>,   tc::attn_tc_pair_kernel<true, true, true>};
-    const Fn fn = fns[(bf16 ? 1 : 0) + (paged ? 2 : 0) + (p.cluster_split > 1 ? 4 : 0)];
+                       tc::attn_tc_pair_kernel<false, true, true>,   tc::attn_tc_pair_kernel<true, true, true>,
+                       tc::attn_tc_pair_kernel<false, false, false, true>, tc::attn_tc_pair_kernel<true, false, false, true>,
+                       tc::attn_tc_pair_kernel<false, true, false, true>,  tc::attn_tc_pair_kernel<true, true, false, true>,
+                       tc::attn_tc_pair_kernel<false, false, true, true>,  tc::attn_tc_pair_kernel<true, false, true, true>,
+                       tc::attn_tc_pair_kernel<false, true, true, true>,   tc::attn_tc_pair_kernel<true, true, true, true>};
+    const Fn fn = fns[(bf16 ? 1 : 0) + (paged ? 2 : 0) + (p.cluster_split > 1 ? 4 : 0) + (scored ? 8 : 0)];
     static bool done[64];
     const size_t smem_max = sizeof(tc::PSmem) + 1024;
     const size_t smem = offsetof(tc::PSmem, anc) + (size_t)2 * ((p.N + 31) / 32) * tc::kRows * sizeof(uint32_t) + 1024;
@@ -821,7 +834,7 @@ int launch_attn_tc_pair_kernel(const CUtensorMap &tm_q, const CUtensorMap &tm_k,
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return fail(HT_ERR_CUDA, "cudaGetDevice: %s", cudaGetErrorString(e));
     if (!(dev >= 0 && dev < 64 && done[dev])) {
-        for (int i = 0; i < 8 && e == cudaSuccess; ++i) {
+        for (int i = 0; i < 16 && e == cudaSuccess; ++i) {
             e = cudaFuncSetAttribute(fns[i], cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_max);
             if (e == cudaSuccess) e = cudaFuncSetAttribute(fns[i], cudaFuncAttributeNonPortableClusterSizeAllowed, 1);   // clusters of 16
         }

@@ -144,16 +144,25 @@ int ht_tree_attention_launches(const ht_attn_desc *user_desc) {
     return splits > 1 ? 2 : 1;
 }
 
-int ht_tree_attention(const ht_attn_desc *user_desc, const void *q, const void *k_cache, const void *v_cache,
-                      const int32_t *kv_len, const int32_t *parent, void *out, void *workspace,
-                      size_t workspace_bytes, int32_t *status, void *stream) {
-    Range range("ht_tree_attention");
+// A call's score descriptor, or null where nothing is to be shaped.
+static int check_score(const ht_score_desc **score) {
+    const ht_score_desc *s = *score;
+    if (!s) return HT_OK;
+    if (!(s->cap >= 0.f) || s->cap > 1e30f) return fail(HT_ERR_INVALID_ARG, "cap must be finite and not negative");
+    if (s->slopes && !s->pos) return fail(HT_ERR_INVALID_ARG, "slopes need pos");
+    if (s->cap == 0.f && !s->slopes) *score = nullptr;
+    return HT_OK;
+}
+
+static int tree_attention(const char *what, const ht_attn_desc *user_desc, const ht_score_desc *score, const void *q,
+                          const void *k_cache, const void *v_cache, const int32_t *kv_len, const int32_t *parent, void *out,
+                          void *workspace, size_t workspace_bytes, int32_t *status, void *stream) {
     int rc = check_attn_desc(user_desc);
     if (rc != HT_OK) return rc;
     const ht_attn_desc d = with_knobs(*user_desc), *desc = &d;
-    trace("ht_tree_attention B=%d N=%d Hq=%d Hkv=%d D=%d cap=%d dtype=%d splits=%d flags=0x%x -> %s", desc->B, desc->N, desc->Hq,
-          desc->Hkv, desc->D, desc->cap, desc->dtype, desc->num_splits, desc->flags,
-          attn_tc_applicable(*desc) ? "tcgen05" : "simt");
+    trace("%s B=%d N=%d Hq=%d Hkv=%d D=%d cap=%d dtype=%d splits=%d flags=0x%x%s%s -> %s", what, desc->B, desc->N, desc->Hq,
+          desc->Hkv, desc->D, desc->cap, desc->dtype, desc->num_splits, desc->flags, score && score->cap > 0.f ? " capped" : "",
+          score && score->slopes ? " biased" : "", attn_tc_applicable(*desc) ? "tcgen05" : "simt");
     if (desc->B == 0 || desc->N == 0) return HT_OK;
     if (!q || !k_cache || !v_cache || !kv_len || !parent || !out || !status)
         return fail(HT_ERR_INVALID_ARG, "NULL pointer");
@@ -165,17 +174,34 @@ int ht_tree_attention(const ht_attn_desc *user_desc, const void *q, const void *
         return fail(HT_ERR_WORKSPACE, "workspace holds %zu bytes, %zu needed", workspace ? workspace_bytes : 0, need);
     if (attn_tc_applicable(*desc))
         return launch_attn_tc(*desc, q, k_cache, v_cache, kv_len, parent, out, workspace, workspace_bytes, status,
-                              static_cast<cudaStream_t>(stream));
+                              static_cast<cudaStream_t>(stream), nullptr, nullptr, score);
     return launch_attn_simt(*desc, q, k_cache, v_cache, kv_len, parent, out, workspace, workspace_bytes,
-                            status, static_cast<cudaStream_t>(stream));
+                            status, static_cast<cudaStream_t>(stream), score);
 }
 
-int ht_tree_attention_paged(const ht_attn_desc *desc, const ht_paged_desc *pages, const void *q, const void *k_pages,
-                            const void *v_pages, const int32_t *block_table, const int32_t *kv_len,
-                            const int32_t *parent, void *out, void *workspace, size_t workspace_bytes,
-                            int32_t *status, void *stream) {
-    Range range("ht_tree_attention_paged");
-    if (desc && pages) trace("ht_tree_attention_paged B=%d N=%d Hq=%d Hkv=%d D=%d page_size=%d max_pages=%d n_pages=%d dtype=%d flags=0x%x", desc->B, desc->N, desc->Hq, desc->Hkv, desc->D, pages->page_size, pages->max_pages, pages->n_pages, desc->dtype, desc->flags);
+int ht_tree_attention(const ht_attn_desc *user_desc, const void *q, const void *k_cache, const void *v_cache,
+                      const int32_t *kv_len, const int32_t *parent, void *out, void *workspace,
+                      size_t workspace_bytes, int32_t *status, void *stream) {
+    Range range("ht_tree_attention");
+    return tree_attention("ht_tree_attention", user_desc, nullptr, q, k_cache, v_cache, kv_len, parent, out, workspace,
+                          workspace_bytes, status, stream);
+}
+
+int ht_tree_attention_scored(const ht_attn_desc *user_desc, const ht_score_desc *score, const void *q, const void *k_cache,
+                             const void *v_cache, const int32_t *kv_len, const int32_t *parent, void *out, void *workspace,
+                             size_t workspace_bytes, int32_t *status, void *stream) {
+    Range range("ht_tree_attention_scored");
+    const int rc = check_score(&score);
+    if (rc != HT_OK) return rc;
+    return tree_attention("ht_tree_attention_scored", user_desc, score, q, k_cache, v_cache, kv_len, parent, out, workspace,
+                          workspace_bytes, status, stream);
+}
+
+static int tree_attention_paged(const char *what, const ht_attn_desc *desc, const ht_paged_desc *pages, const ht_score_desc *score,
+                                const void *q, const void *k_pages, const void *v_pages, const int32_t *block_table,
+                                const int32_t *kv_len, const int32_t *parent, void *out, void *workspace, size_t workspace_bytes,
+                                int32_t *status, void *stream) {
+    if (desc && pages) trace("%s B=%d N=%d Hq=%d Hkv=%d D=%d page_size=%d max_pages=%d n_pages=%d dtype=%d flags=0x%x", what, desc->B, desc->N, desc->Hq, desc->Hkv, desc->D, pages->page_size, pages->max_pages, pages->n_pages, desc->dtype, desc->flags);
     if (!desc || !pages) return fail(HT_ERR_INVALID_ARG, "NULL descriptor");
     const int ps = pages->page_size;
     if (ps < 16 || (ps & (ps - 1)) != 0) return fail(HT_ERR_INVALID_ARG, "page_size must be a power of two >= 16");
@@ -204,7 +230,27 @@ int ht_tree_attention_paged(const ht_attn_desc *desc, const ht_paged_desc *pages
     if (need > 0 && (!workspace || workspace_bytes < need))
         return fail(HT_ERR_WORKSPACE, "workspace holds %zu bytes, %zu needed", workspace ? workspace_bytes : 0, need);
     return launch_attn_tc(d, q, k_pages, v_pages, kv_len, parent, out, workspace, workspace_bytes, status,
-                          static_cast<cudaStream_t>(stream), pages, block_table);
+                          static_cast<cudaStream_t>(stream), pages, block_table, score);
+}
+
+int ht_tree_attention_paged(const ht_attn_desc *desc, const ht_paged_desc *pages, const void *q, const void *k_pages,
+                            const void *v_pages, const int32_t *block_table, const int32_t *kv_len,
+                            const int32_t *parent, void *out, void *workspace, size_t workspace_bytes,
+                            int32_t *status, void *stream) {
+    Range range("ht_tree_attention_paged");
+    return tree_attention_paged("ht_tree_attention_paged", desc, pages, nullptr, q, k_pages, v_pages, block_table, kv_len, parent, out,
+                                workspace, workspace_bytes, status, stream);
+}
+
+int ht_tree_attention_scored_paged(const ht_attn_desc *desc, const ht_paged_desc *pages, const ht_score_desc *score, const void *q,
+                                   const void *k_pages, const void *v_pages, const int32_t *block_table, const int32_t *kv_len,
+                                   const int32_t *parent, void *out, void *workspace, size_t workspace_bytes, int32_t *status,
+                                   void *stream) {
+    Range range("ht_tree_attention_scored_paged");
+    const int rc = check_score(&score);
+    if (rc != HT_OK) return rc;
+    return tree_attention_paged("ht_tree_attention_scored_paged", desc, pages, score, q, k_pages, v_pages, block_table, kv_len, parent,
+                                out, workspace, workspace_bytes, status, stream);
 }
 
 int ht_verify_greedy(const void *logits, int dtype, const int32_t *tokens, const int32_t *parent,

@@ -101,7 +101,8 @@ inline PageMap make_page_map(const ht_paged_desc *pg, const int32_t *table, int 
     return m;
 }
 
-// Entry points of the individual kernels' host launchers (defined in the .cu files).
+// Entry points of the individual kernels' host launchers (defined in the .cu files).  `score` (where not null: a cap or
+// slopes are given) shapes the scores of an attention call.
 int launch_transfer(const void *h, const void *W, void *out, int B, int k, int d, int dtype, cudaStream_t s);
 bool transfer_tc_applicable(int B, int k, int d, int dtype);
 int transfer_tc_tile(int B, int R, int sms);
@@ -109,14 +110,15 @@ int launch_transfer_tc(const void *h, const void *W, void *out, int B, int k, in
 size_t attn_simt_workspace(const ht_attn_desc &d, int *splits_out);
 int launch_attn_simt(const ht_attn_desc &d, const void *q, const void *kc, const void *vc,
                      const int32_t *kv_len, const int32_t *parent, void *out, void *ws, size_t ws_bytes,
-                     int32_t *status, cudaStream_t s);
+                     int32_t *status, cudaStream_t s, const ht_score_desc *score = nullptr);
 bool attn_tc_applicable(const ht_attn_desc &d);
 size_t attn_tc_workspace(const ht_attn_desc &d);
 int attn_tc_launches(const ht_attn_desc &d);      // kernels one call enqueues (contiguous cache)
 // `pages` / `block_table` null: contiguous cache (kc, vc as in ht_tree_attention); else the page pools.
 int launch_attn_tc(const ht_attn_desc &d, const void *q, const void *kc, const void *vc, const int32_t *kv_len,
                    const int32_t *parent, void *out, void *ws, size_t ws_bytes, int32_t *status, cudaStream_t s,
-                   const ht_paged_desc *pages = nullptr, const int32_t *block_table = nullptr);
+                   const ht_paged_desc *pages = nullptr, const int32_t *block_table = nullptr,
+                   const ht_score_desc *score = nullptr);
 struct CompactArgs;
 // rows: logits rows per sequence whose argmax is taken (T <= rows <= N); compact: the compaction to run in the same
 // launch, or null.

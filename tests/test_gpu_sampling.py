@@ -1,0 +1,254 @@
+"""Sampling and sampled verification on the GPU against the fp64 oracle: tokens are whole numbers and have to be equal."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import sample_oracle as so
+
+pytestmark = pytest.mark.gpu
+DT = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
+
+
+@pytest.fixture(scope="module")
+def hb():
+    if not torch.cuda.is_available():
+        pytest.skip("no CUDA device")
+    from paper_2404_12022_b200 import binding
+    binding.load()
+    return binding
+
+
+def dev(a, t=torch.float32):
+    return None if a is None else torch.as_tensor(np.asarray(a), dtype=t).cuda()
+
+
+def check(hb, x, u, T=None, k=None, p=None, m=None, what=""):
+    """x [B, N, V] CUDA logits, u [B, N]."""
+    got, st = hb.sample(x, dev(u), dev(T), dev(k, torch.int32), dev(p), dev(m))
+    f = lambda a: None if a is None else np.asarray(a, np.float32).astype(np.float64)   # noqa: E731
+    want = so.sample(x.double().cpu().numpy(), f(u), f(T), k, f(p), f(m))
+    assert (st == 0).all()
+    assert np.array_equal(got.cpu().numpy(), want), "%s: %s" % (what, np.argwhere(got.cpu().numpy() != want)[:5])
+
+
+def logits(seed, dt, B, N, V, spread=2.0, boost=8.0):
+    g = torch.Generator().manual_seed(seed)
+    x = spread * torch.randn((B, N, V), generator=g)
+    at = torch.randint(0, V, (B, N, 1), generator=g)
+    x.scatter_add_(2, at, boost * torch.rand((B, N, 1), generator=g))
+    return x.to(dt).cuda(), torch.rand((B, N), generator=g).numpy()
+
+
+FILTERS = [dict(), dict(T=0.7), dict(k=1), dict(k=2), dict(k=50), dict(k=600), dict(p=0.1), dict(p=0.5), dict(p=0.95), dict(p=0.999),
+           dict(m=0.05), dict(k=40, p=0.9), dict(k=700, p=0.9), dict(k=700, p=0.97, m=0.01, T=1.3), dict(p=0.8, m=0.1), dict(T=0.05),
+           dict(T=0.05, k=100), dict(T=0.02, k=600, p=0.9), dict(T=20.0, p=0.6), dict(T=0.0, p=0.3)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("V", [1, 2, 7, 1000, 5003])
+@pytest.mark.parametrize("kw", FILTERS, ids=lambda k: "_".join("%s%g" % i for i in k.items()) or "none")
+def test_tokens_are_those_of_the_oracle(hb, dtype, V, kw):
+    B, N = 3, 4
+    x, u = logits(41, DT[dtype], B, N, V)
+    check(hb, x, u, **{n: [v] * B for n, v in kw.items()}, what=str(kw))
+
+
+@pytest.mark.parametrize("dtype,V", [("bf16", 32000), ("f32", 70001), ("f16", 120007), ("bf16", 200001)])
+@pytest.mark.parametrize("spread", [0.5, 2.5])
+def test_large_vocabularies_each_sequence_with_its_own_parameters(hb, dtype, V, spread):
+    """Rows in shared memory and rows too long for it, flat and peaked, long nuclei and short ones."""
+    x, u = logits(42, DT[dtype], 6, 1, V, spread, 6 * spread)
+    check(hb, x, u, T=[1.0, 0.6, 1.4, 0.0, 0.8, 1.0], k=[0, 50, 3000, 5, -1, V], p=[0.9, 0.95, 0.99, 1.0, 1.5, 0.3], m=[0.0, 0.0, 0.01, 0.5, 0.001, -1.0])
+
+
+def test_uniform_numbers_at_the_ends(hb):
+    x, _ = logits(43, torch.float32, 2, 3, 400, 3.0)
+    u = np.array([[0.0, 1.0, np.nextafter(np.float32(1), np.float32(0))]] * 2, np.float32)
+    for kw in (dict(), dict(k=[5, 5]), dict(p=[0.9, 0.9]), dict(m=[0.2, 0.2]), dict(T=[0.01, 0.01]), dict(k=[600, 390], p=[0.99, 0.99])):
+        check(hb, x, u, **kw)
+
+
+def test_weights_far_below_the_largest_still_count(hb):
+    """With uniform 0 the first token of any weight is the answer, down to 2^-1000 of the largest and not below."""
+    x = torch.full((3, 1, 900), -float("inf"))
+    x[:, 0, 700] = 0.0
+    x[0, 0, 3], x[1, 0, 3], x[2, 0, 3] = -500.0, -690.0, -700.0
+    x = x.cuda()
+    check(hb, x, np.zeros((3, 1)))
+    got, _ = hb.sample(x, torch.zeros((3, 1), device="cuda"))
+    assert got.flatten().tolist() == [3, 3, 700]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("V", [6, 3000, 40003])
+def test_rows_of_equal_logits_and_of_few_values(hb, dtype, V):
+    """Ties far beyond what the list of candidates holds: the cut runs through equal tokens, by index."""
+    B = 8
+    x = torch.zeros((B, 2, V))
+    g = torch.Generator().manual_seed(4)
+    x[:, 1] = torch.randint(-2, 2, (B, V), generator=g).float()
+    x[4:, 0] = -3.5
+    u = torch.rand((B, 2), generator=g).numpy()
+    check(hb, x.to(DT[dtype]).cuda(), u, p=[0.5, 0.9, 0.25, 1.0] * 2, k=[0, 0, 2000, 1500, 5, 700, 0, 0])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_nan_infinities_masks_and_signed_zeros(hb, dtype):
+    dt, V, inf, nan = DT[dtype], 1500, float("inf"), float("nan")
+    g = torch.Generator().manual_seed(9)
+    x = torch.randn((12, 1, V), generator=g)
+    x[0] = nan
+    x[1] = -inf
+    x[2, 0] = nan
+    x[2, 0, 40:] = -inf
+    x[3, 0, ::3] = nan
+    x[4, 0, ::2] = -inf
+    x[5, 0, 100], x[5, 0, 900] = inf, inf
+    x[6, 0, 5:] = torch.finfo(dt).min                                                   # a mask of the type's lowest value
+    x[7] = torch.finfo(dt).min
+    x[8, 0] = 0.0
+    x[8, 0, ::2] = -0.0
+    x[9, 0, 1:] = -inf
+    x[10, 0, 100], x[10, 0, 3], x[10, 0, 4] = inf, nan, -inf
+    x = x.to(dt).cuda()
+    for seed in range(4):
+        u = np.random.default_rng(seed).random((12, 1)).astype(np.float32)
+        for kw in (dict(), dict(k=[600] * 12), dict(k=[3] * 12), dict(p=[0.7] * 12), dict(T=[0.0] * 12), dict(m=[0.3] * 12), dict(k=[20] * 12, p=[0.9] * 12)):
+            check(hb, x, u, **kw, what=str(kw))
+
+
+def test_cuts_among_tokens_far_below_the_largest(hb):
+    """The k-th token, or the end of a nucleus of 1 - 1e-7, lies below 2^-32 of the largest weight."""
+    g = torch.Generator().manual_seed(12)
+    x = torch.randn((6, 1, 4000), generator=g)
+    x[:, 0, 17] = 60.0
+    u = np.array([[0.5], [1.0], [0.9999999], [0.3], [1.0], [0.99999994]], np.float32)
+    check(hb, x.cuda(), u, k=[700, 700, 2000, 0, 0, 0], p=[1.0, 0.9, 1.0, 0.9999999, 0.99999994, 0.9999])
+
+
+def test_bad_parameters_are_flagged(hb):
+    B, nan, inf = 9, float("nan"), float("inf")
+    x, _ = logits(44, torch.float16, B, 2, 300)
+    u = np.full((B, 2), 0.4, np.float32)
+    u[6, 1], u[7, 0], u[8, 1] = -0.1, 1.5, nan
+    T = np.array([1, -1, inf, nan, 1, 1, 1, 1, 1], np.float32)
+    p, m = np.full(B, 0.9, np.float32), np.zeros(B, np.float32)
+    p[4], m[5] = nan, 1.5
+    got, st = hb.sample(x, dev(u), dev(T), None, dev(p), dev(m))
+    assert st.tolist() == [0] + [hb.HT_STATUS_BAD_PARAM] * 8
+    assert (got[1:] == -1).all() and (got[0] >= 0).all()
+
+
+def test_frequencies_over_many_uniform_numbers(hb):
+    """20000 draws from one row: each frequency within five standard deviations of its probability (inputs fixed)."""
+    n, V = 20000, 16
+    x = torch.randn(V, generator=torch.Generator().manual_seed(2))
+    u = (torch.arange(n, dtype=torch.float32) + 0.5) / n                                 # evenly spread: counts within one of n p
+    got, _ = hb.sample(x.expand(1, n, V).contiguous().cuda(), u[None].cuda())
+    p = torch.softmax(x.double(), 0)
+    assert ((torch.bincount(got.flatten().cpu(), minlength=V) - n * p).abs() <= 1.01).all()
+
+
+# ---------------------------------------------------------------------------------------------------------------------
+def trees(rng, B, T, N):
+    parent = np.full((B, N), -1, np.int32)
+    for b in range(B):
+        for r in range(1, N):
+            parent[b, r] = rng.integers(max(-1, r - 6), r)
+    return parent
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("shape", [(1, 1, 1, 50), (2, 15, 18, 64), (3, 88, 91, 300), (2, 300, 300, 40), (2, 20, 23, 32003)],
+                         ids=lambda s: "B%dT%dN%dV%d" % s)
+@pytest.mark.parametrize("root", [True, False])
+def test_sampled_verification_is_sampling_and_the_path_search(hb, oracle, dtype, shape, root):
+    B, T, N, V = shape
+    rng = np.random.default_rng(7)
+    x, u = logits(45, DT[dtype], B, N, V, 2.0, 20.0)
+    parent = trees(rng, B, T, N)
+    f64 = lambda a: np.asarray(a, np.float32).astype(np.float64)                        # noqa: E731
+    Tm, k, p = [0.9] * B, [30] * B, [0.9] * B
+    pred = np.full((B, N), -1, np.int32)
+    pred[:, :T] = so.sample(x.double().cpu().numpy()[:, :T], f64(u), f64(Tm), k, f64(p))
+    # drafts that follow the samples with probability 0.7, so that paths of several nodes are accepted
+    root_pred = rng.integers(0, V, B).astype(np.int32)
+    tokens = rng.integers(0, V, (B, T)).astype(np.int32)
+    for b in range(B):
+        for c in range(T):
+            if rng.random() < 0.7:
+                tokens[b, c] = root_pred[b] if parent[b, c] < 0 else pred[b, parent[b, c]]
+    accept_len = torch.zeros(B, dtype=torch.int32, device="cuda")
+    for _ in range(2):                                                                  # the second call starts from the first one's lengths
+        got = hb.verify_sampled(x, dev(u), dev(tokens, torch.int32), dev(parent, torch.int32), dev(root_pred, torch.int32) if root else None,
+                                dev(Tm), dev(k, torch.int32), dev(p), max_path=64, accept_len=accept_len)
+        want = oracle.accept_scan(tokens, parent, pred, root_pred if root else None, 64)
+        assert np.array_equal(got[0].cpu().numpy(), pred)
+        for g, w, name in zip(got[1:], want, ("accept_len", "accept_path", "next_token", "status")):
+            assert np.array_equal(g.cpu().numpy(), w), name
+
+
+def test_greedy_temperature_is_the_greedy_verification(hb):
+    B, T, N, V = 3, 60, 64, 5000
+    x, u = logits(46, torch.bfloat16, B, N, V)
+    parent = dev(trees(np.random.default_rng(3), B, T, N), torch.int32)
+    greedy = x.float().argmax(-1).int()
+    tokens = torch.gather(greedy, 1, parent[:, :T].clamp(min=0).long()).contiguous()
+    a = hb.verify_greedy(x, tokens, parent, greedy[:, 0].contiguous(), 64)
+    b = hb.verify_sampled(x, dev(u), tokens, parent, greedy[:, 0].contiguous(), temperature=torch.zeros(B, device="cuda"), max_path=64)
+    assert torch.equal(a[0][:, :T], b[0][:, :T]) and all(torch.equal(p, q) for p, q in zip(a[1:], b[1:]))
+
+
+def test_statuses_of_sampled_verification(hb):
+    B, T, V = 4, 12, 100
+    x, u = logits(47, torch.float32, B, T, V)
+    parent = np.tile(np.arange(-1, T - 1, dtype=np.int32), (B, 1))                       # chains
+    parent[1, 4] = 4
+    u[2, 7] = 2.0
+    pred = hb.sample(x, dev(np.clip(u, 0, 1)))[0]
+    tokens = torch.cat((torch.zeros((B, 1), dtype=torch.int32, device="cuda"), pred[:, :-1]), 1).contiguous()
+    got = hb.verify_sampled(x, dev(u), tokens, dev(parent, torch.int32), None, max_path=5)
+    assert got[4].tolist() == [4, 1, hb.HT_STATUS_BAD_PARAM, 4]
+    assert got[1].tolist() == [0] * 4 and got[3].tolist() == [-1] * 4 and (got[0][2] == -1).all() and (got[2][2] == -1).all()
+    u[2, 7] = 0.5
+    got = hb.verify_sampled(x, dev(u), tokens, dev(parent, torch.int32), None, max_path=12, accept_len=got[1])
+    assert got[4].tolist() == [0, 1, 0, 0] and got[1].tolist()[0] == T
+
+
+def test_captured_and_replayed_and_two_streams(hb, oracle):
+    B, T, V = 2, 40, 4000
+    sets = [logits(s, torch.bfloat16, B, T, V, 2.0, 15.0) for s in (50, 51, 52)]
+    x, u = sets[0][0].clone(), dev(sets[0][1])
+    parent = dev(trees(np.random.default_rng(1), B, T, T), torch.int32)
+    tokens = torch.randint(0, V, (B, T), generator=torch.Generator().manual_seed(0)).int().cuda()
+    p = torch.full((B,), 0.9, device="cuda")
+    alen = torch.zeros(B, dtype=torch.int32, device="cuda")
+    hb.verify_sampled(x, u, tokens, parent, None, top_p=p, accept_len=alen)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        out = hb.verify_sampled(x, u, tokens, parent, None, top_p=p, accept_len=alen)
+    for xs, us in sets[1:]:
+        x.copy_(xs)
+        u.copy_(dev(us))
+        graph.replay()
+        torch.cuda.synchronize()
+        want = so.sample(xs.double().cpu().numpy(), us.astype(np.float64), None, None, np.full(B, np.float32(0.9), np.float64))
+        assert np.array_equal(out[0].cpu().numpy(), want)
+    streams, got = [torch.cuda.Stream() for _ in range(2)], []
+    torch.cuda.synchronize()
+    for (xs, us), s in zip(sets[1:], streams):
+        with torch.cuda.stream(s):
+            got.append(hb.sample(xs, dev(us), top_p=p)[0])
+    torch.cuda.synchronize()
+    for (xs, us), t in zip(sets[1:], got):
+        assert np.array_equal(t.cpu().numpy(), so.sample(xs.double().cpu().numpy(), us.astype(np.float64), None, None,
+                                                         np.full(B, np.float32(0.9), np.float64)))
+
+
+def test_binding_refuses_what_it_cannot_pass_on(hb):
+    x, u = logits(48, torch.float16, 2, 3, 50)
+    for kw in (dict(u=dev(u)[:1]), dict(u=dev(u).double()), dict(T=torch.ones(3, device="cuda")), dict(k=torch.ones(2, device="cuda")), dict(T=torch.ones(2))):
+        with pytest.raises(ValueError):
+            hb.sample(x, kw.get("u", dev(u)), kw.get("T"), kw.get("k"))

@@ -1,0 +1,220 @@
+"""Tree attention with capped and distance-biased scores on the GPU against the fp64 oracle."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import scored_oracle as so
+
+pytestmark = pytest.mark.gpu
+DT = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
+
+
+@pytest.fixture(scope="module")
+def hb():
+    if not torch.cuda.is_available():
+        pytest.skip("no CUDA device")
+    from paper_2404_12022_b200 import binding
+    binding.load()
+    return binding
+
+
+def f64(t):
+    return t.double().cpu().numpy()
+
+
+def close(got, ref, what=""):
+    """ref: the result o and A, the sums of weight * |v|, by the oracle.
+    16-bit types: the tensor cores take the weights rounded to the type, each off by at most half a step, eps / 2 of itself
+    (their sum is held in 32 bits): eps / 2 * A in all; a float16 weight below the type's range is lost or off by half
+    its smallest step, which against the row's largest weight (at least 2^-8 of the running maximum's) is 2^-17 for all
+    keys at most in the tests' lengths; the result is rounded once, eps / 2 * |o|; the scores' 32-bit sums of 128 products
+    and the exponential move each weight by less than 2e-5 of itself.  Results of order one then differ by up to 6e-3 in
+    bfloat16: tighter than this no such kernel can be held to, looser no result is let through.
+    fp32: a score is a sum of 128 products (values to about 5 in all: rounding errors of 1e-6 at most in the mean square),
+    the cap adds cap * 2^-23 (below 1e-5 for caps to 80) and the exponential 2^-22; an output moves by the score's error
+    times a value spread of about one: 1e-5 (1 + |o|)."""
+    o, size = ref
+    g = f64(got)
+    half = torch.finfo(got.dtype).eps / 2
+    tol = 1e-5 * (1 + np.abs(o)) if got.dtype == torch.float32 else half * (size + np.abs(o)) + 2e-5 * size + 2.0 ** -17
+    bad = np.abs(g - o) > tol
+    assert not bad.any(), "%s: %d of %d off, worst %.3g" % (what, bad.sum(), bad.size, np.abs(g - o).max())
+
+
+def case(seed, dtype, B, N, Hq, Hkv, D, lens, spread=2.0, slope=None):
+    g = torch.Generator().manual_seed(seed)
+    rng = np.random.default_rng(seed)
+    dt = DT[dtype]
+    cap = max(lens) + N + 5
+    q = (spread * torch.randn((B, N, Hq, D), generator=g)).to(dt).cuda()
+    k, v = (torch.randn((B, Hkv, cap, D), generator=g).to(dt).cuda() for _ in range(2))
+    for b, L in enumerate(lens):                                                       # rows behind the tree are not data
+        k[b, :, L + N:] = float("nan")
+        v[b, :, L + N:] = float("inf")
+    parent = np.full((B, N), -1, np.int32)
+    depth = np.zeros((B, N), np.int32)
+    for b in range(B):
+        for r in range(1, N):
+            parent[b, r] = rng.integers(max(-1, r - 7), r)
+            depth[b, r] = depth[b, parent[b, r]] + 1 if parent[b, r] >= 0 else 0
+    pos = np.asarray(lens, np.int32)[:, None] + depth
+    slopes = 2.0 ** (-8.0 * np.arange(1, Hq + 1) / Hq) if slope is None else np.full(Hq, slope)
+    dev = lambda a, t: torch.as_tensor(np.asarray(a), dtype=t).cuda()                   # noqa: E731
+    return (q, k, v, dev(lens, torch.int32), dev(parent, torch.int32), dev(slopes, torch.float32), dev(pos, torch.int32))
+
+
+def reference(c, cap, bias):
+    q, k, v, lens, parent, slopes, pos = c
+    return so.tree_attention(f64(q), f64(k), f64(v), lens.cpu().numpy(), parent.cpu().numpy(), cap, f64(slopes) if bias else None,
+                             pos.cpu().numpy(), spread=True)
+
+
+def check(hb, c, cap, bias, **kw):
+    q, k, v, lens, parent, slopes, pos = c
+    out, st = hb.tree_attention_scored(q, k, v, lens, parent, cap=cap, slopes=slopes if bias else None, pos=pos if bias else None, **kw)
+    assert (st == 0).all()
+    close(out, reference(c, cap, bias), "cap %g bias %s" % (cap, bias))
+
+
+SHAPES = [(1, 1, 2, 2, 128, [0]), (1, 1, 4, 1, 128, [700]), (2, 18, 4, 4, 128, [130, 0]), (3, 40, 8, 2, 128, [127, 128, 333]),
+          (2, 91, 4, 4, 128, [1000, 64]), (1, 67, 16, 2, 128, [515]), (1, 200, 4, 2, 128, [256]), (2, 18, 4, 4, 64, [31, 97]),
+          (1, 24, 6, 2, 128, [200])]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("shape", SHAPES, ids=lambda s: "B%dN%dHq%dHkv%dD%d_%s" % (*s[:5], "_".join(map(str, s[5]))))
+@pytest.mark.parametrize("cap,bias", [(30.0, False), (0.0, True), (4.0, True)], ids=["cap", "bias", "both"])
+def test_scored_attention_against_the_oracle(hb, dtype, shape, cap, bias):
+    check(hb, case(21, dtype, *shape), cap, bias)
+
+
+@pytest.mark.parametrize("cap", [0.01, 1.0, 1000.0, 1e8])
+def test_caps_from_saturated_to_hardly_there(hb, cap):
+    """A cap of 0.01 flattens every score, one of 1e8 leaves them as they are (the series' result is taken there)."""
+    for dtype in ("f32", "bf16"):
+        c = case(22, dtype, 1, 30, 4, 2, 128, [300], spread=6.0)
+        if dtype == "f32" and cap > 1000:
+            continue                                  # tanhf's rounding times such a cap is what fp32 holds of the score
+        check(hb, c, cap, False)
+
+
+@pytest.mark.parametrize("slope", [3.0, 0.5, -0.01, 0.0])
+def test_steep_flat_and_negative_slopes(hb, slope):
+    for dtype in ("f16", "bf16", "f32"):
+        check(hb, case(23, dtype, 2, 40, 4, 4, 128, [384, 200], slope=slope), 0.0, True)
+    check(hb, case(24, "bf16", 1, 40, 16, 2, 128, [384], slope=slope), 0.0, True)
+
+
+def test_nothing_asked_for_is_the_plain_call_bit_for_bit(hb):
+    for shape in ((2, 18, 4, 4, 128, [130, 40]), (1, 67, 16, 2, 128, [515])):
+        c = case(25, "bf16", *shape)
+        a, _ = hb.tree_attention(*c[:5])
+        b, _ = hb.tree_attention_scored(*c[:5])
+        assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("shape", [(1, 19, 8, 8, 128, [9000]), (1, 67, 64, 8, 128, [9000]), (8, 19, 40, 40, 128, [600, 20, 900, 333, 128, 1, 700, 512]),
+                                   (4, 67, 16, 2, 128, [2000, 10, 1500, 800])], ids=lambda s: "B%dN%dHq%dHkv%d" % s[:4])
+@pytest.mark.parametrize("final", [False, True], ids=["plain", "promises"])
+def test_work_splits_clusters_and_promises(hb, shape, final):
+    """Units cut over CTAs, clusters of every size, the tile-pair kernel; with a kept workspace and the early start."""
+    c = case(26, "bf16", *shape)
+    q, k, v, lens, parent, slopes, pos = c
+    ws = torch.zeros(48 << 20, dtype=torch.uint8, device="cuda")
+    flags = (hb.HT_ATTN_WORKSPACE_CLEAN | hb.HT_ATTN_CONTEXT_FINAL) if final else 0
+    ref = reference(c, 30.0, True)
+    for _ in range(2):
+        out, st = hb.tree_attention_scored(q, k, v, lens, parent, cap=30.0, slopes=slopes, pos=pos, workspace=ws, flags=flags)
+        assert (st == 0).all()
+        close(out, ref)
+    plain, _ = hb.tree_attention(q, k, v, lens, parent, workspace=ws, flags=flags)       # the two forms share a workspace
+    close(plain, reference(c, 0.0, False))
+
+
+@pytest.mark.parametrize("splits", [1, 3, 8])
+def test_alu_kernel_splits(hb, splits):
+    check(hb, case(27, "f32", 1, 18, 4, 2, 64, [700]), 20.0, True, num_splits=splits)
+    check(hb, case(28, "f16", 1, 18, 4, 2, 128, [700]), 20.0, True, num_splits=splits)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("ps", [16, 64, 256])
+@pytest.mark.parametrize("shape", [(2, 18, 4, 4, 128, [130, 0]), (2, 67, 16, 2, 128, [515, 90])], ids=["one_tile", "tile_pair"])
+def test_paged_against_the_oracle(hb, dtype, ps, shape):
+    c = case(29, dtype, *shape)
+    q, k, v, lens, parent, slopes, pos = c
+    B, Hkv, cap, D = k.shape
+    per = -(-cap // ps)
+    table = torch.randperm(B * per + 2, generator=torch.Generator().manual_seed(3))[:B * per].int().view(B, per).cuda()
+    pools = []
+    for t in (k, v):
+        full = torch.full((B, Hkv, per * ps, D), float("nan"), dtype=t.dtype, device="cuda")
+        full[:, :, :cap] = t
+        pool = torch.full((B * per + 2, Hkv, ps, D), float("nan"), dtype=t.dtype, device="cuda")
+        pool[table.long().flatten()] = full.view(B, Hkv, per, ps, D).permute(0, 2, 1, 3, 4).reshape(-1, Hkv, ps, D)
+        pools.append(pool)
+    for cap_s, bias in ((30.0, False), (0.0, True), (10.0, True)):
+        out, st = hb.tree_attention_scored_paged(q, *pools, table, lens, parent, cap=cap_s, slopes=slopes if bias else None, pos=pos if bias else None)
+        assert (st == 0).all()
+        close(out, reference(c, cap_s, bias))
+
+
+def test_bad_sequences_are_flagged_and_left_alone(hb):
+    for dtype in ("f32", "bf16"):
+        c = case(30, dtype, 4, 18, 4, 4, 128, [100, 90, 80, 70])
+        q, k, v, lens, parent, slopes, pos = c
+        lens[1] = -1
+        lens[2] = k.shape[2] - 17
+        parent[3, 5] = 5
+        out = torch.full_like(q, 3.0)
+        _, st = hb.tree_attention_scored(q, k, v, lens, parent, cap=30.0, slopes=slopes, pos=pos, out=out)
+        assert st.tolist() == [0, 2, 2, 1]
+        assert (out[1:] == 3).all()
+        close(out[:1], [a[:1] for a in reference(c, 30.0, True)])
+
+
+def test_captured_and_replayed_with_new_slopes_and_positions(hb):
+    c = case(31, "bf16", 2, 18, 8, 8, 128, [300, 170])
+    q, k, v, lens, parent, slopes, pos = c
+    ws = torch.zeros(48 << 20, dtype=torch.uint8, device="cuda")
+    hb.tree_attention_scored(q, k, v, lens, parent, cap=30.0, slopes=slopes, pos=pos, workspace=ws)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph, out = torch.cuda.CUDAGraph(), torch.empty_like(q)
+    with torch.cuda.graph(graph, stream=side):
+        slopes.mul_(0.5)                                                                # the kernel ahead writes what the call reads
+        pos.add_(1)
+        hb.tree_attention_scored(q, k, v, lens, parent, cap=30.0, slopes=slopes, pos=pos, workspace=ws, out=out,
+                                 flags=hb.HT_ATTN_CONTEXT_FINAL)
+    for _ in range(3):
+        graph.replay()
+        torch.cuda.synchronize()
+        close(out, reference(c, 30.0, True))
+
+
+def test_calls_on_two_streams_with_their_own_workspaces(hb):
+    c1, c2 = case(32, "bf16", 2, 40, 8, 8, 128, [700, 900]), case(33, "bf16", 2, 67, 16, 2, 128, [700, 300])
+    streams, outs = [torch.cuda.Stream() for _ in range(2)], []
+    torch.cuda.synchronize()
+    for c, s in zip((c1, c2), streams):
+        with torch.cuda.stream(s):
+            for _ in range(5):
+                out, _ = hb.tree_attention_scored(*c[:5], cap=20.0, slopes=c[5], pos=c[6])
+            outs.append(out)
+    torch.cuda.synchronize()
+    for c, out in zip((c1, c2), outs):
+        close(out, reference(c, 20.0, True))
+
+
+def test_binding_refuses_what_it_cannot_pass_on(hb):
+    q, k, v, lens, parent, slopes, pos = case(34, "f16", 1, 4, 2, 2, 128, [8])
+    with pytest.raises(ValueError):
+        hb.tree_attention_scored(q, k, v, lens, parent, slopes=slopes)
+    with pytest.raises(ValueError):
+        hb.tree_attention_scored(q, k, v, lens, parent, slopes=slopes.double(), pos=pos)
+    with pytest.raises(ValueError):
+        hb.tree_attention_scored(q, k, v, lens, parent, slopes=slopes[:1], pos=pos)
+    with pytest.raises(ValueError):
+        hb.tree_attention_scored(q, k, v, lens, parent, slopes=slopes, pos=pos[:, :2])
+    with pytest.raises(hb.HtError):
+        hb.tree_attention_scored(q, k, v, lens, parent, cap=-1.0)

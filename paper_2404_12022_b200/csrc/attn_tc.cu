@@ -58,9 +58,10 @@ namespace tc {
 // weights to 16 bits is no longer averaged away): P goes to the tensor pipe as a pair hi + lo of 16-bit
 // values, P V is issued for both; chunk c's hi lands in columns [32 c, 32 c + 16) and its lo = P - hi in
 // [32 c + 16, 32 c + 32), i.e. every chunk's results take the chunk's own columns.
-template <bool kBf16, bool kHiLo>
+// kShaped: `shape(x, w)` turns the raw products of chunk w into exponents first.
+template <bool kBf16, bool kHiLo, bool kShaped, typename Shape>
 __device__ __forceinline__ void softmax_pass2(uint32_t s_addr, float *xa, float *xb, unsigned long long scale2,
-                                              unsigned long long nbase2, unsigned long long &acc2) {
+                                              unsigned long long nbase2, unsigned long long &acc2, Shape shape) {
     constexpr int kStep = kHiLo ? 32 : 16;             // columns a chunk's results take
     // 32 scores -> 16 packed pairs at column `col`; with kHiLo eight pairs at a time, each with what its rounding
     // took away (few registers: these tiles share the hot loop's allocation)
@@ -70,7 +71,8 @@ __device__ __forceinline__ void softmax_pass2(uint32_t s_addr, float *xa, float 
 #pragma unroll
             for (int c = 0; c < 16; ++c) {
                 float p0, p1;
-                unpack_f32x2(fma_f32x2(pack_f32x2(x[2 * c], x[2 * c + 1]), scale2, nbase2), p0, p1);
+                if (kShaped) { p0 = x[2 * c]; p1 = x[2 * c + 1]; }
+                else unpack_f32x2(fma_f32x2(pack_f32x2(x[2 * c], x[2 * c + 1]), scale2, nbase2), p0, p1);
                 p0 = ex2(p0);
                 p1 = ex2(p1);
                 acc2 = add_f32x2(acc2, pack_f32x2(p0, p1));
@@ -84,7 +86,8 @@ __device__ __forceinline__ void softmax_pass2(uint32_t s_addr, float *xa, float 
 #pragma unroll
                 for (int c = 0; c < 8; ++c) {
                     float p0, p1;
-                    unpack_f32x2(fma_f32x2(pack_f32x2(x[16 * half + 2 * c], x[16 * half + 2 * c + 1]), scale2, nbase2), p0, p1);
+                    if (kShaped) { p0 = x[16 * half + 2 * c]; p1 = x[16 * half + 2 * c + 1]; }
+                    else unpack_f32x2(fma_f32x2(pack_f32x2(x[16 * half + 2 * c], x[16 * half + 2 * c + 1]), scale2, nbase2), p0, p1);
                     p0 = ex2(p0);
                     p1 = ex2(p1);
                     acc2 = add_f32x2(acc2, pack_f32x2(p0, p1));
@@ -100,9 +103,11 @@ __device__ __forceinline__ void softmax_pass2(uint32_t s_addr, float *xa, float 
     for (int h = 0; h < 2; ++h) {
         tmem_ld_wait();
         tmem_ld32(s_addr + (2 * h + 1) * 32, xb);
+        if (kShaped) shape(xa, 2 * h);
         chunk(xa, s_addr + (2 * h) * kStep);
         tmem_ld_wait();
         if (h == 0) tmem_ld32(s_addr + 2 * 32, xa);
+        if (kShaped) shape(xb, 2 * h + 1);
         chunk(xb, s_addr + (2 * h + 1) * kStep);
     }
 }
@@ -116,8 +121,8 @@ __device__ __forceinline__ void fetch_q_tile(Smem &sm, const CUtensorMap &tm_q, 
 
 // kPaged: the cache is a pool of pages (separate instantiations, so that the contiguous kernels carry none of that code).
 // kClustered: launched as clusters (p.cluster_k > 1); a template parameter so that the persistent form carries no cluster code.
-// kScored: scores capped or biased by distance before the softmax (shape_scores).
-template <bool kBf16, bool kPaged, bool kClustered, bool kScored = false>
+// kShape: scores capped or biased by distance before the softmax (shape_scores); 0: neither.
+template <bool kBf16, bool kPaged, bool kClustered, int kShape = 0>
 __global__ void __launch_bounds__(kThreads, 1)
 attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
                const __grid_constant__ CUtensorMap tm_v, const Params p, const PagedParams pp) {
@@ -125,6 +130,7 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
     Smem &sm = *reinterpret_cast<Smem *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     volatile int *abort_flag = &sm.abort;
+    const bool from_end = (kShape & kShapeBias) && p.from_end;
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < kStages; ++i) { mbar_init(&sm.kv_full[i], 1); mbar_init(&sm.kv_empty[i], 1); }
@@ -206,7 +212,7 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
             cur_v.init(t_begin, t_end, first);
             cur_p.init(t_begin, t_end, first);
             if (kPaged)
-                for (int jt = 0; jt < kPgAhead; ++jt) pages_request(p, pp, sm.pre, sm.nkt, sm.pg, jt, cur_p, lane, 1);
+                for (int jt = 0; jt < kPgAhead; ++jt) pages_request(p, pp, sm.pre, sm.nkt, sm.pg, jt, cur_p, lane, 1, from_end);
             for (int e = 0; e < 2 * n; ++e) {
                 if (kPaged ? __any_sync(0xFFFFFFFFu, *abort_flag != 0) : (*abort_flag != 0)) break;
                 // entry e of the consumption order: K_0, K_1, V_0, K_2, V_1, ..., V_{n-1}
@@ -218,7 +224,7 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
                 s.b = is_v ? cur_v.s.b : cur_k.s.b;
                 s.hk = is_v ? cur_v.s.hk : cur_k.s.hk;
                 s.rt = is_v ? cur_v.s.rt : cur_k.s.rt;
-                const int kt = is_v ? cur_v.kt() : cur_k.kt();
+                const int kt = is_v ? cur_v.kt(from_end) : cur_k.kt(from_end);
                 if (!is_v && cur_k.first()) {
                     // first tile of a segment: its Q tile, once the previous segment's scores are done with Q
                     if (seg_i > 0) release();
@@ -239,7 +245,7 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
                 const CUtensorMap *tm = is_v ? &tm_v : &tm_k;
                 if (kPaged && !is_v) {
                     // the ids of tile j were asked for kPgAhead tiles ago; ask for those of tile j + kPgAhead
-                    pages_request(p, pp, sm.pre, sm.nkt, sm.pg, j + kPgAhead, cur_p, lane, 1);
+                    pages_request(p, pp, sm.pre, sm.nkt, sm.pg, j + kPgAhead, cur_p, lane, 1, from_end);
                     cp_async_wait<kPgAhead>();
                 }
                 if (lane == 0) mbar_expect_tx(&sm.kv_full[slot], kEntryBytes);
@@ -334,7 +340,7 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
                     advance(k_slot, k_ph, j == 0 ? 1 : 2);                    // K entries: 0, 1, 3, 5, ...
                     if (j > 0) issue_pv(j - 1, prev_first, prev_tree);
                     prev_first = i < 2;
-                    prev_tree = (sg.kt0 + i + 1) * kTile > L - (kScored ? p.near_keys : 0);
+                    prev_tree = (from_end ? sg.kt0 + sg.len - i : sg.kt0 + i + 1) * kTile > L - (kShape ? p.near_keys : 0);
                     ++j;
                 }
                 t += sg.len;
@@ -386,7 +392,8 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
             const bool real = node < p.N;
             // a warp none of whose 32 rows is a query row keeps step with the barriers but computes nothing
             const bool warp_real = sg.rt * p.rows_per_tile_nodes + (row & ~31) / p.g < p.N;
-            if (sg.b != anc_b || sg.rt != anc_rt) {
+            const bool new_rows = sg.b != anc_b || sg.rt != anc_rt;
+            if (new_rows) {
                 softmax_groups_sync();                 // previous segment no longer reads parent / anc
                 for (int c = tid256; c < p.N; c += 256) sm.parent[c] = p.parent[(size_t)sg.b * p.N + c];
                 softmax_groups_sync();
@@ -400,6 +407,14 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
                 anc_rt = sg.rt;
             }
             release();
+            // the tree rows' positions (which the kernel ahead may have written) take the place of the parents
+            float *const tree_pos = reinterpret_cast<float *>(sm.parent);
+            if constexpr ((kShape & kShapeBias) != 0) {
+                if (new_rows) {
+                    for (int c = tid256; c < p.N; c += 256) tree_pos[c] = (float)(p.pos[(size_t)sg.b * p.N + c] - L);
+                    softmax_groups_sync();
+                }
+            }
 
             // A segment that is only part of its unit: which CTAs hold the other parts.  How many of
             // them have been delivered is asked anew at every tile and looked at in the epilogue, so
@@ -417,14 +432,14 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
                 cu.cta_mul = 1; cu.cta_add = 0;
             }
 
-            RowShape shape{0.f, 0};
-            if constexpr (kScored) shape = row_shape(p, real, sg.b, node, sg.hk * p.g + row % p.g);
+            RowShape shape{};
+            if constexpr ((kShape & kShapeBias) != 0) shape = row_shape<kShape>(p, real, sg.b, L, node, sg.hk * p.g + row % p.g);
             float m_ref = -INFINITY, l_sum = 0.f;
 #pragma unroll 1
             for (int i = 0; i < sg.len; ++i) {
                 const int jj = J + i;
                 if ((jj & 1) != s) continue;
-                const int kt = sg.kt0 + i;
+                const int kt = from_end ? sg.kt0 + sg.len - 1 - i : sg.kt0 + i;
                 if (!complete && !clustered && tid256 == 0) {
                     delivered_old = delivered;
                     delivered = ld_relaxed_gpu(&p.tickets[cut[cut_k].unit]);
@@ -435,80 +450,73 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
                 const int tile_lo = kt * kTile;
                 float *const xa = xa_e, *const xb = xb_e;
                 if (warp_real) {
-                float mx0 = -INFINITY, mx1 = -INFINITY;
-                if constexpr (kScored) {
-                    // --- shape, mask and row maximum in one sweep; the scores go back to TMEM in log2 units ---
-                    const RowShape rs = shape;
-                    auto sweep = [&](float *x, int w) {
-                        const int key0 = tile_lo + 32 * w;
-                        shape_scores(p, x, key0, L, sg.b, rs);
-                        mask_scores(x, key0, L, &sm.anc[0][row], kRows, words);
+                if (tile_lo + kTile > L) {
+                    // The tile reaches into the tree rows / the tail: overwrite the scores of keys this
+                    // row must not see with -inf, in place, so that the two passes below need no mask.
+                    // Context keys are visible, tree key c iff bit c of the row's ancestor words, the
+                    // tail never (whatever those cache rows hold, NaN included).
+#pragma unroll 1
+                    for (int w = 0; w < 4; ++w) {
+                        const int cc0 = tile_lo + 32 * w - L;           // tree index of the word's first key
+                        if (cc0 <= -32) continue;
+                        const int wi = cc0 >> 5, sh = cc0 & 31;         // arithmetic shift: -1 for cc0 in (-32, 0)
+                        const uint32_t lo = wi < 0 ? 0xFFFFFFFFu : (wi < words ? sm.anc[wi][row] : 0u);
+                        const uint32_t hi = (wi + 1 >= 0 && wi + 1 < words) ? sm.anc[wi + 1][row] : 0u;
+                        const uint32_t vis = __funnelshift_r(lo, hi, sh);
+                        tmem_ld32(s_addr + w * 32, xa);
+                        tmem_ld_wait();
                         uint32_t r[32];
 #pragma unroll
-                        for (int c = 0; c < 32; c += 4) {
-                            mx0 = max3(mx0, x[c], x[c + 1]);
-                            mx1 = max3(mx1, x[c + 2], x[c + 3]);
-                        }
-#pragma unroll
-                        for (int c = 0; c < 32; ++c) r[c] = __float_as_uint(x[c]);
+                        for (int c = 0; c < 32; ++c) r[c] = ((vis >> c) & 1u) ? __float_as_uint(xa[c]) : 0xFF800000u;
                         tmem_st32(s_addr + w * 32, r);
-                    };
-                    tmem_ld32(s_addr, xa);
-#pragma unroll 1
-                    for (int h = 0; h < 2; ++h) {
-                        tmem_ld_wait();
-                        tmem_ld32(s_addr + (2 * h + 1) * 32, xb);
-                        sweep(xa, 2 * h);
-                        tmem_ld_wait();
-                        if (h == 0) tmem_ld32(s_addr + 2 * 32, xa);
-                        sweep(xb, 2 * h + 1);
                     }
                     tmem_st_wait();
-                    tmem_ld32(s_addr, xa);                       // chunk 0 again, for pass 2
-                } else {
-                    if (tile_lo + kTile > L) {
-                        // The tile reaches into the tree rows / the tail: overwrite the scores of keys this
-                        // row must not see with -inf, in place, so that the two passes below need no mask.
-                        // Context keys are visible, tree key c iff bit c of the row's ancestor words, the
-                        // tail never (whatever those cache rows hold, NaN included).
+                }
+                float mx0 = -INFINITY, mx1 = -INFINITY, size = 0.f;
+                // --- pass 1: row maximum, 32 scores at a time, the next chunk in flight meanwhile ---
+                tmem_ld32(s_addr, xa);
 #pragma unroll 1
-                        for (int w = 0; w < 4; ++w) {
-                            const int cc0 = tile_lo + 32 * w - L;           // tree index of the word's first key
-                            if (cc0 <= -32) continue;
-                            const int wi = cc0 >> 5, sh = cc0 & 31;         // arithmetic shift: -1 for cc0 in (-32, 0)
-                            const uint32_t lo = wi < 0 ? 0xFFFFFFFFu : (wi < words ? sm.anc[wi][row] : 0u);
-                            const uint32_t hi = (wi + 1 >= 0 && wi + 1 < words) ? sm.anc[wi + 1][row] : 0u;
-                            const uint32_t vis = __funnelshift_r(lo, hi, sh);
-                            tmem_ld32(s_addr + w * 32, xa);
-                            tmem_ld_wait();
-                            uint32_t r[32];
+                for (int h = 0; h < 2; ++h) {
+                    tmem_ld_wait();
+                    tmem_ld32(s_addr + (2 * h + 1) * 32, xb);
 #pragma unroll
-                            for (int c = 0; c < 32; ++c) r[c] = ((vis >> c) & 1u) ? __float_as_uint(xa[c]) : 0xFF800000u;
-                            tmem_st32(s_addr + w * 32, r);
-                        }
-                        tmem_st_wait();
+                    for (int c = 0; c < 32; c += 4) {
+                        mx0 = max3(mx0, xa[c], xa[c + 1]);
+                        mx1 = max3(mx1, xa[c + 2], xa[c + 3]);
                     }
-                    // --- pass 1: row maximum, 32 scores at a time, the next chunk in flight meanwhile ---
-                    tmem_ld32(s_addr, xa);
+                    if (kShape & kShapeCap) size = shape_size(xa, size, tile_lo + kTile > L);
+                    tmem_ld_wait();
+                    tmem_ld32(s_addr + ((2 * h + 2) & 3) * 32, xa);   // after the last chunk: chunk 0 again, for pass 2
+#pragma unroll
+                    for (int c = 0; c < 32; c += 4) {
+                        mx0 = max3(mx0, xb[c], xb[c + 1]);
+                        mx1 = max3(mx1, xb[c + 2], xb[c + 3]);
+                    }
+                    if (kShape & kShapeCap) size = shape_size(xb, size, tile_lo + kTile > L);
+                }
+                float mx = fmaxf(mx0, mx1) * p.scale_log2;   // scale > 0: max commutes with scaling
+                bool negligible = false;
+                if constexpr (kShape != 0) {
+                    if ((kShape & kShapeCap) && shape_coefficients(p, shape, size, s_addr, 4, xa)) tmem_ld32(s_addr, xa);
+                    mx = shape_bound<kShape>(p, mx, tile_lo, kTile, shape);
+                    if constexpr ((kShape & kShapeBias) != 0) {
+                        const bool tree_keys = tile_lo + kTile > L;
+                        if (tree_keys || __any_sync(0xffffffffu, real && !(mx <= m_ref + kRescaleThreshold))) {
+                            // the reference may have to rise (or some keys are at positions of their own): the exact maximum
+                            mx = -INFINITY;
 #pragma unroll 1
-                    for (int h = 0; h < 2; ++h) {
-                        tmem_ld_wait();
-                        tmem_ld32(s_addr + (2 * h + 1) * 32, xb);
+                            for (int w = 0; w < 4; ++w) {
+                                tmem_ld_wait();
+                                shape_scores<kShape, true>(p, xa, tile_lo + 32 * w, L, tree_pos, shape, 0.f);
 #pragma unroll
-                        for (int c = 0; c < 32; c += 4) {
-                            mx0 = max3(mx0, xa[c], xa[c + 1]);
-                            mx1 = max3(mx1, xa[c + 2], xa[c + 3]);
-                        }
-                        tmem_ld_wait();
-                        tmem_ld32(s_addr + ((2 * h + 2) & 3) * 32, xa);   // after the last chunk: chunk 0 again, for pass 2
-#pragma unroll
-                        for (int c = 0; c < 32; c += 4) {
-                            mx0 = max3(mx0, xb[c], xb[c + 1]);
-                            mx1 = max3(mx1, xb[c + 2], xb[c + 3]);
+                                for (int c = 0; c < 32; c += 2) mx = max3(mx, xa[c], xa[c + 1]);
+                                tmem_ld32(s_addr + ((w + 1) & 3) * 32, xa);       // after the last chunk: chunk 0 again, for pass 2
+                            }
+                        } else {
+                            negligible = __all_sync(0xffffffffu, !real || mx < m_ref - kNegligibleLog2) && tile_lo + kTile <= L - p.near_keys;
                         }
                     }
                 }
-                const float mx = fmaxf(mx0, mx1) * p.scale_log2;   // scale > 0: max commutes with scaling
                 // --- running maximum, raised lazily ---
                 const float m_new = fmaxf(m_ref, mx);
                 const bool grow = (m_ref != -INFINITY) && (m_new > m_ref + kRescaleThreshold);
@@ -537,8 +545,29 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
                 // in columns [16 c, 16 c + 16), which hold scores already consumed. ---
                 const unsigned long long nbase2 = pack_f32x2(-base, -base);
                 unsigned long long acc2 = pack_f32x2(0.f, 0.f);
-                if (tile_lo + kTile > L - (kScored ? p.near_keys : 0)) softmax_pass2<kBf16, true>(s_addr, xa, xb, scale2, nbase2, acc2);
-                else softmax_pass2<kBf16, false>(s_addr, xa, xb, scale2, nbase2, acc2);
+                if constexpr (kShape != 0) {
+                    if (negligible) {
+                        uint32_t r[16];
+#pragma unroll
+                        for (int c = 0; c < 16; ++c) r[c] = 0u;
+                        tmem_ld_wait();
+#pragma unroll
+                        for (int w = 0; w < 4; ++w) tmem_st16(s_addr + w * 16, r);
+                    } else {
+                        if (tile_lo + kTile > L - p.near_keys)
+                            softmax_pass2<kBf16, true, true>(s_addr, xa, xb, scale2, nbase2, acc2, [&](float *x, int w) {
+                                shape_scores<kShape, true>(p, x, tile_lo + 32 * w, L, tree_pos, shape, -base);
+                            });
+                        else
+                            softmax_pass2<kBf16, false, true>(s_addr, xa, xb, scale2, nbase2, acc2, [&](float *x, int w) {
+                                shape_scores<kShape, false>(p, x, tile_lo + 32 * w, L, tree_pos, shape, -base);
+                            });
+                    }
+                } else {
+                    auto none = [](float *, int) {};
+                    if (tile_lo + kTile > L) softmax_pass2<kBf16, true, false>(s_addr, xa, xb, scale2, nbase2, acc2, none);
+                    else softmax_pass2<kBf16, false, false>(s_addr, xa, xb, scale2, nbase2, acc2, none);
+                }
                 {
                     float a0, a1;
                     unpack_f32x2(acc2, a0, a1);
@@ -869,16 +898,24 @@ size_t attn_tc_workspace(const ht_attn_desc &d) {
 }
 
 typedef void (*AttnKernelFn)(const CUtensorMap, const CUtensorMap, const CUtensorMap, const tc::Params, const tc::PagedParams);
-static AttnKernelFn attn_tc_fn(bool bf16, bool paged, bool clustered, bool scored = false) {
-    static const AttnKernelFn fns[16] = {
-        tc::attn_tc_kernel<false, false, false>, tc::attn_tc_kernel<true, false, false>, tc::attn_tc_kernel<false, true, false>,
-        tc::attn_tc_kernel<true, true, false>,   tc::attn_tc_kernel<false, false, true>, tc::attn_tc_kernel<true, false, true>,
-        tc::attn_tc_kernel<false, true, true>,   tc::attn_tc_kernel<true, true, true>,
-        tc::attn_tc_kernel<false, false, false, true>, tc::attn_tc_kernel<true, false, false, true>,
-        tc::attn_tc_kernel<false, true, false, true>,  tc::attn_tc_kernel<true, true, false, true>,
-        tc::attn_tc_kernel<false, false, true, true>,  tc::attn_tc_kernel<true, false, true, true>,
-        tc::attn_tc_kernel<false, true, true, true>,   tc::attn_tc_kernel<true, true, true, true>};
-    return fns[(bf16 ? 1 : 0) + (paged ? 2 : 0) + (clustered ? 4 : 0) + (scored ? 8 : 0)];
+constexpr int kAttnForms = 32;             // bf16, paged, clustered, then the shape of the scores
+template <int kShape>
+static AttnKernelFn attn_tc_form(int form) {
+    static const AttnKernelFn fns[8] = {
+        tc::attn_tc_kernel<false, false, false, kShape>, tc::attn_tc_kernel<true, false, false, kShape>,
+        tc::attn_tc_kernel<false, true, false, kShape>,  tc::attn_tc_kernel<true, true, false, kShape>,
+        tc::attn_tc_kernel<false, false, true, kShape>,  tc::attn_tc_kernel<true, false, true, kShape>,
+        tc::attn_tc_kernel<false, true, true, kShape>,   tc::attn_tc_kernel<true, true, true, kShape>};
+    return fns[form];
+}
+static AttnKernelFn attn_tc_fn(bool bf16, bool paged, bool clustered, int shape = 0) {
+    const int form = (bf16 ? 1 : 0) + (paged ? 2 : 0) + (clustered ? 4 : 0);
+    switch (shape) {
+        case 0: return attn_tc_form<0>(form);
+        case 1: return attn_tc_form<1>(form);
+        case 2: return attn_tc_form<2>(form);
+        default: return attn_tc_form<3>(form);
+    }
 }
 
 // Kernels per call: the attention kernel, and ahead of it the one that zeroes the arrival counters where it is needed.
@@ -891,7 +928,7 @@ static cudaError_t ensure_smem_attr(size_t smem) {
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
     if (dev >= 0 && dev < 64 && done[dev]) return cudaSuccess;
-    for (int i = 0; i < 16; ++i) {
+    for (int i = 0; i < kAttnForms; ++i) {
         const AttnKernelFn fn = attn_tc_fn(i & 1, (i >> 1) & 1, (i >> 2) & 1, i >> 3);
         e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
         if (e != cudaSuccess) return e;
@@ -953,7 +990,7 @@ static int make_map(CUtensorMap *map, const void *base, int dtype, const cuuint6
 
 
 int launch_attn_tc_pair_kernel(const CUtensorMap &tm_q, const CUtensorMap &tm_k, const CUtensorMap &tm_v, const tc::Params &p,
-                               const tc::PagedParams &pp, bool bf16, bool paged, bool scored, cudaStream_t s);
+                               const tc::PagedParams &pp, bool bf16, bool paged, int shape, cudaStream_t s);
 
 int launch_attn_tc(const ht_attn_desc &d, const void *q, const void *kc, const void *vc, const int32_t *kv_len,
                    const int32_t *parent, void *out, void *ws, size_t ws_bytes, int32_t *status, cudaStream_t s,
@@ -1000,15 +1037,35 @@ int launch_attn_tc(const ht_attn_desc &d, const void *q, const void *kc, const v
     p.n_rt = units_per_head(d);
     const float scale = d.scale > 0.f ? d.scale : 1.f / sqrtf((float)d.D);
     p.scale_log2 = scale * 1.4426950408889634f;
-    p.score_mul = 0.f; p.cap_log2 = 0.f; p.slopes = nullptr; p.pos = nullptr; p.near_keys = 0;
+    p.score_mul = 0.f; p.cap_log2 = 0.f; p.series_lim = -1.f;
+    for (int i = 0; i < 6; ++i) p.series[i] = 0.f;
+    p.slopes = nullptr; p.pos = nullptr; p.near_keys = 0; p.from_end = 0;
+    int shape = 0;
     if (score) {
-        p.score_mul = score->cap > 0.f ? (float)fmin((double)scale / score->cap, 1e30) : p.scale_log2;
-        p.cap_log2 = score->cap * 1.4426950408889634f;
-        p.slopes = score->slopes;
-        p.pos = score->pos;
-        // A steep slope leaves a row a handful of keys: the tree's and the context rows right ahead of it.  The rounding of
-        // their weights to 16 bits does not average away, as on tiles with tree keys.
-        p.near_keys = score->slopes ? tc::kTile : 0;
+        const double log2e = 1.4426950408889634074;
+        p.score_mul = p.scale_log2;
+        if (score->cap > 0.f) {
+            shape |= tc::kShapeCap;
+            const double mul = fmin((double)scale / score->cap, 1e30);
+            p.score_mul = (float)mul;
+            p.cap_log2 = (float)(score->cap * log2e);
+            if (mul <= 1000.0) {                     // (beyond, the coefficients leave the range of 32 bits)
+                // Taylor series of tanh
+                const double a[6] = {1.0, -1.0 / 3.0, 2.0 / 15.0, -17.0 / 315.0, 62.0 / 2835.0, -1382.0 / 155925.0};
+                double power = score->cap * log2e * mul;
+                for (int i = 0; i < 6; ++i, power *= mul * mul) p.series[i] = (float)(a[i] * power);
+                p.series_lim = 0.5f;
+            }
+        }
+        if (score->slopes) {
+            shape |= tc::kShapeBias;
+            p.slopes = score->slopes;
+            p.pos = score->pos;
+            // A steep slope leaves a row a handful of keys: the tree's and the context rows right ahead of it.  The rounding
+            // of their weights to 16 bits does not average away, as on tiles with tree keys.
+            p.near_keys = tc::kTile;
+            p.from_end = 1;
+        }
         p.scale_log2 = 1.f;
     }
     p.is_bf16 = d.dtype == HT_BF16;
@@ -1060,7 +1117,7 @@ int launch_attn_tc(const ht_attn_desc &d, const void *q, const void *kc, const v
     trace("ht_tree_attention -> %s kernel, %s, %d CTAs%s%s", pair_mode(d) ? "tile-pair" : "one-tile",
           k > 1 ? (k == 16 ? "clusters of 16" : (k == 8 ? (split == 2 ? "two clusters of 8 per unit" : "clusters of 8") : (k == 4 ? (split == 4 ? "four clusters of 4 per unit" : "clusters of 4") : "clusters of 2"))) : "persistent",
           p.grid, p.early ? ", early start" : "", needs_prepare(d, pages != nullptr) ? ", counters cleared by a kernel" : "");
-    if (pair_mode(d)) return launch_attn_tc_pair_kernel(tm_q, tm_k, tm_v, p, pp, d.dtype == HT_BF16, pages != nullptr, score != nullptr, s);
+    if (pair_mode(d)) return launch_attn_tc_pair_kernel(tm_q, tm_k, tm_v, p, pp, d.dtype == HT_BF16, pages != nullptr, shape, s);
     e = ensure_smem_attr(sizeof(tc::Smem) + 1024);
     if (e != cudaSuccess) return fail(HT_ERR_CUDA, "cudaFuncSetAttribute: %s", cudaGetErrorString(e));
     // Few (sequence, KV head) units: one cluster of 16, 8, 4 or 2 CTAs per unit, parts reduced through
@@ -1080,7 +1137,7 @@ int launch_attn_tc(const ht_attn_desc &d, const void *q, const void *kc, const v
     attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = k > 1 ? 2 : 1;
-    e = cudaLaunchKernelEx(&cfg, attn_tc_fn(d.dtype == HT_BF16, pages != nullptr, k > 1, score != nullptr), tm_q, tm_k, tm_v, p, pp);
+    e = cudaLaunchKernelEx(&cfg, attn_tc_fn(d.dtype == HT_BF16, pages != nullptr, k > 1, shape), tm_q, tm_k, tm_v, p, pp);
     if (e != cudaSuccess) {
         cudaGetLastError();
         return fail(HT_ERR_CUDA, "ht_tree_attention (tcgen05, clusters of %d): %s", k > 1 ? k : 1, cudaGetErrorString(e));

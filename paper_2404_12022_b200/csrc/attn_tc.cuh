@@ -42,10 +42,13 @@ struct Params {
     int early;             // HT_ATTN_CONTEXT_FINAL: lengths, trees and context rows may be read while the kernel ahead still runs
     // The scored instantiations only (scale_log2 is 1 there: their scores are shaped into log2 units before the softmax):
     float score_mul;       // with a cap: scale / cap; without: scale * log2(e)
-    float cap_log2;        // cap * log2(e); 0: no cap
-    const float *slopes;   // [Hq] or null: distance bias
+    float cap_log2;        // cap * log2(e)
+    float series[6];       // cap * log2(e) * tanh(score_mul x) = x (series[0] + u (series[1] + u (...))), u = x^2
+    float series_lim;      // |score_mul x| up to which it is taken (negative: never)
+    const float *slopes;   // [Hq]: distance bias
     const int32_t *pos;    // [B, N] position ids of the query rows (with slopes)
     int near_keys;         // tiles reaching past context row kv_len - near_keys send P as a hi + lo pair
+    int from_end;          // a segment's tiles are taken from its last to its first
 };
 // The launch is serialized programmatically behind the kernel before it in the stream: a thread passes this point once
 // that kernel has completed and what it wrote is visible, and only then lets this kernel's own dependents be set up.
@@ -300,17 +303,36 @@ __device__ __forceinline__ unsigned long long add_f32x2(unsigned long long a, un
     return d;
 }
 
-// --- shaped scores (the scored instantiations): cap tanh(s / cap), then slope * (position of the key - of the row) ---
-// What a row's thread knows about its row.
+// --- shaped scores (the scored instantiations; kShape: kShapeCap, kShapeBias or both) ---
+//     s = cap tanh(scale q.k / cap) - slope (position of the row - of the key), in log2 units.
+// What decides is how many instructions, and how much code, stand between a tile's products and its weights:
+//   - tanh is its series to t^11 (the next term: 9e-7 of t at t = 1/2), the powers of scale / cap folded into the
+//     coefficients: seven paired fused multiply-adds, which run beside the exponentials' special-function unit.  Where a
+//     warp meets a score beyond half the cap, the tile is first rewritten in tensor memory by a rolled loop with the general
+//     form (cap_one), and the coefficients become those of the identity: a second form in line costs the tiles that never
+//     take it a third of their time (16 x 67 rows on 8192 keys: 890 us against 635 us).
+//   - Tree tiles (masked keys, keys at positions of their own) have instantiations of their own (kTree) for the same reason.
+//   - The running maximum needs no shaped maximum: tanh is monotone, so without a bias the maximum is the shaped raw
+//     maximum; with one, the raw maximum and the bias's larger end bound it, and the exact maximum is only formed where
+//     that bound may raise the reference -- in the first tiles, since a segment's tiles are taken from the nearest keys to
+//     the farthest (p.from_end).  A tile whose bound lies 2^-40 below the reference adds nothing to the 32-bit sum of a
+//     part of up to 2^15 keys: its weights are zero.
+constexpr int kShapeCap = 1, kShapeBias = 2;
+constexpr float kNegligibleLog2 = 40.f;
+// What a row's thread knows about its row, and the coefficients of the tile.
 struct RowShape {
-    float slope;           // in log2 units; 0 without a distance bias
+    float slope;           // in log2 units
     int pos;
+    float from_len;        // pos - kv_len
+    float a[6];            // a shaped score is x (a[0] + u (a[1] + u (...))), u = x^2
 };
-__device__ __forceinline__ RowShape row_shape(const Params &p, bool real, int b, int node, int head) {
-    RowShape r{0.f, 0};
-    if (p.slopes && real) {
+template <int kShape>
+__device__ __forceinline__ RowShape row_shape(const Params &p, bool real, int b, int L, int node, int head) {
+    RowShape r{};
+    if ((kShape & kShapeBias) && real) {
         r.slope = p.slopes[head] * 1.4426950408889634f;
         r.pos = p.pos[(size_t)b * p.N + node];
+        r.from_len = (float)(r.pos - L);
     }
     return r;
 }
@@ -319,77 +341,100 @@ __device__ __forceinline__ float rcp(float x) {
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-// 32 raw products q . k of keys key0, ... of a sequence with L context rows -> scores in log2 units.
-// tanh t by its series to t^11 while all 32 x 32 values of the warp stay within 1/2 (the next term: 4e-7): seven fp32
-// operations, paired, against two of the special-function unit (each worth eight) for 1 - 2 / (1 + e^2t) -- which in
-// turn loses all digits at small t, so that a lane takes the series' result there as well.
-__device__ __forceinline__ void shape_scores(const Params &p, float *x, int key0, int L, int b, const RowShape row) {
-    if (p.cap_log2 > 0.f) {
-        const float mul = p.score_mul, cap = p.cap_log2;
-        float mx = 0.f;
-#pragma unroll
-        for (int c = 0; c < 32; c += 2) mx = max3(mx, fabsf(x[c]), fabsf(x[c + 1]));
-        const bool small = mx * mul <= 0.5f;                 // (false for NaN in a masked place: that lane's values take the general form)
-        const unsigned long long mul2 = pack_f32x2(mul, mul), cap2 = pack_f32x2(cap, cap), zero = pack_f32x2(0.f, 0.f);
-        const unsigned long long a11 = pack_f32x2(-1382.f / 155925.f, -1382.f / 155925.f), a9 = pack_f32x2(62.f / 2835.f, 62.f / 2835.f),
-                                 a7 = pack_f32x2(-17.f / 315.f, -17.f / 315.f), a5 = pack_f32x2(2.f / 15.f, 2.f / 15.f),
-                                 a3 = pack_f32x2(-1.f / 3.f, -1.f / 3.f);
-        auto series = [&](unsigned long long t) {            // cap * tanh t
-            const unsigned long long u = fma_f32x2(t, t, zero);
-            unsigned long long q = fma_f32x2(u, a11, a9);
-            q = fma_f32x2(q, u, a7);
-            q = fma_f32x2(q, u, a5);
-            q = fma_f32x2(q, u, a3);
-            const unsigned long long ct = fma_f32x2(t, cap2, zero);
-            return fma_f32x2(fma_f32x2(q, u, zero), ct, ct);
-        };
-        if (__all_sync(0xffffffffu, small)) {
-#pragma unroll
-            for (int c = 0; c < 32; c += 2) unpack_f32x2(series(fma_f32x2(pack_f32x2(x[c], x[c + 1]), mul2, zero)), x[c], x[c + 1]);
-        } else {
-#pragma unroll
-            for (int c = 0; c < 32; c += 2) {
-                const float t0 = x[c] * mul, t1 = x[c + 1] * mul;
-                float s0, s1;
-                unpack_f32x2(series(pack_f32x2(t0, t1)), s0, s1);
-                const float g0 = fmaf(-2.f * cap, rcp(1.f + ex2(t0 * 2.8853900817779268f)), cap);
-                const float g1 = fmaf(-2.f * cap, rcp(1.f + ex2(t1 * 2.8853900817779268f)), cap);
-                x[c] = fabsf(t0) <= 0.5f ? s0 : g0;
-                x[c + 1] = fabsf(t1) <= 0.5f ? s1 : g1;
-            }
-        }
-    } else {
-        const unsigned long long mul2 = pack_f32x2(p.score_mul, p.score_mul), zero = pack_f32x2(0.f, 0.f);
-#pragma unroll
-        for (int c = 0; c < 32; c += 2) unpack_f32x2(fma_f32x2(pack_f32x2(x[c], x[c + 1]), mul2, zero), x[c], x[c + 1]);
-    }
-    if (p.slopes) {
-        if (key0 + 32 <= L) {                                // context keys: position = row
-            const float first = row.slope * (float)(key0 - row.pos);
-#pragma unroll
-            for (int c = 0; c < 32; ++c) x[c] += fmaf(row.slope, (float)c, first);
-        } else {
-            const int32_t *pos = p.pos + (size_t)b * p.N;
-#pragma unroll
-            for (int c = 0; c < 32; ++c) {
-                const int cc = key0 + c - L;
-                const int at = cc < 0 ? key0 + c : (cc < p.N ? pos[cc] : row.pos);
-                x[c] = fmaf(row.slope, (float)(at - row.pos), x[c]);
-            }
-        }
-    }
+// cap tanh(x scale / cap), any x; -inf (a masked key) stays.
+__device__ __forceinline__ float cap_one(const Params &p, float x) {
+    const float u = x * x;
+    const float near = x * fmaf(u, fmaf(u, fmaf(u, fmaf(u, fmaf(u, p.series[5], p.series[4]), p.series[3]), p.series[2]), p.series[1]), p.series[0]);
+    const float far = fmaf(-2.f * p.cap_log2, rcp(1.f + ex2(x * (2.8853900817779268f * p.score_mul))), p.cap_log2);
+    return fabsf(x * p.score_mul) <= p.series_lim ? near : (x == -INFINITY ? x : far);
 }
-// Scores of tree keys the row must not see, and of the tail, become -inf (context visible; `anc`: the row's ancestor
-// words, `stride` apart).
-__device__ __forceinline__ void mask_scores(float *x, int key0, int L, const uint32_t *anc, int stride, int words) {
-    const int cc0 = key0 - L;
-    if (cc0 <= -32) return;
-    const int wi = cc0 >> 5, sh = cc0 & 31;                  // arithmetic shift: -1 for cc0 in (-32, 0)
-    const uint32_t lo = wi < 0 ? 0xFFFFFFFFu : (wi < words ? anc[wi * stride] : 0u);
-    const uint32_t hi = (wi + 1 >= 0 && wi + 1 < words) ? anc[(wi + 1) * stride] : 0u;
-    const uint32_t vis = __funnelshift_r(lo, hi, sh);
+// The largest |product| of 32, masked keys (-inf) of a tile with tree keys left out.
+__device__ __forceinline__ float shape_size(const float *x, float size, bool tree_keys) {
+    if (tree_keys) {
 #pragma unroll
-    for (int c = 0; c < 32; ++c) x[c] = ((vis >> c) & 1u) ? x[c] : -INFINITY;
+        for (int c = 0; c < 32; ++c) size = fmaxf(size, x[c] == -INFINITY ? 0.f : fabsf(x[c]));
+    } else {
+#pragma unroll
+        for (int c = 0; c < 32; c += 8)
+            size = max3(size, fmaxf(max3(fabsf(x[c]), fabsf(x[c + 1]), fabsf(x[c + 2])), fabsf(x[c + 3])),
+                        fmaxf(max3(fabsf(x[c + 4]), fabsf(x[c + 5]), fabsf(x[c + 6])), fabsf(x[c + 7])));
+    }
+    return size;
+}
+// The tile's coefficients; its `chunks` x 32 products at s_addr rewritten as capped scores where the series does not
+// reach (a register array of 32 as scratch; size: the row's largest |product|).  True where they were rewritten.
+__device__ __forceinline__ bool shape_coefficients(const Params &p, RowShape &row, float size, uint32_t s_addr, int chunks, float *x) {
+    const bool far = __any_sync(0xffffffffu, !(size * p.score_mul <= p.series_lim));
+#pragma unroll
+    for (int i = 0; i < 6; ++i) row.a[i] = far ? (i == 0 ? 1.f : 0.f) : p.series[i];
+    if (far) {
+        tmem_ld_wait();                                      // whatever was on its way into x
+#pragma unroll 1
+        for (int w = 0; w < chunks; ++w) {
+            tmem_ld32(s_addr + w * 32, x);
+            tmem_ld_wait();
+            uint32_t r[32];
+#pragma unroll
+            for (int c = 0; c < 32; ++c) r[c] = __float_as_uint(cap_one(p, x[c]));
+            tmem_st32(s_addr + w * 32, r);
+        }
+        tmem_st_wait();
+    }
+    return far;
+}
+// An upper bound of the shaped scores of `keys` context keys from key0 on whose largest raw product is mx.
+template <int kShape>
+__device__ __forceinline__ float shape_bound(const Params &p, float mx, int key0, int keys, const RowShape &row) {
+    float s = (kShape & kShapeCap) ? cap_one(p, mx) : mx * p.score_mul;
+    if (kShape & kShapeBias) s += row.slope * (float)((row.slope > 0.f ? key0 + keys - 1 : key0) - row.pos);
+    return s;
+}
+// 32 raw products of keys key0, ... of a sequence with L context rows -> shaped scores plus `add`.  kTree: some may be
+// tree keys or masked (masked keys, -inf, stay masked).  tree_pos: positions of the tree rows less L.
+template <int kShape, bool kTree>
+__device__ __forceinline__ void shape_scores(const Params &p, float *x, int key0, int L, const float *tree_pos, const RowShape &row, float add) {
+    const bool tree = kTree && key0 + 32 > L;
+    uint32_t masked = 0u;                                    // (the series loses a -inf)
+    if (kTree && (kShape & kShapeCap)) {
+#pragma unroll
+        for (int c = 0; c < 32; ++c) masked |= (x[c] == -INFINITY ? 1u : 0u) << c;
+    }
+    // context keys: the bias is linear in the key
+    const float slope = (kShape & kShapeBias) && !tree ? row.slope : 0.f;
+    const float first = (kShape & kShapeBias) && !tree ? fmaf(row.slope, (float)(key0 - row.pos), add) : add;
+    const unsigned long long slope2 = pack_f32x2(slope, slope), first2 = pack_f32x2(first, first);
+    auto rest = [&](int c) {                                 // what is added to the (capped) scores of keys c and c + 1
+        return (kShape & kShapeBias) ? fma_f32x2(slope2, pack_f32x2((float)c, (float)(c + 1)), first2) : first2;
+    };
+    if (!(kShape & kShapeCap)) {
+        const unsigned long long mul2 = pack_f32x2(p.score_mul, p.score_mul);
+#pragma unroll
+        for (int c = 0; c < 32; c += 2) unpack_f32x2(fma_f32x2(pack_f32x2(x[c], x[c + 1]), mul2, rest(c)), x[c], x[c + 1]);
+    } else {
+        const unsigned long long zero = pack_f32x2(0.f, 0.f);
+        unsigned long long a[6];
+#pragma unroll
+        for (int i = 0; i < 6; ++i) a[i] = pack_f32x2(row.a[i], row.a[i]);
+#pragma unroll
+        for (int c = 0; c < 32; c += 2) {
+            const unsigned long long v = pack_f32x2(x[c], x[c + 1]), u = fma_f32x2(v, v, zero);
+            unsigned long long q = fma_f32x2(u, fma_f32x2(u, fma_f32x2(u, a[5], a[4]), a[3]), a[2]);
+            q = fma_f32x2(u, fma_f32x2(u, q, a[1]), a[0]);
+            unpack_f32x2(fma_f32x2(v, q, rest(c)), x[c], x[c + 1]);
+        }
+    }
+    if (kTree && (kShape & kShapeCap)) {
+#pragma unroll
+        for (int c = 0; c < 32; ++c) x[c] = (masked >> c) & 1u ? -INFINITY : x[c];
+    }
+    if ((kShape & kShapeBias) && tree) {                     // some of the 32 are tree keys, at the positions given
+        float at[32];                                        // position of the key - L (index clamped: the tail is masked)
+#pragma unroll
+        for (int c = 0; c < 32; ++c) at[c] = tree_pos[min(max(key0 + c - L, 0), p.N - 1)];
+#pragma unroll
+        for (int c = 0; c < 32; ++c)
+            x[c] = fmaf(row.slope, (key0 + c < L ? (float)(key0 + c - L) : at[c]) - row.from_len, x[c]);
+    }
 }
 
 __device__ __forceinline__ void softmax_groups_sync() {   // the 256 softmax threads
@@ -549,7 +594,8 @@ struct TileCursor {
         ++t;
         return true;
     }
-    __device__ __forceinline__ int kt() const { return s.kt0 + i - 1; }
+    // from_end: the segment's tiles from its last to its first
+    __device__ __forceinline__ int kt(bool from_end = false) const { return from_end ? s.kt0 + s.len - i : s.kt0 + i - 1; }
     __device__ __forceinline__ bool first() const { return i == 1; }
 };
 
@@ -743,10 +789,10 @@ __device__ __forceinline__ void plan_sequences(const Params &p, int32_t *s_len, 
 // never stalls the fetches.
 // ---------------------------------------------------------------------------------------
 __device__ __forceinline__ void pages_request(const Params &p, const PagedParams &pp, const int32_t *pre, const int32_t *nkt,
-                                              int32_t (*pg)[kPgSub], int jt, TileCursor &cur, int lane, int n_rt_list) {
+                                              int32_t (*pg)[kPgSub], int jt, TileCursor &cur, int lane, int n_rt_list, bool from_end) {
     if (cur.next(pre, nkt, p.B, n_rt_list)) {               // `cur` walks the range one tile per call: this is tile jt
         const int sub = pp.page_size >= kTile ? 1 : kTile >> pp.page_shift;
-        const int first = (cur.kt() * kTile) >> pp.page_shift;
+        const int first = (cur.kt(from_end) * kTile) >> pp.page_shift;
         if (lane < sub) {                                // lane x: page x of the tile
             if (first + lane < pp.max_pages)
                 cp_async4(&pg[jt % kPgTiles][lane], pp.block_table + (size_t)cur.s.b * pp.max_pages + first + lane);

@@ -137,8 +137,8 @@ __device__ __noinline__ void cluster_merge_pair(const Params &p, const unsigned 
 }
 
 
-// kScored: scores capped or biased by distance before the softmax (shape_scores).
-template <bool kBf16, bool kPaged, bool kSplit, bool kScored = false>
+// kShape: scores capped or biased by distance before the softmax (shape_scores); 0: neither.
+template <bool kBf16, bool kPaged, bool kSplit, int kShape = 0>
 __global__ void __launch_bounds__(kPThreads, 1)
 attn_tc_pair_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
                     const __grid_constant__ CUtensorMap tm_v, const Params p, const PagedParams pp) {
@@ -146,6 +146,7 @@ attn_tc_pair_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     PSmem &sm = *reinterpret_cast<PSmem *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     volatile int *abort_flag = &sm.abort;
+    const bool from_end = (kShape & kShapeBias) && p.from_end;
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < kPStages; ++i) { mbar_init(&sm.kv_full[i], 1); mbar_init(&sm.kv_empty[i], 2); }
@@ -247,7 +248,7 @@ attn_tc_pair_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
             TileCursor cur_p;                         // page-id lookahead
             cur_p.init(t_begin, t_end, first);
             if (kPaged)
-                for (int jt = 0; jt < kPgAhead; ++jt) pages_request(p, pp, sm.pre, sm.nkt, sm.pg, jt, cur_p, lane, lrt);
+                for (int jt = 0; jt < kPgAhead; ++jt) pages_request(p, pp, sm.pre, sm.nkt, sm.pg, jt, cur_p, lane, lrt, from_end);
             bool stop = false;
             bool waited = !early;                  // early: the range's first Q tiles are fetched by stream 0's issuing thread, behind its wait
             auto release = [&]() {
@@ -273,7 +274,7 @@ attn_tc_pair_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                 if (lane == 0 && !(early && seg_i == 0)) fetch_q(s);
                 ++seg_i;
                 for (int i = 0; i < 2 * s.len; ++i) {
-                    const int kt = s.kt0 + (i >> 1);
+                    const int kt = from_end ? s.kt0 + s.len - 1 - (i >> 1) : s.kt0 + (i >> 1);
                     // early: context tiles only, and no more of them than the ring holds, ahead of the wait
                     if (!waited && ((kt + 1) * kTile > sm.len[s.b] || ring_i >= kPStages)) release();
                     const int slot = ring_i % kPStages, use = ring_i / kPStages;
@@ -283,7 +284,7 @@ attn_tc_pair_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                     const CUtensorMap *tm = (i & 1) ? &tm_v : &tm_k;
                     const int jt = t - t_begin + (i >> 1);            // tile of this CTA's range
                     if (kPaged && !(i & 1)) {
-                        pages_request(p, pp, sm.pre, sm.nkt, sm.pg, jt + kPgAhead, cur_p, lane, lrt);
+                        pages_request(p, pp, sm.pre, sm.nkt, sm.pg, jt + kPgAhead, cur_p, lane, lrt, from_end);
                         cp_async_wait<kPgAhead>();
                     }
                     if (lane == 0) mbar_expect_tx(&sm.kv_full[slot], kEntryBytes);
@@ -391,7 +392,7 @@ attn_tc_pair_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                         tc_commit_addr(bar_kv_empty + v_slot * 8);
                         continue;
                     }
-                    const int key_hi = (sg.kt0 + i) * kTile + kHalf;        // end of the tile's first half
+                    const int key_hi = (from_end ? sg.kt0 + sg.len - 1 - i : sg.kt0 + i) * kTile + kHalf;        // end of the tile's first half
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
                         // K-major operands: 16 features = 32 bytes inside the 128-byte swizzled line; the second
@@ -405,7 +406,7 @@ attn_tc_pair_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                         if (pend) issue_pv();
                         pend = true;
                         pend_first = (i == 0 && h == 0);
-                        pend_tree = key_hi + h * kHalf > L - (kScored ? p.near_keys : 0);
+                        pend_tree = key_hi + h * kHalf > L - (kShape ? p.near_keys : 0);
                         pend_h = h;
                         pend_slot = v_slot;
                         pend_ph = v_ph;
@@ -461,7 +462,8 @@ attn_tc_pair_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
             const bool real = active && node < p.N;
             // a warp none of whose 32 rows is a query row keeps step with the barriers but computes nothing
             const bool warp_real = active && row_tile * p.rows_per_tile_nodes + (row & ~31) / p.g < p.N;
-            if (sg.b != anc_b || sg.rt != anc_rt) {
+            const bool new_rows = sg.b != anc_b || sg.rt != anc_rt;
+            if (new_rows) {
                 softmax_groups_sync();                 // previous segment no longer reads parent / anc
                 for (int c = tid256; c < p.N; c += 256) sm.parent[c] = p.parent[(size_t)sg.b * p.N + c];
                 softmax_groups_sync();
@@ -473,6 +475,14 @@ attn_tc_pair_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                 anc_rt = sg.rt;
             }
             release();
+            // the tree rows' positions (which the kernel ahead may have written) take the place of the parents
+            float *const tree_pos = reinterpret_cast<float *>(sm.parent);
+            if constexpr ((kShape & kShapeBias) != 0) {
+                if (new_rows) {
+                    for (int c = tid256; c < p.N; c += 256) tree_pos[c] = (float)(p.pos[(size_t)sg.b * p.N + c] - L);
+                    softmax_groups_sync();
+                }
+            }
             // A segment that is only part of its unit: see the one-tile kernel.
             const bool complete = sg.kt0 == 0 && sg.len == sg.nkt;
             const int cut_k = (t == t_begin) ? 0 : 1;
@@ -487,15 +497,15 @@ attn_tc_pair_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                 cu.c_hi = (cu.t0 + sg.nkt - 1) / per;
             }
 
-            RowShape shape{0.f, 0};
-            if constexpr (kScored) shape = row_shape(p, real, sg.b, node, sg.hk * p.g + row % p.g);
+            RowShape shape{};
+            if constexpr ((kShape & kShapeBias) != 0) shape = row_shape<kShape>(p, real, sg.b, L, node, sg.hk * p.g + row % p.g);
             float m_ref = -INFINITY, l_sum = 0.f;
             int last_h = -1;                            // score buffer of this stream's latest P V in this segment
             if (active) {
 #pragma unroll 1
                 for (int ih = 0; ih < 2 * sg.len; ++ih) {
                     const int i = ih >> 1, h = ih & 1;
-                    const int kt = sg.kt0 + i;
+                    const int kt = from_end ? sg.kt0 + sg.len - 1 - i : sg.kt0 + i;
                     if (!complete && !clustered && tid256 == 0 && h == 0) {
                         delivered_old = delivered;
                         delivered = ld_relaxed_gpu(&p.tickets[cut[cut_k].unit]);
@@ -506,7 +516,7 @@ attn_tc_pair_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                     const uint32_t s_addr = tmem + lane_base + s * 128 + h * kHalf;
                     const int key_lo = kt * kTile + h * kHalf;
                     if (warp_real) {
-                    if (!kScored && key_lo + kHalf > L) {
+                    if (key_lo + kHalf > L) {
                         // Reaches into the tree rows / the tail: scores of keys this row must not see
                         // become -inf in place (context visible, tree key c iff ancestor bit c, tail never).
 #pragma unroll 1
@@ -531,12 +541,6 @@ attn_tc_pair_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                     tmem_ld32(s_addr, xa);
                     tmem_ld32(s_addr + 32, xb);
                     tmem_ld_wait();
-                    if constexpr (kScored) {                // shaped and masked in registers
-                        shape_scores(p, xa, key_lo, L, sg.b, shape);
-                        mask_scores(xa, key_lo, L, &sm.anc[s * words * kRows + row], kRows, words);
-                        shape_scores(p, xb, key_lo + 32, L, sg.b, shape);
-                        mask_scores(xb, key_lo + 32, L, &sm.anc[s * words * kRows + row], kRows, words);
-                    }
 #pragma unroll
                     for (int c = 0; c < 32; c += 4) {
                         mx0 = max3(mx0, xa[c], xa[c + 1]);
@@ -547,7 +551,36 @@ attn_tc_pair_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                         mx0 = max3(mx0, xb[c], xb[c + 1]);
                         mx1 = max3(mx1, xb[c + 2], xb[c + 3]);
                     }
-                    const float mx = fmaxf(mx0, mx1) * p.scale_log2;
+                    float mx = fmaxf(mx0, mx1) * p.scale_log2;
+                    bool negligible = false;
+                    if constexpr (kShape != 0) {
+                        float size = 0.f;                   // the largest |product| of the row
+                        if (kShape & kShapeCap) size = shape_size(xb, shape_size(xa, size, key_lo + kHalf > L), key_lo + kHalf > L);
+                        if ((kShape & kShapeCap) && shape_coefficients(p, shape, size, s_addr, 2, xa)) {
+                            tmem_ld32(s_addr, xa);
+                            tmem_ld32(s_addr + 32, xb);
+                            tmem_ld_wait();
+                        }
+                        mx = shape_bound<kShape>(p, mx, key_lo, kHalf, shape);
+                        const bool exact = (kShape & kShapeBias) &&
+                                           (key_lo + kHalf > L || __any_sync(0xffffffffu, real && !(mx <= m_ref + kRescaleThreshold)));
+                        if (kShape & kShapeBias)
+                            negligible = !exact && __all_sync(0xffffffffu, !real || mx < m_ref - kNegligibleLog2) && key_lo + kHalf <= L - p.near_keys;
+                        if (!negligible) {
+                            if (key_lo + kHalf > L) {
+                                shape_scores<kShape, true>(p, xa, key_lo, L, tree_pos, shape, 0.f);
+                                shape_scores<kShape, true>(p, xb, key_lo + 32, L, tree_pos, shape, 0.f);
+                            } else {
+                                shape_scores<kShape, false>(p, xa, key_lo, L, tree_pos, shape, 0.f);
+                                shape_scores<kShape, false>(p, xb, key_lo + 32, L, tree_pos, shape, 0.f);
+                            }
+                            if (exact) {                    // the reference may have to rise: the exact maximum
+                                mx = -INFINITY;
+#pragma unroll
+                                for (int c = 0; c < 32; ++c) mx = max3(mx, xa[c], xb[c]);
+                            }
+                        }
+                    }
                     // --- running maximum, raised lazily ---
                     const float m_new = fmaxf(m_ref, mx);
                     const bool grow = (m_ref != -INFINITY) && (m_new > m_ref + kRescaleThreshold);
@@ -583,7 +616,7 @@ attn_tc_pair_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                     // to the tensor pipe as a pair hi + lo of 16-bit values: a second sweep forms the same exponentials
                     // again and stores what the rounding took away 32 columns further (all 64 scores are in registers,
                     // so the buffer's upper half is free), and P V is issued for both.
-                    const bool hi_lo = key_lo + kHalf > L - (kScored ? p.near_keys : 0);
+                    const bool hi_lo = key_lo + kHalf > L - (kShape ? p.near_keys : 0);
                     auto chunk = [&](const float *x, uint32_t col) {
                         uint32_t r[16];
 #pragma unroll
@@ -618,8 +651,16 @@ attn_tc_pair_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                             tmem_st16(col + 32, r);
                         }
                     };
-                    chunk(xa, s_addr);
-                    chunk(xb, s_addr + 16);
+                    if (kShape && negligible) {
+                        uint32_t r[16];
+#pragma unroll
+                        for (int c = 0; c < 16; ++c) r[c] = 0u;
+                        tmem_st16(s_addr, r);
+                        tmem_st16(s_addr + 16, r);
+                    } else {
+                        chunk(xa, s_addr);
+                        chunk(xb, s_addr + 16);
+                    }
                     {
                         float a0, a1;
                         unpack_f32x2(acc2, a0, a1);
@@ -814,19 +855,30 @@ attn_tc_pair_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
 
 }  // namespace tc
 
+typedef void (*PairKernelFn)(const CUtensorMap, const CUtensorMap, const CUtensorMap, const tc::Params, const tc::PagedParams);
+template <int kShape>
+static PairKernelFn pair_form(int form) {
+    static const PairKernelFn fns[8] = {
+        tc::attn_tc_pair_kernel<false, false, false, kShape>, tc::attn_tc_pair_kernel<true, false, false, kShape>,
+        tc::attn_tc_pair_kernel<false, true, false, kShape>,  tc::attn_tc_pair_kernel<true, true, false, kShape>,
+        tc::attn_tc_pair_kernel<false, false, true, kShape>,  tc::attn_tc_pair_kernel<true, false, true, kShape>,
+        tc::attn_tc_pair_kernel<false, true, true, kShape>,   tc::attn_tc_pair_kernel<true, true, true, kShape>};
+    return fns[form];
+}
+static PairKernelFn pair_fn(int form, int shape) {
+    switch (shape) {
+        case 0: return pair_form<0>(form);
+        case 1: return pair_form<1>(form);
+        case 2: return pair_form<2>(form);
+        default: return pair_form<3>(form);
+    }
+}
+
 // Raises the kernels' dynamic shared memory limit (once per device) and launches.
 int launch_attn_tc_pair_kernel(const CUtensorMap &tm_q, const CUtensorMap &tm_k, const CUtensorMap &tm_v, const tc::Params &p,
-                               const tc::PagedParams &pp, bool bf16, bool paged, bool scored, cudaStream_t s) {
-    typedef void (*Fn)(const CUtensorMap, const CUtensorMap, const CUtensorMap, const tc::Params, const tc::PagedParams);
-    const Fn fns[16] = {tc::attn_tc_pair_kernel<false, false, false>, tc::attn_tc_pair_kernel<true, false, false>,
-                       tc::attn_tc_pair_kernel<false, true, false>,  tc::attn_tc_pair_kernel<true, true, false>,
-                       tc::attn_tc_pair_kernel<false, false, true>,  tc::attn_tc_pair_kernel<true, false, true>,
-                       tc::attn_tc_pair_kernel<false, true, true>,   tc::attn_tc_pair_kernel<true, true, true>,
-                       tc::attn_tc_pair_kernel<false, false, false, true>, tc::attn_tc_pair_kernel<true, false, false, true>,
-                       tc::attn_tc_pair_kernel<false, true, false, true>,  tc::attn_tc_pair_kernel<true, true, false, true>,
-                       tc::attn_tc_pair_kernel<false, false, true, true>,  tc::attn_tc_pair_kernel<true, false, true, true>,
-                       tc::attn_tc_pair_kernel<false, true, true, true>,   tc::attn_tc_pair_kernel<true, true, true, true>};
-    const Fn fn = fns[(bf16 ? 1 : 0) + (paged ? 2 : 0) + (p.cluster_split > 1 ? 4 : 0) + (scored ? 8 : 0)];
+                               const tc::PagedParams &pp, bool bf16, bool paged, int shape, cudaStream_t s) {
+    const int form = (bf16 ? 1 : 0) + (paged ? 2 : 0) + (p.cluster_split > 1 ? 4 : 0);
+    const PairKernelFn fn = pair_fn(form, shape);
     static bool done[64];
     const size_t smem_max = sizeof(tc::PSmem) + 1024;
     const size_t smem = offsetof(tc::PSmem, anc) + (size_t)2 * ((p.N + 31) / 32) * tc::kRows * sizeof(uint32_t) + 1024;
@@ -834,9 +886,9 @@ int launch_attn_tc_pair_kernel(const CUtensorMap &tm_q, const CUtensorMap &tm_k,
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return fail(HT_ERR_CUDA, "cudaGetDevice: %s", cudaGetErrorString(e));
     if (!(dev >= 0 && dev < 64 && done[dev])) {
-        for (int i = 0; i < 16 && e == cudaSuccess; ++i) {
-            e = cudaFuncSetAttribute(fns[i], cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_max);
-            if (e == cudaSuccess) e = cudaFuncSetAttribute(fns[i], cudaFuncAttributeNonPortableClusterSizeAllowed, 1);   // clusters of 16
+        for (int i = 0; i < 32 && e == cudaSuccess; ++i) {
+            e = cudaFuncSetAttribute(pair_fn(i & 7, i >> 3), cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_max);
+            if (e == cudaSuccess) e = cudaFuncSetAttribute(pair_fn(i & 7, i >> 3), cudaFuncAttributeNonPortableClusterSizeAllowed, 1);   // clusters of 16
         }
         if (e != cudaSuccess) return fail(HT_ERR_CUDA, "cudaFuncSetAttribute: %s", cudaGetErrorString(e));
         if (dev >= 0 && dev < 64) done[dev] = true;

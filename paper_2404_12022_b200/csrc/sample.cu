@@ -10,13 +10,15 @@
 // Every filter keeps a prefix of the order, so a kept set is one pair (x, index): the first element left out.
 //
 // The token is a whole number, and the cut of a flat distribution moves all that follows it, so weights and sums are
-// held in 64 bits (relative error about 1e-13): a row's answer does not depend on how its sum was split.  Nothing is
-// added by atomics but counts.
+// held in 64 bits (relative error about 1e-13; tokens below 2^-32 of the largest, whose sum is below 1e-5 of the whole,
+// are added up in 32): a row's answer does not depend on how its sum was split.  Nothing is added by atomics but counts.
 //
-// One block per row, the row in shared memory.  A histogram of the tokens over the logarithm of their weight (1/64
-// octave per bin) bounds the running weight at every bin, which leaves the cut in a zone of a bin or a few; the zone's
-// tokens (or the whole kept set, where it is small) are sorted and the cut is found exactly.  A small top-k needs no
-// weights at all: the k-th largest of the threads' maxima is a lower bound of the k-th largest token.
+// A row is split over the blocks of a cluster (one block where the rows fill the GPU by themselves), its slices in
+// shared memory; one read of the logits.  A histogram of the tokens over the logarithm of their weight (1/64 octave per
+// bin) bounds the running weight at every bin, which leaves the cut in a zone of a bin or a few; the zone's tokens (or
+// the whole kept set, where it is small) are sorted by the cluster's first block and the cut is found exactly.  A small
+// top-k needs no weights at all: the k-th largest of the threads' maxima is a lower bound of the k-th largest token.
+// Bound by the 64-bit pipe (ten operations per token that counts) and by the shared memory's atomics, not by HBM.
 #include <limits.h>
 
 #include "accept.cuh"
@@ -28,6 +30,7 @@ constexpr int kSampleWarps = kSampleThreads / 32;
 constexpr int kBins = 2048;
 constexpr int kBinsPerOctave = 64;
 constexpr int kList = 1024;               // tokens that are sorted at most
+constexpr int kMaxTeam = 8;               // blocks per row
 constexpr float kLog2eF = 1.4426950408889634f;
 
 struct SampleSmem {
@@ -36,11 +39,19 @@ struct SampleSmem {
         unsigned long long list[kList];
     };
     double pow2[16];                      // 2^(i / 16)
-    double wsum[kSampleWarps];
+    double wsum[kSampleWarps];            // per warp, of the block's latest sum
+    double part[kSampleWarps];            // per warp: kept weight of its range of the row
     float wmax[kSampleWarps];
     unsigned int wcount[kSampleWarps];
+    struct {
+        double d;
+        float f;
+        unsigned int u;
+    } slot[2];                            // what the row's other blocks read, by turns
     int n_list, n_above, zone_lo, zone_hi, answer, first_thread;
     unsigned int total;
+    float cut_x;
+    int cut_i;
 };
 
 // Ordered integer of a value: larger value, larger integer; -0 counts as 0.
@@ -58,36 +69,57 @@ __device__ __forceinline__ float key_value(unsigned int k) {
 struct Weights {
     double m, c;                          // largest logit, 16 log2(e) / T
     const double *pow2;
-    __device__ __forceinline__ double operator()(float x) const {
-        const double t = ((double)x - m) * c;
-        if (!(t >= -16000.0)) return 0.0;
+    // w = q * s
+    __device__ __forceinline__ void factors(float x, double &q, double &s) const {
+        // The value in 64 bits by moving its fields (the conversion shares a slow unit): infinities become 2^128, and so
+        // their distance to themselves 0 and to everything else immense; zeros become 2^-127.
+        const unsigned int u = __float_as_uint(x);
+        const double v = __hiloint2double((int)((((int)u >> 3) & 0x8fffffffu) + 0x38000000u), (int)(u << 29));
+        const double d = v - m;
         constexpr double kMagic = 6755399441055744.0;          // 1.5 * 2^52: adding it rounds to a whole number
-        const double kd = t + kMagic;
+        const double kd = fma(d, c, kMagic);
         const int k = __double2loint(kd);
-        const double r = t - (kd - kMagic);
+        const double r = fma(d, c, -(kd - kMagic));
         constexpr double a = 0.693147180559945309417 / 16.0;   // ln 2 / 16
-        double q = a * a * a * a * a / 120.0;
+        q = a * a * a * a * a / 120.0;
         q = fma(q, r, a * a * a * a / 24.0);
         q = fma(q, r, a * a * a / 6.0);
         q = fma(q, r, a * a / 2.0);
         q = fma(q, r, a);
         q = fma(q, r, 1.0);
-        const double w = q * pow2[k & 15];
-        return __hiloint2double(__double2hiint(w) + ((k >> 4) << 20), __double2loint(w));
+        s = pow2[k & 15];
+        s = __hiloint2double(__double2hiint(s) + ((k >> 4) << 20), __double2loint(s));
+        if (!(d * c >= -16000.0)) { q = 0.0; s = 0.0; }
+    }
+    __device__ __forceinline__ double operator()(float x) const {
+        double q, s;
+        factors(x, q, s);
+        return q * s;
+    }
+    __device__ __forceinline__ void add_to(double &sum, float x) const {
+        double q, s;
+        factors(x, q, s);
+        sum = fma(q, s, sum);
     }
 };
+// The value `factors` sees x as.
+__device__ __forceinline__ double wide(float x) {
+    const unsigned int u = __float_as_uint(x);
+    return __hiloint2double((int)((((int)u >> 3) & 0x8fffffffu) + 0x38000000u), (int)(u << 29));
+}
 
-// A row: in shared memory at the 16-byte phase it has in global memory, with -inf around it (kStaged), or in global
-// memory.  NaN reads as -inf; where the largest value is +inf (`peak`), +inf reads as 0 and all else as -inf.
+// A block's slice of a row: vectors [v_lo, v_hi) of 16 bytes, in shared memory at the phase they have in global memory
+// with -inf around the row (kStaged), or in global memory.  NaN reads as -inf; where the largest value is +inf
+// (`peak`), +inf reads as 0 and all else as -inf.
 template <typename T, bool kStaged>
 struct Row {
     static constexpr int VE = Vec16<T>::n;
-    const T *base;                        // vector 0 (16-byte aligned); element i of the row is base[phase + i]
-    int phase, V, vecs;
+    const T *base;                        // vector v_lo (kStaged) or vector 0; element i of the row is number phase + i from vector 0
+    int phase, V, v_lo, v_hi;
     bool peak;
     __device__ __forceinline__ void load(int v, float *x) const {
         if (kStaged) {
-            unpack16<T>(*reinterpret_cast<const uint4 *>(base + v * VE), x);
+            unpack16<T>(*reinterpret_cast<const uint4 *>(base + (v - v_lo) * VE), x);
             return;
         }
         const int i0 = v * VE - phase;
@@ -105,7 +137,7 @@ struct Row {
     }
     __device__ __forceinline__ int index(int v, int e) const { return v * VE - phase + e; }
     // the vectors of warp w: consecutive, so that sums per warp are sums over ranges of the index
-    __device__ __forceinline__ int warp_first(int w) const { return (int)((long long)vecs * w / kSampleWarps); }
+    __device__ __forceinline__ int warp_first(int w) const { return v_lo + (int)((long long)(v_hi - v_lo) * w / kSampleWarps); }
     // f(value, index) for this thread's elements
     template <typename F>
     __device__ __forceinline__ void each(F f) const {
@@ -119,14 +151,11 @@ struct Row {
     }
 };
 
-// The kept set: elements ahead of (key, index) in the order.
+// The kept set: elements ahead of (x, index) in the order; at first everything above -inf.
 struct Cut {
-    unsigned int key;
+    float x;
     int index;
-    __device__ __forceinline__ bool keeps(float x, int i) const {
-        const unsigned int k = order_key(x);
-        return k > key || (k == key && i < index);
-    }
+    __device__ __forceinline__ bool keeps(float v, int i) const { return v > x || (v == x && i < index); }
 };
 
 __device__ __forceinline__ double warp_sum(double v) {
@@ -180,15 +209,114 @@ __device__ __forceinline__ S block_scan(S v, S *warp_buf, S *total) {
     return before + excl;
 }
 
+// The blocks that share a row: a cluster (kTeam), or one block.  Values cross through `slot`, by turns, so that one
+// barrier per exchange is enough: a block can be one exchange ahead of another, not two.
+template <bool kTeam>
+struct Team {
+    SampleSmem &sm;
+    int rank, size, turn;
+    template <typename U>
+    __device__ __forceinline__ U *of(U *p, int r) const {    // block r's copy of a shared variable
+        if (!kTeam) return p;
+        U *q;
+        asm("mapa.u64 %0, %1, %2;" : "=l"(q) : "l"(p), "r"(r));
+        return q;
+    }
+    __device__ __forceinline__ void barrier() const {
+        if (kTeam) asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+        else __syncthreads();
+    }
+    __device__ __forceinline__ double sum(double block_value) {              // of the blocks' values, in their order
+        if (!kTeam) return block_value;
+        if (threadIdx.x == 0) sm.slot[turn].d = block_value;
+        barrier();
+        double s = 0.0;
+        for (int r = 0; r < size; ++r) s += *of(&sm.slot[turn].d, r);
+        turn ^= 1;
+        return s;
+    }
+    // ... and what the blocks ahead of this one have
+    __device__ __forceinline__ double sum(double block_value, double &before) {
+        before = 0.0;
+        if (!kTeam) return block_value;
+        if (threadIdx.x == 0) sm.slot[turn].d = block_value;
+        barrier();
+        double s = 0.0;
+        for (int r = 0; r < size; ++r) {
+            if (r == rank) before = s;
+            s += *of(&sm.slot[turn].d, r);
+        }
+        turn ^= 1;
+        return s;
+    }
+    __device__ __forceinline__ unsigned int count(unsigned int block_value) {
+        if (!kTeam) return block_value;
+        if (threadIdx.x == 0) sm.slot[turn].u = block_value;
+        barrier();
+        unsigned int s = 0;
+        for (int r = 0; r < size; ++r) s += *of(&sm.slot[turn].u, r);
+        turn ^= 1;
+        return s;
+    }
+    // the largest of f, and the smallest and largest of u
+    __device__ __forceinline__ float max(float block_value) {
+        if (!kTeam) return block_value;
+        if (threadIdx.x == 0) sm.slot[turn].f = block_value;
+        barrier();
+        float s = -INFINITY;
+        for (int r = 0; r < size; ++r) s = fmaxf(s, *of(&sm.slot[turn].f, r));
+        turn ^= 1;
+        return s;
+    }
+    __device__ __forceinline__ int min_int(int block_value) {
+        if (!kTeam) return block_value;
+        if (threadIdx.x == 0) sm.slot[turn].u = (unsigned int)block_value;
+        barrier();
+        int s = INT_MAX;
+        for (int r = 0; r < size; ++r) s = ::min(s, (int)*of(&sm.slot[turn].u, r));
+        turn ^= 1;
+        return s;
+    }
+    __device__ __forceinline__ unsigned int max_key(unsigned int block_value) {
+        if (!kTeam) return block_value;
+        if (threadIdx.x == 0) sm.slot[turn].u = block_value;
+        barrier();
+        unsigned int s = 0;
+        for (int r = 0; r < size; ++r) s = ::max(s, *of(&sm.slot[turn].u, r));
+        turn ^= 1;
+        return s;
+    }
+    __device__ __forceinline__ unsigned int min_key(unsigned int block_value) {
+        if (!kTeam) return block_value;
+        return ~max_key(~block_value);
+    }
+};
+
 // Ascending sort of list[0, n), n <= kList, by the whole block (bitonic network on the next power of two).
 __device__ __forceinline__ void sort_list(SampleSmem &sm, int n) {
     int size = 2;
     while (size < n) size <<= 1;
     __syncthreads();
     for (int i = n + threadIdx.x; i < size; i += kSampleThreads) sm.list[i] = ~0ull;
+    __syncthreads();
+    if (size <= 32) {                                        // one warp, in registers
+        if (threadIdx.x < 32) {
+            unsigned long long v = (int)threadIdx.x < size ? sm.list[threadIdx.x] : ~0ull;
+#pragma unroll
+            for (int k = 2; k <= 32; k <<= 1)
+#pragma unroll
+                for (int j = k >> 1; j > 0; j >>= 1) {
+                    const unsigned long long o = __shfl_xor_sync(0xffffffffu, v, j);
+                    const bool up = ((threadIdx.x & k) == 0) == ((threadIdx.x & j) == 0);
+                    v = up ? ::min(v, o) : ::max(v, o);
+                }
+            if ((int)threadIdx.x < size) sm.list[threadIdx.x] = v;
+        }
+        __syncthreads();
+        return;
+    }
     for (int k = 2; k <= size; k <<= 1)
         for (int j = k >> 1; j > 0; j >>= 1) {
-            __syncthreads();
             for (int t = threadIdx.x; t < size / 2; t += kSampleThreads) {
                 const int i = 2 * t - (t & (j - 1)), o = i + j;
                 const unsigned long long a = sm.list[i], b = sm.list[o];
@@ -197,18 +325,16 @@ __device__ __forceinline__ void sort_list(SampleSmem &sm, int n) {
                     sm.list[o] = a;
                 }
             }
+            // distances up to 32 stay within the 64 entries of a warp's threads
+            if (j > 32 || (j == 1 && k >= 64)) __syncthreads();
+            else __syncwarp();
         }
     __syncthreads();
 }
 // A token as a list entry that sorts in the order: larger key first, lower index among equals.
 __device__ __forceinline__ unsigned long long list_entry(float x, int i) { return ((unsigned long long)~order_key(x) << 32) | (unsigned)i; }
-__device__ __forceinline__ unsigned int entry_key(unsigned long long e) { return ~(unsigned int)(e >> 32); }
+__device__ __forceinline__ float entry_value(unsigned long long e) { return key_value(~(unsigned int)(e >> 32)); }
 __device__ __forceinline__ int entry_index(unsigned long long e) { return (int)(unsigned int)e; }
-
-__device__ __forceinline__ void append(SampleSmem &sm, float x, int i) {
-    const int at = atomicAdd(&sm.n_list, 1);
-    if (at < kList) sm.list[at] = list_entry(x, i);
-}
 
 // The first entry of the sorted list[0, n) at which `above` plus the weight of the entries ahead reaches `goal`; n if none.
 // `sum_all` receives the weight of the whole list.
@@ -218,7 +344,7 @@ __device__ __forceinline__ int list_cut(SampleSmem &sm, const Weights &wt, int n
 #pragma unroll
     for (int u = 0; u < PER; ++u) {
         const int i = threadIdx.x * PER + u;
-        w[u] = i < n ? wt(key_value(entry_key(sm.list[i]))) : 0.0;
+        w[u] = i < n ? wt(entry_value(sm.list[i])) : 0.0;
         mine += w[u];
     }
     if (threadIdx.x == 0) sm.answer = n;
@@ -243,13 +369,12 @@ __device__ __forceinline__ int list_draw(SampleSmem &sm, const Weights &wt, int 
     if (n == 1) return entry_index(sm.list[0]);
     constexpr int PER = kList / kSampleThreads;
     __syncthreads();
-    unsigned long long e[PER];
 #pragma unroll
     for (int x = 0; x < PER; ++x) {
         const int i = threadIdx.x + x * kSampleThreads;
         if (i < n) {
-            e[x] = sm.list[i];
-            sm.list[i] = (e[x] << 32) | (e[x] >> 32);       // index first
+            const unsigned long long e = sm.list[i];
+            sm.list[i] = (e << 32) | (e >> 32);             // index first
         }
     }
     sort_list(sm, n);
@@ -277,33 +402,37 @@ __device__ __forceinline__ int list_draw(SampleSmem &sm, const Weights &wt, int 
     return (int)(unsigned int)(sm.list[at] >> 32);
 }
 
-template <typename T, bool kStaged>
+// What a block answers: a token, or that another block of the row has it.
+constexpr int kElsewhere = -2;
+
+template <typename T, bool kStaged, bool kTeam>
 struct Sampler {
+    static constexpr int VE = Vec16<T>::n;
     SampleSmem &sm;
+    Team<kTeam> &team;
     Row<T, kStaged> row;
     Weights wt;
     float m, cf;                          // largest logit; bins per unit of logit
 
-    __device__ __forceinline__ int bin(float x) const {
-        const float y = (m - x) * cf;
-        return y < (float)(kBins - 1) ? (int)y : kBins - 1;
-    }
+    // Distance to the largest in bins, and the bin (nearest whole number; the last bin takes all from there on).
+    __device__ __forceinline__ float depth(float x) const { return fminf((m - x) * cf, (float)(kBins - 1)); }
+    __device__ __forceinline__ int bin_of(float depth) const { return (int)(__float_as_uint(depth + 8388608.f) & 0x7ffu); }
 
-    // Elements ahead of the cut of a running count (top_k > 0) or weight (goal), by halving the range of the keys and
+    // Elements ahead of the cut of a running count (count_goal > 0) or weight (goal), by halving the range of the keys and
     // then of the indexes: exact for every distribution, one pass over the row per step.  For rows whose zone does not
     // fit the list: very many equal tokens, or a cut among tokens below 2^-32 of the largest.
-    __device__ __forceinline__ Cut slow_cut(const Cut &in, unsigned int count_goal, double goal) {
+    __device__ __noinline__ Cut slow_cut(const Cut in, unsigned int count_goal, double goal) {
         auto reaches = [&](unsigned int key, double *weight, unsigned int *count) {
             double w = 0.0;
             unsigned int c = 0;
             row.each([&](float x, int i) {
-                if (x > -INFINITY && order_key(x) >= key && in.keeps(x, i)) {
+                if (in.keeps(x, i) && order_key(x) >= key) {
                     ++c;
                     if (!count_goal) w += wt(x);
                 }
             });
-            *count = block_count(sm, c);
-            *weight = count_goal ? 0.0 : block_sum(sm, w);
+            *count = team.count(block_count(sm, c));
+            *weight = count_goal ? 0.0 : team.sum(block_sum(sm, w));
             return count_goal ? *count >= count_goal : *weight >= goal;
         };
         unsigned int lo = 0, hi = order_key(m);              // the answer: the largest key whose elements at or above it reach the goal
@@ -316,8 +445,7 @@ struct Sampler {
         }
         double w_above;
         unsigned int c_above;
-        if (lo == 0xFFFFFFFFu) { w_above = 0.0; c_above = 0; }
-        else reaches(lo + 1, &w_above, &c_above);
+        reaches(lo + 1, &w_above, &c_above);                 // (lo is the key of a finite value)
         // elements equal to it, in index order, are kept while the running count or weight before them is below the goal
         unsigned int ties;
         if (count_goal) {
@@ -334,71 +462,104 @@ struct Sampler {
             const int mid = a + (z - a) / 2;
             unsigned int n = 0;
             row.each([&](float x, int i) { n += order_key(x) == lo && i < mid && in.keeps(x, i); });
-            if (block_count(sm, n) >= ties) z = mid;
+            if (team.count(block_count(sm, n)) >= ties) z = mid;
             else a = mid + 1;
         }
-        return Cut{lo, a};
+        return Cut{key_value(lo), a};
     }
 
-    // Gathers the kept elements of bins [lo, hi] into the list; returns their number, which may exceed what the list holds.
-    // `above`: weight of the kept elements of lower bins (where asked for).
-    __device__ __forceinline__ int gather(const Cut &in, int lo, int hi, double *above) {
+    __device__ __forceinline__ void open_list() {            // (a barrier of the row lies behind every open_list)
         __syncthreads();
         if (threadIdx.x == 0) sm.n_list = 0;
-        __syncthreads();
-        double w = 0.0;
-        row.each([&](float x, int i) {
-            const int b = bin(x);
-            if (b <= hi && x > -INFINITY && in.keeps(x, i)) {
-                if (b >= lo) append(sm, x, i);
-                else if (above) w += wt(x);
-            }
-        });
-        if (above) *above = block_sum(sm, w);
-        __syncthreads();
-        return sm.n_list;
+        team.barrier();
+    }
+    __device__ __forceinline__ void append(float x, int i) { // to the first block's list
+        const int at = atomicAdd(team.of(&sm.n_list, 0), 1);
+        if (at < kList) *team.of(&sm.list[at], 0) = list_entry(x, i);
+    }
+    __device__ __forceinline__ int close_list() {            // entries asked for; they may exceed what the list holds
+        team.barrier();
+        return *team.of(&sm.n_list, 0);
     }
 
-    // Counts of the kept elements by bin, and their weight.
+    // Gathers the kept elements of bins [lo, hi] into the first block's list.  kAbove: *above receives the weight of the kept
+    // elements of lower bins; sm.part the warps' shares of it.
+    template <bool kAbove>
+    __device__ __forceinline__ int gather(const Cut &in, int lo, int hi, double *above) {
+        open_list();
+        double w = 0.0;
+        row.each([&](float x, int i) {
+            const int b = bin_of(depth(x));
+            if (b <= hi && in.keeps(x, i)) {
+                if (b >= lo) append(x, i);
+                else if (kAbove) wt.add_to(w, x);
+            }
+        });
+        if (kAbove) {
+            *above = team.sum(block_sum(sm, w));
+            if (threadIdx.x < kSampleWarps) sm.part[threadIdx.x] = sm.wsum[threadIdx.x];
+        }
+        return close_list();
+    }
+
+    // Counts of the kept elements by bin, summed over the row's blocks in the first one, and (kWeight) their weight.
+    // The histogram shares its memory with the list: a barrier of the row lies between the uses.
     template <bool kWeight>
     __device__ __forceinline__ double histogram(const Cut &in) {
         __syncthreads();
         for (int i = threadIdx.x; i < kBins; i += kSampleThreads) sm.hist[i] = 0u;
         __syncthreads();
         double w = 0.0;
+        float w_low = 0.f;                                   // below 2^-32 of the largest: 32 bits are enough
         unsigned int low = 0;                                // the last bin may hold most of the row: counted in registers
         row.each([&](float x, int i) {
-            if (x > -INFINITY && in.keeps(x, i)) {
-                const int b = bin(x);
-                if (b < kBins - 1) atomicAdd(&sm.hist[b], 1u);
-                else ++low;
-                if (kWeight) w += wt(x);
+            if (in.keeps(x, i)) {
+                const int b = bin_of(depth(x));
+                if (b < kBins - 1) {
+                    atomicAdd(&sm.hist[b], 1u);
+                    if (kWeight) wt.add_to(w, x);
+                } else {
+                    ++low;
+                    if (kWeight) w_low += exp2f((x - m) * (cf * (1.f / kBinsPerOctave)));
+                }
             }
         });
         low = block_count(sm, low);
         if (threadIdx.x == 0) sm.hist[kBins - 1] = low;
-        return kWeight ? block_sum(sm, w) : 0.0;
+        double sum = 0.0;
+        if (kWeight) sum = team.sum(block_sum(sm, w + (double)w_low));
+        else team.barrier();
+        if (kTeam && team.rank == 0) {
+            for (int i = threadIdx.x; i < kBins; i += kSampleThreads) {
+                unsigned int c = sm.hist[i];
+                for (int r = 1; r < team.size; ++r) c += *team.of(&sm.hist[i], r);
+                sm.hist[i] = c;
+            }
+        }
+        return sum;
     }
 
-    // First bin at which the running count reaches `goal` (sm.zone_lo = sm.zone_hi), counts before it (sm.n_above) and in all (sm.total).
+    // First bin at which the running count reaches `goal` (sm.zone_lo = -1: none does), and the count before it (sm.n_above).
     __device__ __forceinline__ void find_count(unsigned int goal) {
         constexpr int PER = kBins / kSampleThreads;
         __syncthreads();
-        unsigned int c[PER], mine = 0, all;
+        if (!kTeam || team.rank == 0) {
+            unsigned int c[PER], mine = 0, all;
 #pragma unroll
-        for (int u = 0; u < PER; ++u) mine += c[u] = sm.hist[threadIdx.x * PER + u];
-        unsigned int before = block_scan(mine, sm.wcount, &all);
-        if (threadIdx.x == 0) { sm.total = all; sm.zone_lo = -1; }
-        __syncthreads();
+            for (int u = 0; u < PER; ++u) mine += c[u] = sm.hist[threadIdx.x * PER + u];
+            unsigned int before = block_scan(mine, sm.wcount, &all);
+            if (threadIdx.x == 0) sm.zone_lo = -1;
+            __syncthreads();
 #pragma unroll
-        for (int u = 0; u < PER; ++u) {
-            if (before < goal && before + c[u] >= goal) {
-                sm.zone_lo = threadIdx.x * PER + u;
-                sm.n_above = (int)before;
+            for (int u = 0; u < PER; ++u) {
+                if (before < goal && before + c[u] >= goal) {
+                    sm.zone_lo = threadIdx.x * PER + u;
+                    sm.n_above = (int)before;
+                }
+                before += c[u];
             }
-            before += c[u];
         }
-        __syncthreads();
+        team.barrier();
     }
 
     // Bins that may hold the cut of a running weight, `total` being the weight of all.  With every element of a bin taken
@@ -411,81 +572,110 @@ struct Sampler {
     __device__ __forceinline__ void find_weight(double goal, double total) {
         constexpr int PER = kBins / kSampleThreads;
         __syncthreads();
-        unsigned int c[PER], mine_c = 0, all_c;
-        double up[PER], dn[PER], mine_up = 0.0, mine_dn = 0.0, all_up, all_dn;
+        if (!kTeam || team.rank == 0) {
+            unsigned int c[PER], mine_c = 0, all_c;
+            double up[PER], dn[PER], mine_up = 0.0, mine_dn = 0.0, all_up, all_dn;
 #pragma unroll
-        for (int u = 0; u < PER; ++u) {
-            const int b = threadIdx.x * PER + u;
-            c[u] = sm.hist[b];
-            const float edge = exp2f(-(float)b / kBinsPerOctave);
-            up[u] = c[u] * ((double)edge * 1.00001);
-            dn[u] = b == kBins - 1 ? 0.0 : c[u] * ((double)edge * (0.98922 * 0.99999));   // 2^(-1/64) = 0.989228...
-            mine_c += c[u];
-            mine_up += up[u];
-            mine_dn += dn[u];
-        }
-        unsigned int before_c = block_scan(mine_c, sm.wcount, &all_c);
-        double sum_up = block_scan(mine_up, sm.wsum, &all_up);
-        double sum_dn = block_scan(mine_dn, sm.wsum, &all_dn);
-        if (threadIdx.x == 0) { sm.zone_lo = kBins - 1; sm.zone_hi = kBins - 1; sm.total = all_c; }
-        __syncthreads();
+            for (int u = 0; u < PER; ++u) {
+                const int b = threadIdx.x * PER + u;
+                c[u] = sm.hist[b];
+                const float edge = exp2f((0.5f - (float)b) / kBinsPerOctave);
+                up[u] = c[u] * ((double)edge * 1.00001);
+                dn[u] = b == kBins - 1 ? 0.0 : c[u] * ((double)edge * (0.98922 * 0.99999));   // 2^(-1/64) = 0.989228...
+                mine_c += c[u];
+                mine_up += up[u];
+                mine_dn += dn[u];
+            }
+            unsigned int before_c = block_scan(mine_c, sm.wcount, &all_c);
+            double sum_up = block_scan(mine_up, sm.wsum, &all_up);
+            double sum_dn = block_scan(mine_dn, sm.wsum, &all_dn);
+            if (threadIdx.x == 0) { sm.zone_lo = kBins - 1; sm.zone_hi = kBins - 1; sm.total = all_c; }
+            __syncthreads();
 #pragma unroll
-        for (int u = 0; u < PER; ++u) {
-            const int b = threadIdx.x * PER + u;
-            sum_up += up[u];
-            sum_dn += dn[u];
-            if (fmin(sum_up, total - (all_dn - sum_dn)) >= goal) atomicMin(&sm.zone_lo, b);
-            if (fmax(sum_dn, total - (all_up - sum_up)) >= goal) atomicMin(&sm.zone_hi, b);
-        }
-        __syncthreads();
-        const int hi = sm.zone_hi;
+            for (int u = 0; u < PER; ++u) {
+                const int b = threadIdx.x * PER + u;
+                sum_up += up[u];
+                sum_dn += dn[u];
+                if (fmin(sum_up, total - (all_dn - sum_dn)) >= goal) atomicMin(&sm.zone_lo, b);
+                if (fmax(sum_dn, total - (all_up - sum_up)) >= goal) atomicMin(&sm.zone_hi, b);
+            }
+            __syncthreads();
+            const int hi = sm.zone_hi;
 #pragma unroll
-        for (int u = 0; u < PER; ++u) {
-            before_c += c[u];
-            if (threadIdx.x * PER + u == hi) sm.total = before_c;
+            for (int u = 0; u < PER; ++u) {
+                before_c += c[u];
+                if (threadIdx.x * PER + u == hi) sm.total = before_c;
+            }
         }
+        team.barrier();
+    }
+
+    // Weight of an element for the draw: ahead of the cut and w >= floor.
+    __device__ __forceinline__ double kept_weight(const Cut &cut, double floor, float x, int i) const {
+        if (!cut.keeps(x, i)) return 0.0;
+        const double w = wt(x);
+        return w >= floor ? w : 0.0;
+    }
+
+    // sm.part: the warps' kept weights.
+    __device__ __forceinline__ void sum_kept(const Cut &cut, double floor, bool exact) {
+        double mine = 0.0;
+        float low = 0.f;
+        const float none = (float)(kBins - 1) - 0.5f;
+        if (floor > 0.0 || exact) {
+            row.each([&](float x, int i) { mine += kept_weight(cut, floor, x, i); });
+        } else {
+            row.each([&](float x, int i) {
+                if (cut.keeps(x, i)) {
+                    if (depth(x) < none) wt.add_to(mine, x);
+                    else low += exp2f((x - m) * (cf * (1.f / kBinsPerOctave)));
+                }
+            });
+        }
+        mine = warp_sum(mine + (double)low);
+        if ((threadIdx.x & 31) == 0) sm.part[threadIdx.x >> 5] = mine;
         __syncthreads();
     }
 
-    // The token by one pass of sums and the walk of one warp's range: kept = ahead of the cut and w >= floor.
-    __device__ __forceinline__ int draw(const Cut &cut, double floor, double u) {
-        auto weight = [&](float x, int i) {
-            if (!(x > -INFINITY) || !cut.keeps(x, i)) return 0.0;
-            const double w = wt(x);
-            return w >= floor ? w : 0.0;
-        };
-        double mine = 0.0;
-        row.each([&](float x, int i) { mine += weight(x, i); });
-        const double goal = u * block_sum(sm, mine);
-        double before = 0.0;
+    // The token, given the warps' kept weights in sm.part: the block that holds it walks one warp's range.
+    __device__ __forceinline__ int locate(const Cut &cut, double floor, double u) {
+        double block = 0.0, before;
+        for (int w = 0; w < kSampleWarps; ++w) block += sm.part[w];
+        const double goal = u * team.sum(block, before);
         int seg = -1;
         for (int w = 0; w < kSampleWarps; ++w) {
-            const double s = sm.wsum[w];
+            const double s = sm.part[w];
             if (s > 0.0) {
                 if (before + s > goal) { seg = w; break; }
                 before += s;
             }
         }
-        __syncthreads();
-        if (seg < 0) {                                        // uniform = 1: the last one with a weight
+        // the first block of the row with such a warp
+        const int owner_block = team.min_int(seg >= 0 ? team.rank : INT_MAX);
+        if (owner_block == INT_MAX) {                         // uniform = 1 (or rounding): the last one with a weight
+            int last = -1;
+            row.each([&](float x, int i) { if (kept_weight(cut, floor, x, i) > 0.0) last = ::max(last, i); });
+            last = __reduce_max_sync(0xffffffffu, last);
+            __syncthreads();
             if (threadIdx.x == 0) sm.answer = -1;
             __syncthreads();
-            int last = -1;
-            row.each([&](float x, int i) { if (weight(x, i) > 0.0) last = max(last, i); });
-            atomicMax(&sm.answer, last);
+            if ((threadIdx.x & 31) == 0) atomicMax(&sm.answer, last);
             __syncthreads();
-            return sm.answer;
+            last = -1 - team.min_int(-1 - sm.answer);         // the largest
+            return team.rank == 0 ? last : kElsewhere;
         }
+        if (owner_block != team.rank) return kElsewhere;
         const int first = row.warp_first(seg), n = row.warp_first(seg + 1) - first;
         const int per = (n + kSampleThreads - 1) / kSampleThreads;
-        const int v0 = first + min(n, (int)threadIdx.x * per), v1 = first + min(n, ((int)threadIdx.x + 1) * per);
-        mine = 0.0;
+        const int v0 = first + ::min(n, (int)threadIdx.x * per), v1 = first + ::min(n, ((int)threadIdx.x + 1) * per);
+        double mine = 0.0;
         for (int v = v0; v < v1; ++v) {
-            float x[Row<T, kStaged>::VE];
+            float x[VE];
             row.load(v, x);
 #pragma unroll
-            for (int e = 0; e < Row<T, kStaged>::VE; ++e) mine += weight(x[e], row.index(v, e));
+            for (int e = 0; e < VE; ++e) mine += kept_weight(cut, floor, x[e], row.index(v, e));
         }
+        __syncthreads();
         if (threadIdx.x == 0) { sm.first_thread = INT_MAX; sm.answer = -1; }
         double all, running = before + block_scan(mine, sm.wsum, &all);
         // the first thread whose range passes the goal; should rounding leave none, the last with a weight
@@ -498,12 +688,11 @@ struct Sampler {
             int best = -1;
             bool found = false;
             for (int v = v0; v < v1 && !found; ++v) {
-                float x[Row<T, kStaged>::VE];
+                float x[VE];
                 row.load(v, x);
-#pragma unroll
-                for (int e = 0; e < Row<T, kStaged>::VE; ++e) {
-                    const double w = weight(x[e], row.index(v, e));
-                    if (!found && w > 0.0) {
+                for (int e = 0; e < VE && !found; ++e) {
+                    const double w = kept_weight(cut, floor, x[e], row.index(v, e));
+                    if (w > 0.0) {
                         running += w;
                         best = row.index(v, e);
                         found = running > goal;
@@ -516,73 +705,125 @@ struct Sampler {
         return sm.answer;
     }
 
-    __device__ int sample(float thread_max, float Tm, int top_k, float top_p, float min_p, float uniform) {
+    // The cut that the first block found, told to all.
+    __device__ __forceinline__ Cut share(const Cut &cut) {
+        if (threadIdx.x == 0 && team.rank == 0) { sm.cut_x = cut.x; sm.cut_i = cut.index; }
+        team.barrier();
+        return Cut{*team.of(&sm.cut_x, 0), *team.of(&sm.cut_i, 0)};
+    }
+
+    __device__ __forceinline__ int sample(float thread_max, int top_k, float top_p, float min_p, float uniform) {
         const double u = (double)uniform, floor = min_p > 0.f ? (double)min_p : 0.0;
-        Cut cut{0u, INT_MAX};                                 // keeps everything above -inf
-        bool p_on = top_p < 1.f;
+        const bool first = !kTeam || team.rank == 0;
+        Cut cut{-INFINITY, 0};                                // keeps everything above -inf
+        const bool p_on = top_p < 1.f;
         if (top_k > 0 && top_k < row.V) {
             if (top_k <= kSampleThreads) {
-                // the k-th largest of the threads' maxima bounds the k-th largest token from below
+                // Lower bounds of the k-th largest token: the k-th largest of a block's thread maxima, and the smallest of
+                // the blocks' ceil(k / blocks)-th largest.
                 const unsigned int mine = order_key(thread_max);
-                unsigned int key = 0;
-                for (int bit = 31; bit >= (sizeof(T) == 2 ? 13 : 0); --bit) {     // (a 16-bit value has no lower bits: fp16 reaches bit 13)
-                    const unsigned int cand = key | (1u << bit);
-                    if (__syncthreads_count(mine >= cand) >= top_k) key = cand;
-                }
-                if (threadIdx.x == 0) sm.n_list = 0;
-                __syncthreads();
-                row.each([&](float x, int i) { if (x > -INFINITY && order_key(x) >= key) append(sm, x, i); });
-                __syncthreads();
-                int n = sm.n_list;
+                auto kth = [&](int k) {
+                    unsigned int key = 0;
+                    for (int bit = 31; bit >= (sizeof(T) == 2 ? 13 : 0); --bit) {    // (a 16-bit value has no lower bits: fp16 reaches bit 13)
+                        const unsigned int cand = key | (1u << bit);
+                        if (__syncthreads_count(mine >= cand) >= k) key = cand;
+                    }
+                    return key;
+                };
+                unsigned int key = team.max_key(kth(top_k));
+                if (kTeam) key = ::max(key, team.min_key(kth((top_k + team.size - 1) / team.size)));
+                open_list();
+                row.each([&](float x, int i) { if (x > -INFINITY && order_key(x) >= key) append(x, i); });
+                int n = close_list();
                 if (n <= kList) {
+                    if (!first) return kElsewhere;
                     sort_list(sm, n);
-                    n = min(n, top_k);
+                    n = ::min(n, top_k);
                     return finish_list(n, p_on, top_p, -1.0, floor, u);
                 }
+                team.barrier();                               // (the first block's list is done with)
             }
             histogram<false>(cut);
             find_count((unsigned int)top_k);
-            if (sm.zone_lo >= 0) {                            // more than k tokens above -inf
-                const int zone = sm.zone_lo, above = sm.n_above;
+            const int zone = *team.of(&sm.zone_lo, 0), above = *team.of(&sm.n_above, 0);
+            if (zone >= 0) {                                  // at least k tokens above -inf
                 bool done = false;
                 if (zone < kBins - 1) {
-                    const int n = gather(cut, zone, zone, nullptr);
+                    const int n = gather<false>(cut, zone, zone, nullptr);
                     if (n <= kList) {
-                        sort_list(sm, n);
-                        if (top_k - above < n) cut = Cut{entry_key(sm.list[top_k - above]), entry_index(sm.list[top_k - above])};
-                        else cut = Cut{entry_key(sm.list[n - 1]), INT_MAX};
+                        Cut c = cut;
+                        if (first) {
+                            sort_list(sm, n);
+                            const bool inside = top_k - above < n;
+                            const unsigned long long e = sm.list[inside ? top_k - above : n - 1];
+                            c = Cut{entry_value(e), inside ? entry_index(e) : INT_MAX};
+                        }
+                        cut = share(c);
                         done = true;
                     }
                 }
                 if (!done) cut = slow_cut(cut, (unsigned int)top_k, 0.0);
             }
+            team.barrier();
         }
         if (p_on) {
             const double Z = histogram<true>(cut);
             const double goal = (double)top_p * Z;
             find_weight(goal, Z);
-            const int lo = sm.zone_lo, hi = sm.zone_hi;
-            const unsigned int upto = sm.total;
+            const int lo = *team.of(&sm.zone_lo, 0), hi = *team.of(&sm.zone_hi, 0);
+            const unsigned int upto = *team.of(&sm.total, 0);
             if (hi < kBins - 1 && upto <= kList) {            // the whole kept set fits the list
-                const int n = gather(cut, 0, hi, nullptr);
+                const int n = gather<false>(cut, 0, hi, nullptr);
+                if (!first) return kElsewhere;
                 sort_list(sm, n);
                 return finish_list(n, true, top_p, Z, floor, u);
             }
             bool done = false;
             if (hi < kBins - 1) {
                 double above;
-                const int n = gather(cut, lo, hi, &above);
+                const int n = gather<true>(cut, lo, hi, &above);
                 if (n <= kList) {
-                    sort_list(sm, n);
-                    double sum;
-                    const int at = list_cut(sm, wt, n, above, goal, &sum);
-                    cut = at < n ? Cut{entry_key(sm.list[at]), entry_index(sm.list[at])} : Cut{entry_key(sm.list[n - 1]), INT_MAX};
+                    Cut c = cut;
+                    if (first) {
+                        sort_list(sm, n);
+                        double sum;
+                        const int at = list_cut(sm, wt, n, above, goal, &sum);
+                        c = at < n ? Cut{entry_value(sm.list[at]), entry_index(sm.list[at])} : Cut{entry_value(sm.list[n - 1]), INT_MAX};
+                    }
+                    const Cut p_cut = share(c);
+                    if (floor == 0.0 && u > 0.0) {
+                        // the warps' kept weights: what lies above the zone, and their tokens of the list
+                        add_list(n, p_cut);
+                        return locate(p_cut, 0.0, u);
+                    }
+                    cut = p_cut;
                     done = true;
                 }
             }
             if (!done) cut = slow_cut(cut, 0u, goal);
         }
-        return draw(cut, floor, u);
+        sum_kept(cut, floor, u == 0.0);
+        return locate(cut, floor, u);
+    }
+
+    // Adds the kept tokens of the first block's list[0, n) to the warps' weights in sm.part, in the list's order.
+    __device__ __forceinline__ void add_list(int n, const Cut &cut) {
+        if (kTeam && team.rank != 0) {
+            for (int i = threadIdx.x; i < n; i += kSampleThreads) sm.list[i] = *team.of(&sm.list[i], 0);
+        }
+        team.barrier();
+        const int w = threadIdx.x >> 5, lane = threadIdx.x & 31;
+        const int i0 = row.index(row.warp_first(w), 0), i1 = row.index(row.warp_first(w + 1), 0);
+        double mine = 0.0;
+        for (int i = lane; i < n; i += 32) {
+            const unsigned long long e = sm.list[i];
+            const int at = entry_index(e);
+            if (at >= i0 && at < i1 && cut.keeps(entry_value(e), at)) mine += wt(entry_value(e));
+        }
+        mine = warp_sum(mine);
+        __syncwarp();
+        if (lane == 0) sm.part[w] += mine;
+        __syncthreads();
     }
 
     // list[0, n): the first n of the order.  total < 0: the weight that top_p refers to is the list's own.
@@ -593,49 +834,64 @@ struct Sampler {
                 list_cut(sm, wt, n, 0.0, INFINITY, &sum);
                 total = sum;
             }
-            n = max(1, list_cut(sm, wt, n, 0.0, (double)top_p * total, &sum));
+            n = ::max(1, list_cut(sm, wt, n, 0.0, (double)top_p * total, &sum));
         }
         if (n > 1 && floor > 0.0) {
             int c = 0;
-            for (int i = threadIdx.x; i < n; i += kSampleThreads) c += wt(key_value(entry_key(sm.list[i]))) >= floor;
-            n = max(1, (int)block_count(sm, (unsigned int)c));
+            for (int i = threadIdx.x; i < n; i += kSampleThreads) c += wt(entry_value(sm.list[i])) >= floor;
+            n = ::max(1, (int)block_count(sm, (unsigned int)c));
         }
         return list_draw(sm, wt, n, u);
     }
 };
 
-// Copies the row into shared memory at its own 16-byte phase (nothing outside the row is read), -inf around it.
+// Copies vectors [v_lo, v_hi) of the row into shared memory at their own 16-byte phase (nothing outside the row is read),
+// -inf around the row.
 template <typename T>
-__device__ __forceinline__ void stage_row(T *dst, const T *src, int V, int phase, int vecs) {
+__device__ __forceinline__ void stage_row(T *dst, const T *src, int V, int phase, int v_lo, int v_hi) {
     constexpr int VE = Vec16<T>::n;
     const T *base = src - phase;
-    for (int v = threadIdx.x; v < vecs; v += kSampleThreads) {
+    for (int v = v_lo + threadIdx.x; v < v_hi; v += kSampleThreads) {
         const int i0 = v * VE - phase;
+        T *d = dst + (v - v_lo) * VE;
         if (i0 >= 0 && i0 + VE <= V) {
-            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(dst + v * VE)), "l"(base + (size_t)v * VE) : "memory");
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(d)), "l"(base + (size_t)v * VE) : "memory");
         } else {
-            for (int e = 0; e < VE; ++e) dst[v * VE + e] = (i0 + e >= 0 && i0 + e < V) ? src[i0 + e] : from_float<T>(-INFINITY);
+            for (int e = 0; e < VE; ++e) d[e] = (i0 + e >= 0 && i0 + e < V) ? src[i0 + e] : from_float<T>(-INFINITY);
         }
     }
-    asm volatile("cp.async.commit_group;\ncp.async.wait_group 0;" ::: "memory");
-    __syncthreads();
+    asm volatile("cp.async.commit_group;" ::: "memory");
 }
 
-template <typename T, bool kStaged, bool kVerify>
+template <typename T, bool kStaged, bool kTeam, bool kVerify>
 __global__ void __launch_bounds__(kSampleThreads, 2)
 sample_kernel(const SampleArgs a) {
     constexpr int VE = Vec16<T>::n;
     extern __shared__ uint4 s_dyn[];
     __shared__ SampleSmem sm;
     __shared__ int s_last;
-    const int b = blockIdx.x / a.R, r = blockIdx.x - b * a.R;
+    Team<kTeam> team{sm, 0, 1, 0};
+    if (kTeam) {
+        asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(team.rank));
+        asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(team.size));
+    }
+    const int unit = kTeam ? (int)blockIdx.x / team.size : (int)blockIdx.x;
+    const int b = unit / a.R, r = unit - b * a.R;
+    if (threadIdx.x < 16) sm.pow2[threadIdx.x] = exp2((double)threadIdx.x / 16.0);
+    // The launch is serialized programmatically behind the kernel ahead of it in the stream: from here on everything
+    // that kernel wrote may be read.  A kernel serialized behind this one may set itself up meanwhile.
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const T *src = static_cast<const T *>(a.logits) + ((size_t)b * a.N + r) * a.V;
     Row<T, kStaged> row;
     row.phase = (int)((reinterpret_cast<uintptr_t>(src) & 15) / sizeof(T));
     row.V = a.V;
-    row.vecs = (row.phase + a.V + VE - 1) / VE;
+    const int vecs = (row.phase + a.V + VE - 1) / VE, share = (vecs + team.size - 1) / team.size;
+    row.v_lo = min(vecs, team.rank * share);
+    row.v_hi = min(vecs, row.v_lo + share);
     row.peak = false;
-    if (threadIdx.x < 16) sm.pow2[threadIdx.x] = exp2((double)threadIdx.x / 16.0);
+    if (kStaged) stage_row<T>(reinterpret_cast<T *>(s_dyn), src, a.V, row.phase, row.v_lo, row.v_hi);
+    row.base = kStaged ? reinterpret_cast<const T *>(s_dyn) : src - row.phase;
     // parameters of the sequence; every block of it comes to the same decision
     const float Tm = a.temperature ? a.temperature[b] : 1.f;
     const int top_k = a.top_k ? a.top_k[b] : 0;
@@ -646,16 +902,10 @@ sample_kernel(const SampleArgs a) {
         const float x = a.uniform[(size_t)b * a.N + i];
         bad |= !(x >= 0.f && x <= 1.f);
     }
+    if (kStaged) asm volatile("cp.async.wait_group 0;" ::: "memory");
     bad = __syncthreads_or(bad);
     int token = -1;
     if (!bad) {
-        if (kStaged) {
-            T *dst = reinterpret_cast<T *>(s_dyn);
-            stage_row<T>(dst, src, a.V, row.phase, row.vecs);
-            row.base = dst;
-        } else {
-            row.base = src - row.phase;
-        }
         // largest value (NaN aside); staged rows are rewritten without NaN
         float mx = -INFINITY;
         {
@@ -670,7 +920,7 @@ sample_kernel(const SampleArgs a) {
                     mx = fmaxf(mx, x[e]);                    // (the other operand where one is NaN)
                 }
                 if (kStaged && nan) {
-                    T *d = reinterpret_cast<T *>(s_dyn) + v * VE;
+                    T *d = reinterpret_cast<T *>(s_dyn) + (v - row.v_lo) * VE;
                     for (int e = 0; e < VE; ++e)
                         if (!(x[e] == x[e])) d[e] = from_float<T>(-INFINITY);
                 }
@@ -683,14 +933,19 @@ sample_kernel(const SampleArgs a) {
         __syncthreads();
 #pragma unroll
         for (int w = 0; w < kSampleWarps; ++w) m = fmaxf(m, sm.wmax[w]);
+        m = team.max(m);
         if (m == -INFINITY) {
             // nothing above -inf: the first -inf, or 0 in a row of NaNs, as the greedy verification has it
-            if (threadIdx.x == 0) sm.answer = INT_MAX;
-            __syncthreads();
-            for (int i = threadIdx.x; i < a.V; i += kSampleThreads)
-                if (to_float<T>(src[i]) == -INFINITY) { atomicMin(&sm.answer, i); break; }
-            __syncthreads();
-            token = sm.answer == INT_MAX ? 0 : sm.answer;
+            if (team.rank == 0) {
+                if (threadIdx.x == 0) sm.answer = INT_MAX;
+                __syncthreads();
+                for (int i = threadIdx.x; i < a.V; i += kSampleThreads)
+                    if (to_float<T>(src[i]) == -INFINITY) { atomicMin(&sm.answer, i); break; }
+                __syncthreads();
+                token = sm.answer == INT_MAX ? 0 : sm.answer;
+            } else {
+                token = kElsewhere;
+            }
         } else if (Tm == 0.f || top_k == 1 || top_p <= 0.f) {
             if (threadIdx.x == 0) sm.answer = INT_MAX;
             __syncthreads();
@@ -699,12 +954,13 @@ sample_kernel(const SampleArgs a) {
             first = __reduce_min_sync(0xffffffffu, first);
             if ((threadIdx.x & 31) == 0) atomicMin(&sm.answer, first);
             __syncthreads();
-            token = sm.answer;
+            token = team.min_int(sm.answer);
+            if (team.rank != 0) token = kElsewhere;
         } else {
             if (m == INFINITY) {                             // the +inf tokens share the weight, the others have none
                 if (kStaged) {
                     T *d = reinterpret_cast<T *>(s_dyn);
-                    for (int i = threadIdx.x; i < row.vecs * VE; i += kSampleThreads)
+                    for (int i = threadIdx.x; i < (row.v_hi - row.v_lo) * VE; i += kSampleThreads)
                         d[i] = from_float<T>(to_float<T>(d[i]) == INFINITY ? 0.f : -INFINITY);
                 }
                 row.peak = true;
@@ -713,10 +969,13 @@ sample_kernel(const SampleArgs a) {
                 __syncthreads();
             }
             const float cf = fminf(kBinsPerOctave * kLog2eF / Tm, 1e30f);
-            Sampler<T, kStaged> s{sm, row, Weights{(double)m, 16.0 * 1.4426950408889634074 / (double)Tm, sm.pow2}, m, cf};
-            token = s.sample(mx, Tm, top_k, top_p, min_p, a.uniform[(size_t)b * a.N + r]);
+            Sampler<T, kStaged, kTeam> s{sm, team, row, Weights{wide(m), 16.0 * 1.4426950408889634074 / (double)Tm, sm.pow2}, m, cf};
+            token = s.sample(mx, top_k, top_p, min_p, a.uniform[(size_t)b * a.N + r]);
         }
     }
+    // A block leaves its shared memory behind only when no other block of the row may still read it.
+    if (kTeam) team.barrier();
+    if (bad ? team.rank != 0 : token == kElsewhere) return;
     if (!kVerify) {
         if (threadIdx.x == 0) {
             a.token[(size_t)b * a.N + r] = token;
@@ -758,38 +1017,61 @@ sample_kernel(const SampleArgs a) {
 // Shared memory a block may take beyond its static part (227 KB per SM in all).
 constexpr size_t kSampleDynMax = 227 * 1024 - sizeof(SampleSmem) - 1024;
 
-template <typename T, bool kStaged, bool kVerify>
-static cudaError_t launch_shape(const SampleArgs &a, size_t smem, cudaStream_t s) {
+template <typename T, bool kStaged, bool kTeam, bool kVerify>
+static cudaError_t launch_shape(const SampleArgs &a, int team, size_t smem, cudaStream_t s) {
     static bool raised[64];                                  // per device: the kernel's shared memory limit
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
+    auto kernel = sample_kernel<T, kStaged, kTeam, kVerify>;
     if (dev < 0 || dev >= 64 || !raised[dev]) {
-        e = cudaFuncSetAttribute(sample_kernel<T, kStaged, kVerify>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSampleDynMax);
+        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSampleDynMax);
         if (e != cudaSuccess) return e;
         if (dev >= 0 && dev < 64) raised[dev] = true;
     }
-    sample_kernel<T, kStaged, kVerify><<<(unsigned)((long long)a.B * a.R), kSampleThreads, smem, s>>>(a);
-    return cudaPeekAtLastError();
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)((long long)a.B * a.R * team));
+    cfg.blockDim = dim3(kSampleThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)team;
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = kTeam ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, kernel, a);
 }
 
 template <typename T>
-static cudaError_t launch_t(const SampleArgs &a, cudaStream_t s) {
-    const size_t staged = ((size_t)a.V * sizeof(T) + 15 + 15) / 16 * 16;
+static cudaError_t launch_t(const SampleArgs &a, const char *what, cudaStream_t s) {
+    // Blocks per row: as many as rows are too few to fill the GPU with, and as many as it takes for the slices to fit
+    // shared memory two to an SM.
+    const long long rows = (long long)a.B * a.R;
+    auto slice = [&](int team) { return (((size_t)a.V * sizeof(T) + 15 + 15) / 16 + team - 1) / team * 16; };
+    int team = 1;
+    while (team < kMaxTeam && (slice(team) > kSampleDynMax / 2 || (rows * team * 2 <= 2 * 148 && slice(team) > 8192))) team *= 2;
+    const bool staged = slice(team) <= kSampleDynMax;
     const size_t tree = a.tokens ? sizeof(TreeSmem) : 0;
-    if (staged <= kSampleDynMax) {
-        const size_t smem = staged > tree ? staged : tree;
-        return a.tokens ? launch_shape<T, true, true>(a, smem, s) : launch_shape<T, true, false>(a, smem, s);
+    const size_t smem = staged && slice(team) > tree ? slice(team) : tree;
+    trace("%s -> %d block(s) per row, %s", what, team, staged ? "staged" : "from global memory");
+    if (a.tokens) {
+        if (!staged) return launch_shape<T, false, true, true>(a, team, smem, s);
+        return team > 1 ? launch_shape<T, true, true, true>(a, team, smem, s) : launch_shape<T, true, false, true>(a, team, smem, s);
     }
-    return a.tokens ? launch_shape<T, false, true>(a, tree, s) : launch_shape<T, false, false>(a, tree, s);
+    if (!staged) return launch_shape<T, false, true, false>(a, team, smem, s);
+    return team > 1 ? launch_shape<T, true, true, false>(a, team, smem, s) : launch_shape<T, true, false, false>(a, team, smem, s);
 }
 
 int launch_sample(const SampleArgs &a, int dtype, const char *what, cudaStream_t s) {
     cudaError_t e;
     switch (dtype) {
-        case HT_F32: e = launch_t<float>(a, s); break;
-        case HT_F16: e = launch_t<__half>(a, s); break;
-        default: e = launch_t<__nv_bfloat16>(a, s); break;
+        case HT_F32: e = launch_t<float>(a, what, s); break;
+        case HT_F16: e = launch_t<__half>(a, what, s); break;
+        default: e = launch_t<__nv_bfloat16>(a, what, s); break;
     }
     if (e != cudaSuccess) {
         cudaGetLastError();

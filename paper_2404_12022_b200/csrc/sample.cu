@@ -19,6 +19,7 @@
 // the whole kept set, where it is small) are sorted by the cluster's first block and the cut is found exactly.  A small
 // top-k needs no weights at all: the k-th largest of the threads' maxima is a lower bound of the k-th largest token.
 // Bound by the 64-bit pipe (ten operations per token that counts) and by the shared memory's atomics, not by HBM.
+#include <float.h>
 #include <limits.h>
 
 #include "accept.cuh"
@@ -31,7 +32,6 @@ constexpr int kBins = 2048;
 constexpr int kBinsPerOctave = 64;
 constexpr int kList = 1024;               // tokens that are sorted at most
 constexpr int kMaxTeam = 8;               // blocks per row
-constexpr float kLog2eF = 1.4426950408889634f;
 
 struct SampleSmem {
     union {
@@ -41,6 +41,7 @@ struct SampleSmem {
     double pow2[16];                      // 2^(i / 16)
     double wsum[kSampleWarps];            // per warp, of the block's latest sum
     double part[kSampleWarps];            // per warp: kept weight of its range of the row
+    double scan[3 * kSampleWarps];
     float wmax[kSampleWarps];
     unsigned int wcount[kSampleWarps];
     struct {
@@ -63,50 +64,50 @@ __device__ __forceinline__ float key_value(unsigned int k) {
     return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k);
 }
 
-// Weight of a logit.  exp(d / T) = 2^(t / 16) with t = 16 log2(e) d / T = 16 n + i + r, |r| <= 1/2: a table of
-// 2^(i / 16) (16 doubles: a gather without bank conflicts), the Taylor series of e^(r ln2 / 16) to the fifth power (the
-// next term is below 2e-13) and n into the exponent.  All in 64 bits.
+// In constant memory, where an instruction reads them as operands (as literals each would be put together in two
+// registers first, for every token anew).
+constexpr double kLn2By64 = 0.693147180559945309417 / 64.0;
+__constant__ double kSeries[6] = {1.0, kLn2By64, kLn2By64 *kLn2By64 / 2.0, kLn2By64 *kLn2By64 *kLn2By64 / 6.0,
+                                  kLn2By64 *kLn2By64 *kLn2By64 *kLn2By64 / 24.0,
+                                  kLn2By64 *kLn2By64 *kLn2By64 *kLn2By64 *kLn2By64 / 120.0};
+__constant__ double kMagicC = 6755399441055744.0 + (1 << 30);      // 1.5 * 2^52 + the bias below: adding it rounds to a whole number
+
+// Weight of a logit.  exp(d / T) = 2^(t / 64) with t = 64 log2(e) d / T.  k = t rounded is the token's bin (its distance
+// to the largest in 1/64 octaves); k rounded to fours, 64 n + 4 i, leaves |r| <= 5/2: a table of 2^(i / 16) (16 doubles:
+// a gather without bank conflicts), the Taylor series of e^(r ln2 / 64) to the fifth power (the next term is below
+// 6e-13) and n into the exponent.  All in 64 bits.
 struct Weights {
-    double m, c;                          // largest logit, 16 log2(e) / T
+    double m, c;                          // largest logit, 64 log2(e) / T
+    float m32, low, c32;                  // largest logit; logits below `low` lie in the last bin; log2(e) / T
     const double *pow2;
-    // w = q * s
-    __device__ __forceinline__ void factors(float x, double &q, double &s) const {
-        // The value in 64 bits by moving its fields (the conversion shares a slow unit): infinities become 2^128, and so
-        // their distance to themselves 0 and to everything else immense; zeros become 2^-127.
-        const unsigned int u = __float_as_uint(x);
-        const double v = __hiloint2double((int)((((int)u >> 3) & 0x8fffffffu) + 0x38000000u), (int)(u << 29));
-        const double d = v - m;
-        constexpr double kMagic = 6755399441055744.0;          // 1.5 * 2^52: adding it rounds to a whole number
-        const double kd = fma(d, c, kMagic);
-        const int k = __double2loint(kd);
-        const double r = fma(d, c, -(kd - kMagic));
-        constexpr double a = 0.693147180559945309417 / 16.0;   // ln 2 / 16
-        q = a * a * a * a * a / 120.0;
-        q = fma(q, r, a * a * a * a / 24.0);
-        q = fma(q, r, a * a * a / 6.0);
-        q = fma(q, r, a * a / 2.0);
-        q = fma(q, r, a);
-        q = fma(q, r, 1.0);
-        s = pow2[k & 15];
-        s = __hiloint2double(__double2hiint(s) + ((k >> 4) << 20), __double2loint(s));
-        if (!(d * c >= -16000.0)) { q = 0.0; s = 0.0; }
+    static constexpr unsigned int kBias = 1u << 30;                // keeps k's 32 bits away from a change of sign
+    // distance in bins of a logit that is not below `low`, and the two factors of its weight
+    __device__ __forceinline__ int split(float x, double &q, double &s) const {
+        const double d = (double)x - m;
+        const double kd = fma(d, c, kMagicC);
+        const unsigned int k = (unsigned int)__double2loint(kd), k4 = (k + 2u) & ~3u;
+        const double r = fma(d, c, kMagicC - __hiloint2double(__double2hiint(kd), (int)k4));
+        q = kSeries[5];
+#pragma unroll
+        for (int i = 4; i >= 0; --i) q = fma(q, r, kSeries[i]);
+        s = *reinterpret_cast<const double *>(reinterpret_cast<const char *>(pow2) + ((k4 << 1) & 0x78u));
+        // (the bias leaves no trace above bit 31)
+        s = __hiloint2double((int)((unsigned int)__double2hiint(s) + ((k4 & ~63u) << 14)), __double2loint(s));
+        return (int)(kBias - k);
     }
+    // any logit: zero below 2^-1000
     __device__ __forceinline__ double operator()(float x) const {
         double q, s;
-        factors(x, q, s);
-        return q * s;
+        split(x, q, s);
+        return ((double)x - m) * c >= -64000.0 ? q * s : 0.0;
     }
-    __device__ __forceinline__ void add_to(double &sum, float x) const {
-        double q, s;
-        factors(x, q, s);
-        sum = fma(q, s, sum);
+    // the weight of a logit below `low` (under 2^-31 of the largest): their sum is below 1e-4 of the whole, 32 bits are enough
+    __device__ __forceinline__ float small(float x) const {
+        float y;
+        asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"((x - m32) * c32));
+        return y;
     }
 };
-// The value `factors` sees x as.
-__device__ __forceinline__ double wide(float x) {
-    const unsigned int u = __float_as_uint(x);
-    return __hiloint2double((int)((((int)u >> 3) & 0x8fffffffu) + 0x38000000u), (int)(u << 29));
-}
 
 // A block's slice of a row: vectors [v_lo, v_hi) of 16 bytes, in shared memory at the phase they have in global memory
 // with -inf around the row (kStaged), or in global memory.  NaN reads as -inf; where the largest value is +inf
@@ -130,24 +131,47 @@ struct Row {
             for (int e = 0; e < VE; ++e) x[e] = (i0 + e >= 0 && i0 + e < V) ? to_float<T>(base[(size_t)v * VE + e]) : -INFINITY;
         }
 #pragma unroll
-        for (int e = 0; e < VE; ++e) {
-            if (!(x[e] == x[e])) x[e] = -INFINITY;
-            if (peak) x[e] = x[e] == INFINITY ? 0.f : -INFINITY;
-        }
+        for (int e = 0; e < VE; ++e) x[e] = clean(x[e]);
     }
     __device__ __forceinline__ int index(int v, int e) const { return v * VE - phase + e; }
     // the vectors of warp w: consecutive, so that sums per warp are sums over ranges of the index
     __device__ __forceinline__ int warp_first(int w) const { return v_lo + (int)((long long)(v_hi - v_lo) * w / kSampleWarps); }
-    // f(value, index) for this thread's elements
+    // f(value, index) for this thread's elements.  Two at a time: the loop's code, not its loads, is what has to be short.
     template <typename F>
     __device__ __forceinline__ void each(F f) const {
-        const int w = threadIdx.x >> 5, end = warp_first(w + 1);
-        for (int v = warp_first(w) + (threadIdx.x & 31); v < end; v += 32) {
-            float x[VE];
-            load(v, x);
-#pragma unroll
-            for (int e = 0; e < VE; ++e) f(x[e], index(v, e));
+        const int w = threadIdx.x >> 5, end = warp_first(w + 1) * (VE / 2);
+#pragma unroll 1
+        for (int j = warp_first(w) * (VE / 2) + (threadIdx.x & 31); j < end; j += 32) {
+            float x0, x1;
+            const int i = 2 * j - phase;
+            if (kStaged) {
+                pair(base + 2 * j - v_lo * VE, x0, x1);
+            } else {
+                x0 = i >= 0 && i < V ? clean(to_float<T>(base[2 * (size_t)j])) : -INFINITY;
+                x1 = i + 1 >= 0 && i + 1 < V ? clean(to_float<T>(base[2 * (size_t)j + 1])) : -INFINITY;
+            }
+            f(x0, i);
+            f(x1, i + 1);
         }
+    }
+    __device__ __forceinline__ float clean(float x) const {
+        if (!(x == x)) x = -INFINITY;
+        return peak ? (x == INFINITY ? 0.f : -INFINITY) : x;
+    }
+    static __device__ __forceinline__ void pair(const float *p, float &x0, float &x1) {
+        const float2 v = *reinterpret_cast<const float2 *>(p);
+        x0 = v.x;
+        x1 = v.y;
+    }
+    static __device__ __forceinline__ void pair(const __half *p, float &x0, float &x1) {
+        const float2 v = __half22float2(*reinterpret_cast<const __half2 *>(p));
+        x0 = v.x;
+        x1 = v.y;
+    }
+    static __device__ __forceinline__ void pair(const __nv_bfloat16 *p, float &x0, float &x1) {
+        const unsigned int u = *reinterpret_cast<const unsigned int *>(p);
+        x0 = __uint_as_float(u << 16);
+        x1 = __uint_as_float(u & 0xFFFF0000u);
     }
 };
 
@@ -207,6 +231,35 @@ __device__ __forceinline__ S block_scan(S v, S *warp_buf, S *total) {
     S excl = __shfl_up_sync(0xffffffffu, incl, 1);
     if (lane == 0) excl = 0;
     return before + excl;
+}
+
+// The same for two sums and a count at once.
+struct Sums {
+    double up, dn;
+    unsigned int c;
+};
+__device__ __forceinline__ Sums block_scan3(const Sums v, Sums *warp_buf, Sums *total) {
+    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+    Sums in = v;
+#pragma unroll
+    for (int off = 1; off < 32; off <<= 1) {
+        const double up = __shfl_up_sync(0xffffffffu, in.up, off), dn = __shfl_up_sync(0xffffffffu, in.dn, off);
+        const unsigned int c = __shfl_up_sync(0xffffffffu, in.c, off);
+        if (lane >= off) { in.up += up; in.dn += dn; in.c += c; }
+    }
+    __syncthreads();
+    if (lane == 31) warp_buf[w] = in;
+    __syncthreads();
+    Sums before{0.0, 0.0, 0u}, all{0.0, 0.0, 0u};
+#pragma unroll
+    for (int i = 0; i < kSampleWarps; ++i) {
+        if (i == w) before = all;
+        all.up += warp_buf[i].up; all.dn += warp_buf[i].dn; all.c += warp_buf[i].c;
+    }
+    *total = all;
+    Sums ex{__shfl_up_sync(0xffffffffu, in.up, 1), __shfl_up_sync(0xffffffffu, in.dn, 1), __shfl_up_sync(0xffffffffu, in.c, 1)};
+    if (lane == 0) ex = Sums{0.0, 0.0, 0u};
+    return Sums{before.up + ex.up, before.dn + ex.dn, before.c + ex.c};
 }
 
 // The blocks that share a row: a cluster (kTeam), or one block.  Values cross through `slot`, by turns, so that one
@@ -292,43 +345,46 @@ struct Team {
     }
 };
 
-// Ascending sort of list[0, n), n <= kList, by the whole block (bitonic network on the next power of two).
+// Ascending sort of list[0, n), n <= kList, by the whole block: a bitonic network on the next power of two, two
+// neighbouring entries per thread.  Entries up to 32 apart meet by shuffles, within a warp and without a barrier; farther
+// ones through shared memory (ten of the 55 steps for 1024 entries).
 __device__ __forceinline__ void sort_list(SampleSmem &sm, int n) {
+    static_assert(kList == 2 * kSampleThreads, "two entries per thread");
     int size = 2;
     while (size < n) size <<= 1;
+    const int i0 = 2 * threadIdx.x, lane = threadIdx.x & 31;
     __syncthreads();
-    for (int i = n + threadIdx.x; i < size; i += kSampleThreads) sm.list[i] = ~0ull;
-    __syncthreads();
-    if (size <= 32) {                                        // one warp, in registers
-        if (threadIdx.x < 32) {
-            unsigned long long v = (int)threadIdx.x < size ? sm.list[threadIdx.x] : ~0ull;
-#pragma unroll
-            for (int k = 2; k <= 32; k <<= 1)
-#pragma unroll
-                for (int j = k >> 1; j > 0; j >>= 1) {
-                    const unsigned long long o = __shfl_xor_sync(0xffffffffu, v, j);
-                    const bool up = ((threadIdx.x & k) == 0) == ((threadIdx.x & j) == 0);
-                    v = up ? ::min(v, o) : ::max(v, o);
-                }
-            if ((int)threadIdx.x < size) sm.list[threadIdx.x] = v;
-        }
-        __syncthreads();
-        return;
-    }
-    for (int k = 2; k <= size; k <<= 1)
-        for (int j = k >> 1; j > 0; j >>= 1) {
-            for (int t = threadIdx.x; t < size / 2; t += kSampleThreads) {
-                const int i = 2 * t - (t & (j - 1)), o = i + j;
-                const unsigned long long a = sm.list[i], b = sm.list[o];
-                if ((a > b) == ((i & k) == 0)) {
-                    sm.list[i] = b;
-                    sm.list[o] = a;
-                }
+    unsigned long long a = i0 < n ? sm.list[i0] : ~0ull, b = i0 + 1 < n ? sm.list[i0 + 1] : ~0ull;
+    const bool active = i0 - 2 * lane < size;               // whole warps
+    for (int k = 2; k <= size; k <<= 1) {
+        const bool up = (i0 & k) == 0;
+        for (int j = k >> 1; j >= 64; j >>= 1) {
+            __syncthreads();
+            if (active) { sm.list[i0] = a; sm.list[i0 + 1] = b; }
+            __syncthreads();
+            if (active) {
+                const unsigned long long oa = sm.list[i0 ^ j], ob = sm.list[(i0 + 1) ^ j];
+                const bool keep_small = ((i0 & j) == 0) == up;
+                a = keep_small ? ::min(a, oa) : ::max(a, oa);
+                b = keep_small ? ::min(b, ob) : ::max(b, ob);
             }
-            // distances up to 32 stay within the 64 entries of a warp's threads
-            if (j > 32 || (j == 1 && k >= 64)) __syncthreads();
-            else __syncwarp();
         }
+        if (active) {
+            for (int j = ::min(k >> 1, 32); j >= 2; j >>= 1) {
+                const unsigned long long oa = __shfl_xor_sync(0xffffffffu, a, j >> 1), ob = __shfl_xor_sync(0xffffffffu, b, j >> 1);
+                const bool keep_small = ((i0 & j) == 0) == up;
+                a = keep_small ? ::min(a, oa) : ::max(a, oa);
+                b = keep_small ? ::min(b, ob) : ::max(b, ob);
+            }
+            if ((a > b) == up) {
+                const unsigned long long o = a;
+                a = b;
+                b = o;
+            }
+        }
+    }
+    __syncthreads();
+    if (active) { sm.list[i0] = a; sm.list[i0 + 1] = b; }
     __syncthreads();
 }
 // A token as a list entry that sorts in the order: larger key first, lower index among equals.
@@ -412,11 +468,7 @@ struct Sampler {
     Team<kTeam> &team;
     Row<T, kStaged> row;
     Weights wt;
-    float m, cf;                          // largest logit; bins per unit of logit
-
-    // Distance to the largest in bins, and the bin (nearest whole number; the last bin takes all from there on).
-    __device__ __forceinline__ float depth(float x) const { return fminf((m - x) * cf, (float)(kBins - 1)); }
-    __device__ __forceinline__ int bin_of(float depth) const { return (int)(__float_as_uint(depth + 8388608.f) & 0x7ffu); }
+    float m;                              // largest logit
 
     // Elements ahead of the cut of a running count (count_goal > 0) or weight (goal), by halving the range of the keys and
     // then of the indexes: exact for every distribution, one pass over the row per step.  For rows whose zone does not
@@ -482,17 +534,23 @@ struct Sampler {
         return *team.of(&sm.n_list, 0);
     }
 
-    // Gathers the kept elements of bins [lo, hi] into the first block's list.  kAbove: *above receives the weight of the kept
-    // elements of lower bins; sm.part the warps' shares of it.
+    // Gathers the kept elements of bins [lo, hi], hi < kBins - 1, into the first block's list.  kAbove: *above receives the
+    // weight of the kept elements of lower bins; sm.part the warps' shares of it.
     template <bool kAbove>
     __device__ __forceinline__ int gather(const Cut &in, int lo, int hi, double *above) {
         open_list();
         double w = 0.0;
+        const float bottom = fmaxf(wt.low, in.x);
         row.each([&](float x, int i) {
-            const int b = bin_of(depth(x));
-            if (b <= hi && in.keeps(x, i)) {
-                if (b >= lo) append(x, i);
-                else if (kAbove) wt.add_to(w, x);
+            if (x >= bottom) {
+                if (x == in.x && i >= in.index) return;
+                double q, s;
+                const int b = wt.split(x, q, s);
+                if (b < lo) {
+                    if (kAbove) w = fma(q, s, w);
+                } else if (b <= hi) {
+                    append(x, i);
+                }
             }
         });
         if (kAbove) {
@@ -504,36 +562,42 @@ struct Sampler {
 
     // Counts of the kept elements by bin, summed over the row's blocks in the first one, and (kWeight) their weight.
     // The histogram shares its memory with the list: a barrier of the row lies between the uses.
-    template <bool kWeight>
+    // kAll: nothing is cut off yet.
+    template <bool kWeight, bool kAll>
     __device__ __forceinline__ double histogram(const Cut &in) {
         __syncthreads();
         for (int i = threadIdx.x; i < kBins; i += kSampleThreads) sm.hist[i] = 0u;
         __syncthreads();
         double w = 0.0;
-        float w_low = 0.f;                                   // below 2^-32 of the largest: 32 bits are enough
+        float w_low = 0.f;
         unsigned int low = 0;                                // the last bin may hold most of the row: counted in registers
+        const float top = kAll ? wt.low : fmaxf(wt.low, in.x);
+        const bool deep = kAll || in.x < wt.low;             // are any elements of the last bin kept?
         row.each([&](float x, int i) {
-            if (in.keeps(x, i)) {
-                const int b = bin_of(depth(x));
-                if (b < kBins - 1) {
-                    atomicAdd(&sm.hist[b], 1u);
-                    if (kWeight) wt.add_to(w, x);
-                } else {
-                    ++low;
-                    if (kWeight) w_low += exp2f((x - m) * (cf * (1.f / kBinsPerOctave)));
-                }
+            if (x >= top) {
+                if (!kAll && x == in.x && i >= in.index) return;
+                double q, s;
+                const int b = wt.split(x, q, s);
+                atomicAdd(&sm.hist[::min(b, kBins - 1)], 1u);
+                if (kWeight) w = fma(q, s, w);
+            } else if (deep && (kAll || in.keeps(x, i))) {
+                low += kWeight || x > -INFINITY;             // (with weights the last bin's count only bounds: -inf may be in it)
+                if (kWeight) w_low += wt.small(x);
             }
         });
-        low = block_count(sm, low);
-        if (threadIdx.x == 0) sm.hist[kBins - 1] = low;
+        low = __reduce_add_sync(0xffffffffu, low);
+        if ((threadIdx.x & 31) == 0) atomicAdd(&sm.hist[kBins - 1], low);
         double sum = 0.0;
         if (kWeight) sum = team.sum(block_sum(sm, w + (double)w_low));
         else team.barrier();
         if (kTeam && team.rank == 0) {
             for (int i = threadIdx.x; i < kBins; i += kSampleThreads) {
-                unsigned int c = sm.hist[i];
-                for (int r = 1; r < team.size; ++r) c += *team.of(&sm.hist[i], r);
-                sm.hist[i] = c;
+                unsigned int c[kMaxTeam], all = sm.hist[i];
+#pragma unroll
+                for (int r = 1; r < kMaxTeam; ++r) c[r] = r < team.size ? *team.of(&sm.hist[i], r) : 0u;
+#pragma unroll
+                for (int r = 1; r < kMaxTeam; ++r) all += c[r];
+                sm.hist[i] = all;
             }
         }
         return sum;
@@ -573,8 +637,9 @@ struct Sampler {
         constexpr int PER = kBins / kSampleThreads;
         __syncthreads();
         if (!kTeam || team.rank == 0) {
-            unsigned int c[PER], mine_c = 0, all_c;
-            double up[PER], dn[PER], mine_up = 0.0, mine_dn = 0.0, all_up, all_dn;
+            unsigned int c[PER];
+            double up[PER], dn[PER];
+            Sums mine{0.0, 0.0, 0u}, all;
 #pragma unroll
             for (int u = 0; u < PER; ++u) {
                 const int b = threadIdx.x * PER + u;
@@ -582,30 +647,34 @@ struct Sampler {
                 const float edge = exp2f((0.5f - (float)b) / kBinsPerOctave);
                 up[u] = c[u] * ((double)edge * 1.00001);
                 dn[u] = b == kBins - 1 ? 0.0 : c[u] * ((double)edge * (0.98922 * 0.99999));   // 2^(-1/64) = 0.989228...
-                mine_c += c[u];
-                mine_up += up[u];
-                mine_dn += dn[u];
+                mine.c += c[u];
+                mine.up += up[u];
+                mine.dn += dn[u];
             }
-            unsigned int before_c = block_scan(mine_c, sm.wcount, &all_c);
-            double sum_up = block_scan(mine_up, sm.wsum, &all_up);
-            double sum_dn = block_scan(mine_dn, sm.wsum, &all_dn);
-            if (threadIdx.x == 0) { sm.zone_lo = kBins - 1; sm.zone_hi = kBins - 1; sm.total = all_c; }
+            Sums run = block_scan3(mine, reinterpret_cast<Sums *>(sm.scan), &all);
+            if (threadIdx.x == 0) { sm.zone_lo = kBins - 1; sm.zone_hi = kBins - 1; sm.total = all.c; }
             __syncthreads();
+            int lo = INT_MAX, hi = INT_MAX;                  // this thread's first bins that reach the goal
+            unsigned int run_c[PER];
 #pragma unroll
             for (int u = 0; u < PER; ++u) {
                 const int b = threadIdx.x * PER + u;
-                sum_up += up[u];
-                sum_dn += dn[u];
-                if (fmin(sum_up, total - (all_dn - sum_dn)) >= goal) atomicMin(&sm.zone_lo, b);
-                if (fmax(sum_dn, total - (all_up - sum_up)) >= goal) atomicMin(&sm.zone_hi, b);
+                run.up += up[u];
+                run.dn += dn[u];
+                run_c[u] = run.c += c[u];
+                if (fmin(run.up, total - (all.dn - run.dn)) >= goal) lo = ::min(lo, b);
+                if (fmax(run.dn, total - (all.up - run.up)) >= goal) hi = ::min(hi, b);
+            }
+            lo = __reduce_min_sync(0xffffffffu, lo);
+            hi = __reduce_min_sync(0xffffffffu, hi);
+            if ((threadIdx.x & 31) == 0) {
+                atomicMin(&sm.zone_lo, lo);
+                atomicMin(&sm.zone_hi, hi);
             }
             __syncthreads();
-            const int hi = sm.zone_hi;
 #pragma unroll
-            for (int u = 0; u < PER; ++u) {
-                before_c += c[u];
-                if (threadIdx.x * PER + u == hi) sm.total = before_c;
-            }
+            for (int u = 0; u < PER; ++u)
+                if ((int)threadIdx.x * PER + u == sm.zone_hi) sm.total = run_c[u];
         }
         team.barrier();
     }
@@ -621,14 +690,19 @@ struct Sampler {
     __device__ __forceinline__ void sum_kept(const Cut &cut, double floor, bool exact) {
         double mine = 0.0;
         float low = 0.f;
-        const float none = (float)(kBins - 1) - 0.5f;
         if (floor > 0.0 || exact) {
             row.each([&](float x, int i) { mine += kept_weight(cut, floor, x, i); });
         } else {
+            const float top = fmaxf(wt.low, cut.x);
+            const bool deep = cut.x < wt.low;
             row.each([&](float x, int i) {
-                if (cut.keeps(x, i)) {
-                    if (depth(x) < none) wt.add_to(mine, x);
-                    else low += exp2f((x - m) * (cf * (1.f / kBinsPerOctave)));
+                if (x >= top) {
+                    if (x == cut.x && i >= cut.index) return;
+                    double q, s;
+                    wt.split(x, q, s);
+                    mine = fma(q, s, mine);
+                } else if (deep && cut.keeps(x, i)) {
+                    low += wt.small(x);
                 }
             });
         }
@@ -705,6 +779,46 @@ struct Sampler {
         return sm.answer;
     }
 
+    // The k-th largest of the block's thread maxima, rounded down to the upper sixteen bits of its key: two steps of a
+    // radix selection with 256 counts each.
+    __device__ __forceinline__ unsigned int kth_maximum(float thread_max, int k) {
+        const unsigned int mine = order_key(thread_max);
+        unsigned int prefix = 0;
+#pragma unroll
+        for (int step = 0; step < 2; ++step) {
+            const int shift = 24 - 8 * step;
+            __syncthreads();
+            if (threadIdx.x < 256) sm.hist[threadIdx.x] = 0u;
+            __syncthreads();
+            if (step == 0 || mine >> 24 == prefix) atomicAdd(&sm.hist[(mine >> shift) & 255u], 1u);
+            __syncthreads();
+            if (threadIdx.x < 32) {                          // lane l: counts 255 - 8 l and the seven below
+                unsigned int c[8], sum = 0, before;
+#pragma unroll
+                for (int u = 0; u < 8; ++u) sum += c[u] = sm.hist[255 - 8 * threadIdx.x - u];
+                before = sum;
+#pragma unroll
+                for (int off = 1; off < 32; off <<= 1) {
+                    const unsigned int o = __shfl_up_sync(0xffffffffu, before, off);
+                    if ((int)threadIdx.x >= off) before += o;
+                }
+                before -= sum;
+#pragma unroll
+                for (int u = 0; u < 8; ++u) {
+                    if ((int)before < k && (int)(before + c[u]) >= k) {
+                        sm.zone_lo = 255 - 8 * (int)threadIdx.x - u;
+                        sm.n_above = (int)before;
+                    }
+                    before += c[u];
+                }
+            }
+            __syncthreads();
+            prefix = step == 0 ? (unsigned int)sm.zone_lo : (prefix << 8) | (unsigned int)sm.zone_lo;
+            k -= sm.n_above;
+        }
+        return prefix << 16;
+    }
+
     // The cut that the first block found, told to all.
     __device__ __forceinline__ Cut share(const Cut &cut) {
         if (threadIdx.x == 0 && team.rank == 0) { sm.cut_x = cut.x; sm.cut_i = cut.index; }
@@ -715,25 +829,17 @@ struct Sampler {
     __device__ __forceinline__ int sample(float thread_max, int top_k, float top_p, float min_p, float uniform) {
         const double u = (double)uniform, floor = min_p > 0.f ? (double)min_p : 0.0;
         const bool first = !kTeam || team.rank == 0;
-        Cut cut{-INFINITY, 0};                                // keeps everything above -inf
+        Cut cut{-INFINITY, INT_MIN};                          // keeps everything above -inf (padding has indexes below 0)
         const bool p_on = top_p < 1.f;
         if (top_k > 0 && top_k < row.V) {
             if (top_k <= kSampleThreads) {
                 // Lower bounds of the k-th largest token: the k-th largest of a block's thread maxima, and the smallest of
                 // the blocks' ceil(k / blocks)-th largest.
-                const unsigned int mine = order_key(thread_max);
-                auto kth = [&](int k) {
-                    unsigned int key = 0;
-                    for (int bit = 31; bit >= (sizeof(T) == 2 ? 13 : 0); --bit) {    // (a 16-bit value has no lower bits: fp16 reaches bit 13)
-                        const unsigned int cand = key | (1u << bit);
-                        if (__syncthreads_count(mine >= cand) >= k) key = cand;
-                    }
-                    return key;
-                };
-                unsigned int key = team.max_key(kth(top_k));
-                if (kTeam) key = ::max(key, team.min_key(kth((top_k + team.size - 1) / team.size)));
+                unsigned int key = team.max_key(kth_maximum(thread_max, top_k));
+                if (kTeam) key = ::max(key, team.min_key(kth_maximum(thread_max, (top_k + team.size - 1) / team.size)));
+                const float bound = key <= order_key(-INFINITY) ? -INFINITY : key_value(key);
                 open_list();
-                row.each([&](float x, int i) { if (x > -INFINITY && order_key(x) >= key) append(x, i); });
+                row.each([&](float x, int i) { if (x >= bound && x > -INFINITY) append(x, i); });
                 int n = close_list();
                 if (n <= kList) {
                     if (!first) return kElsewhere;
@@ -743,14 +849,14 @@ struct Sampler {
                 }
                 team.barrier();                               // (the first block's list is done with)
             }
-            histogram<false>(cut);
+            histogram<false, true>(cut);
             find_count((unsigned int)top_k);
             const int zone = *team.of(&sm.zone_lo, 0), above = *team.of(&sm.n_above, 0);
             if (zone >= 0) {                                  // at least k tokens above -inf
                 bool done = false;
                 if (zone < kBins - 1) {
                     const int n = gather<false>(cut, zone, zone, nullptr);
-                    if (n <= kList) {
+                    if (n >= 1 && n <= kList) {
                         Cut c = cut;
                         if (first) {
                             sort_list(sm, n);
@@ -767,10 +873,10 @@ struct Sampler {
             team.barrier();
         }
         if (p_on) {
-            const double Z = histogram<true>(cut);
+            const double Z = cut.x == -INFINITY ? histogram<true, true>(cut) : histogram<true, false>(cut);
             const double goal = (double)top_p * Z;
             find_weight(goal, Z);
-            const int lo = *team.of(&sm.zone_lo, 0), hi = *team.of(&sm.zone_hi, 0);
+            const int hi = *team.of(&sm.zone_hi, 0), lo = ::min(*team.of(&sm.zone_lo, 0), hi);
             const unsigned int upto = *team.of(&sm.total, 0);
             if (hi < kBins - 1 && upto <= kList) {            // the whole kept set fits the list
                 const int n = gather<false>(cut, 0, hi, nullptr);
@@ -782,7 +888,7 @@ struct Sampler {
             if (hi < kBins - 1) {
                 double above;
                 const int n = gather<true>(cut, lo, hi, &above);
-                if (n <= kList) {
+                if (n >= 1 && n <= kList) {
                     Cut c = cut;
                     if (first) {
                         sort_list(sm, n);
@@ -968,8 +1074,12 @@ sample_kernel(const SampleArgs a) {
                 mx = mx == INFINITY ? 0.f : -INFINITY;
                 __syncthreads();
             }
-            const float cf = fminf(kBinsPerOctave * kLog2eF / Tm, 1e30f);
-            Sampler<T, kStaged, kTeam> s{sm, team, row, Weights{wide(m), 16.0 * 1.4426950408889634074 / (double)Tm, sm.pow2}, m, cf};
+            const double log2e = 1.4426950408889634074;
+            // (`low` may lie a little inside the last bin or the one before: what is not below it is told by its bin)
+            const float low = (float)((double)m - (double)(kBins - 1) / kBinsPerOctave / log2e * (double)Tm);
+            Sampler<T, kStaged, kTeam> s{sm, team, row,
+                                         Weights{(double)m, kBinsPerOctave * log2e / (double)Tm, m, fmaxf(low, -FLT_MAX),
+                                                 (float)fmin(log2e / (double)Tm, 1e30), sm.pow2}, m};
             token = s.sample(mx, top_k, top_p, min_p, a.uniform[(size_t)b * a.N + r]);
         }
     }

@@ -31,6 +31,7 @@ constexpr int kSampleWarps = kSampleThreads / 32;
 constexpr int kBins = 2048;
 constexpr int kBinsPerOctave = 64;
 constexpr int kList = 1024;               // tokens that are sorted at most
+constexpr unsigned int kShort = 128;      // kept sets up to this are sorted whole instead of cut in their zone and walked
 constexpr int kMaxTeam = 8;               // blocks per row
 
 struct SampleSmem {
@@ -95,6 +96,8 @@ struct Weights {
         s = __hiloint2double((int)((unsigned int)__double2hiint(s) + ((k4 & ~63u) << 14)), __double2loint(s));
         return (int)(kBias - k);
     }
+    // the distance in bins as such
+    __device__ __forceinline__ double depth(float x) const { return (m - (double)x) * c; }
     // any logit: zero below 2^-1000
     __device__ __forceinline__ double operator()(float x) const {
         double q, s;
@@ -458,8 +461,9 @@ __device__ __forceinline__ int list_draw(SampleSmem &sm, const Weights &wt, int 
     return (int)(unsigned int)(sm.list[at] >> 32);
 }
 
-// What a block answers: a token, or that another block of the row has it.
-constexpr int kElsewhere = -2;
+// What a block answers: a token, that another block of the row has it, or that besides nothing of this block's shared memory
+// is read any more.
+constexpr int kElsewhere = -2, kGone = -3;
 
 template <typename T, bool kStaged, bool kTeam>
 struct Sampler {
@@ -534,11 +538,29 @@ struct Sampler {
         return *team.of(&sm.n_list, 0);
     }
 
-    // Gathers the kept elements of bins [lo, hi], hi < kBins - 1, into the first block's list.  kAbove: *above receives the
-    // weight of the kept elements of lower bins; sm.part the warps' shares of it.
-    template <bool kAbove>
-    __device__ __forceinline__ int gather(const Cut &in, int lo, int hi, double *above) {
-        open_list();
+    // A part of the order where the cut must lie: bins [lo, hi], hi < kBins - 1, and where those hold more than the list
+    // takes, steps [fine_lo, fine_hi] of them: kBins even steps from bin lo to bin hi.
+    struct Zone {
+        int lo, hi, fine_lo, fine_hi;
+        __device__ __forceinline__ double start() const { return lo - 0.5; }
+        __device__ __forceinline__ double step() const { return (hi - lo + 1) * (1.0 / kBins); }
+    };
+    __device__ __forceinline__ int fine_step(const Zone &z, float x) const {
+        const int f = (int)((wt.depth(x) - z.start()) * ((double)kBins / (z.hi - z.lo + 1)));
+        return ::min(::max(f, 0), kBins - 1);
+    }
+
+    // Gathers the kept elements of the zone into the first block's list (kCount: counts them by their steps instead).
+    // kAbove: *above receives the weight of the kept elements ahead of the zone; sm.part the warps' shares of it.
+    template <bool kAbove, bool kFine, bool kCount>
+    __device__ __forceinline__ int gather(const Cut &in, const Zone z, double *above) {
+        if (kCount) {
+            __syncthreads();
+            for (int i = threadIdx.x; i < kBins; i += kSampleThreads) sm.hist[i] = 0u;
+            __syncthreads();
+        } else {
+            open_list();
+        }
         double w = 0.0;
         const float bottom = fmaxf(wt.low, in.x);
         row.each([&](float x, int i) {
@@ -546,18 +568,44 @@ struct Sampler {
                 if (x == in.x && i >= in.index) return;
                 double q, s;
                 const int b = wt.split(x, q, s);
-                if (b < lo) {
-                    if (kAbove) w = fma(q, s, w);
-                } else if (b <= hi) {
-                    append(x, i);
+                if (b > z.hi) return;
+                bool ahead = b < z.lo;
+                if (!ahead) {
+                    if (kCount) {
+                        atomicAdd(&sm.hist[fine_step(z, x)], 1u);
+                        return;
+                    }
+                    const int f = kFine ? fine_step(z, x) : 0;
+                    ahead = kFine && f < z.fine_lo;
+                    if (!ahead && (!kFine || f <= z.fine_hi)) append(x, i);
                 }
+                if (kAbove && ahead) w = fma(q, s, w);
             }
         });
         if (kAbove) {
             *above = team.sum(block_sum(sm, w));
             if (threadIdx.x < kSampleWarps) sm.part[threadIdx.x] = sm.wsum[threadIdx.x];
         }
+        if (kCount) {
+            if (!kAbove) team.barrier();
+            merge_counts();
+            return 0;
+        }
         return close_list();
+    }
+
+    // The blocks' counts summed in the first one's (a barrier of the row lies behind the counting).
+    __device__ __forceinline__ void merge_counts() {
+        if (kTeam && team.rank == 0) {
+            for (int i = threadIdx.x; i < kBins; i += kSampleThreads) {
+                unsigned int c[kMaxTeam], all = sm.hist[i];
+#pragma unroll
+                for (int r = 1; r < kMaxTeam; ++r) c[r] = r < team.size ? *team.of(&sm.hist[i], r) : 0u;
+#pragma unroll
+                for (int r = 1; r < kMaxTeam; ++r) all += c[r];
+                sm.hist[i] = all;
+            }
+        }
     }
 
     // Counts of the kept elements by bin, summed over the row's blocks in the first one, and (kWeight) their weight.
@@ -590,20 +638,12 @@ struct Sampler {
         double sum = 0.0;
         if (kWeight) sum = team.sum(block_sum(sm, w + (double)w_low));
         else team.barrier();
-        if (kTeam && team.rank == 0) {
-            for (int i = threadIdx.x; i < kBins; i += kSampleThreads) {
-                unsigned int c[kMaxTeam], all = sm.hist[i];
-#pragma unroll
-                for (int r = 1; r < kMaxTeam; ++r) c[r] = r < team.size ? *team.of(&sm.hist[i], r) : 0u;
-#pragma unroll
-                for (int r = 1; r < kMaxTeam; ++r) all += c[r];
-                sm.hist[i] = all;
-            }
-        }
+        merge_counts();
         return sum;
     }
 
-    // First bin at which the running count reaches `goal` (sm.zone_lo = -1: none does), and the count before it (sm.n_above).
+    // First bin at which the running count reaches `goal` (sm.zone_lo = -1: none does), the count before it
+    // (sm.n_above) and in it (sm.total).
     __device__ __forceinline__ void find_count(unsigned int goal) {
         constexpr int PER = kBins / kSampleThreads;
         __syncthreads();
@@ -619,6 +659,7 @@ struct Sampler {
                 if (before < goal && before + c[u] >= goal) {
                     sm.zone_lo = threadIdx.x * PER + u;
                     sm.n_above = (int)before;
+                    sm.total = c[u];
                 }
                 before += c[u];
             }
@@ -630,10 +671,12 @@ struct Sampler {
     // at the bin's upper or lower end, running sums `up` and `dn` enclose the running weight M_b at the end of bin b from
     // the front, and what is left behind it encloses it from the back (a cut close to the end has little behind it):
     //     max(dn_b, total - (up_all - up_b)) <= M_b <= min(up_b, total - (dn_all - dn_b)).
+    // kFine: the same for the steps of a zone, from the front alone, `total` being the weight ahead of the zone.
     // sm.zone_lo: the first bin where the upper bound reaches the goal, sm.zone_hi: the first where the lower one does,
-    // sm.total: elements up to zone_hi.  Bins are formed in 32 bits: 1e-5 relative covers what their edges move by; the
-    // last bin has no lower end.
-    __device__ __forceinline__ void find_weight(double goal, double total) {
+    // sm.total: elements up to zone_hi, sm.n_above: before zone_lo.  Bins' edges are formed in 32 bits: 1e-5 relative covers that; the last bin has no
+    // lower end.
+    template <bool kFine>
+    __device__ __forceinline__ void find_weight(double goal, double total, const Zone z) {
         constexpr int PER = kBins / kSampleThreads;
         __syncthreads();
         if (!kTeam || team.rank == 0) {
@@ -644,15 +687,20 @@ struct Sampler {
             for (int u = 0; u < PER; ++u) {
                 const int b = threadIdx.x * PER + u;
                 c[u] = sm.hist[b];
-                const float edge = exp2f((0.5f - (float)b) / kBinsPerOctave);
-                up[u] = c[u] * ((double)edge * 1.00001);
-                dn[u] = b == kBins - 1 ? 0.0 : c[u] * ((double)edge * (0.98922 * 0.99999));   // 2^(-1/64) = 0.989228...
+                if (kFine) {
+                    up[u] = c[u] * (exp2(-(z.start() + b * z.step()) / kBinsPerOctave) * (1.0 + 1e-9));
+                    dn[u] = c[u] * (exp2(-(z.start() + (b + 1) * z.step()) / kBinsPerOctave) * (1.0 - 1e-9));
+                } else {
+                    const float edge = exp2f((0.5f - (float)b) / kBinsPerOctave);
+                    up[u] = c[u] * ((double)edge * 1.00001);
+                    dn[u] = b == kBins - 1 ? 0.0 : c[u] * ((double)edge * (0.98922 * 0.99999));   // 2^(-1/64) = 0.989228...
+                }
                 mine.c += c[u];
                 mine.up += up[u];
                 mine.dn += dn[u];
             }
             Sums run = block_scan3(mine, reinterpret_cast<Sums *>(sm.scan), &all);
-            if (threadIdx.x == 0) { sm.zone_lo = kBins - 1; sm.zone_hi = kBins - 1; sm.total = all.c; }
+            if (threadIdx.x == 0) { sm.zone_lo = kBins - 1; sm.zone_hi = kBins - 1; sm.total = all.c; sm.n_above = 0; }
             __syncthreads();
             int lo = INT_MAX, hi = INT_MAX;                  // this thread's first bins that reach the goal
             unsigned int run_c[PER];
@@ -662,8 +710,8 @@ struct Sampler {
                 run.up += up[u];
                 run.dn += dn[u];
                 run_c[u] = run.c += c[u];
-                if (fmin(run.up, total - (all.dn - run.dn)) >= goal) lo = ::min(lo, b);
-                if (fmax(run.dn, total - (all.up - run.up)) >= goal) hi = ::min(hi, b);
+                if ((kFine ? total + run.up : fmin(run.up, total - (all.dn - run.dn))) >= goal) lo = ::min(lo, b);
+                if ((kFine ? total + run.dn : fmax(run.dn, total - (all.up - run.up))) >= goal) hi = ::min(hi, b);
             }
             lo = __reduce_min_sync(0xffffffffu, lo);
             hi = __reduce_min_sync(0xffffffffu, hi);
@@ -673,8 +721,10 @@ struct Sampler {
             }
             __syncthreads();
 #pragma unroll
-            for (int u = 0; u < PER; ++u)
+            for (int u = 0; u < PER; ++u) {
                 if ((int)threadIdx.x * PER + u == sm.zone_hi) sm.total = run_c[u];
+                if ((int)threadIdx.x * PER + u == sm.zone_lo) sm.n_above = (int)(run_c[u] - c[u]);
+            }
         }
         team.barrier();
     }
@@ -842,7 +892,7 @@ struct Sampler {
                 row.each([&](float x, int i) { if (x >= bound && x > -INFINITY) append(x, i); });
                 int n = close_list();
                 if (n <= kList) {
-                    if (!first) return kElsewhere;
+                    if (!first) return kGone;
                     sort_list(sm, n);
                     n = ::min(n, top_k);
                     return finish_list(n, p_on, top_p, -1.0, floor, u);
@@ -852,17 +902,28 @@ struct Sampler {
             histogram<false, true>(cut);
             find_count((unsigned int)top_k);
             const int zone = *team.of(&sm.zone_lo, 0), above = *team.of(&sm.n_above, 0);
+            const unsigned int inside = *team.of(&sm.total, 0);
             if (zone >= 0) {                                  // at least k tokens above -inf
                 bool done = false;
                 if (zone < kBins - 1) {
-                    const int n = gather<false>(cut, zone, zone, nullptr);
+                    Zone z{zone, zone, 0, kBins - 1};
+                    int ahead = above, n;
+                    if (inside <= kList) {
+                        n = gather<false, false, false>(cut, z, nullptr);
+                    } else {                                  // step by step
+                        gather<false, false, true>(cut, z, nullptr);
+                        find_count((unsigned int)(top_k - above));
+                        z.fine_lo = z.fine_hi = ::max(*team.of(&sm.zone_lo, 0), 0);
+                        ahead += *team.of(&sm.n_above, 0);
+                        n = gather<false, true, false>(cut, z, nullptr);
+                    }
                     if (n >= 1 && n <= kList) {
                         Cut c = cut;
                         if (first) {
                             sort_list(sm, n);
-                            const bool inside = top_k - above < n;
-                            const unsigned long long e = sm.list[inside ? top_k - above : n - 1];
-                            c = Cut{entry_value(e), inside ? entry_index(e) : INT_MAX};
+                            const bool within = top_k - ahead < n;
+                            const unsigned long long e = sm.list[within ? top_k - ahead : n - 1];
+                            c = Cut{entry_value(e), within ? entry_index(e) : INT_MAX};
                         }
                         cut = share(c);
                         done = true;
@@ -875,19 +936,31 @@ struct Sampler {
         if (p_on) {
             const double Z = cut.x == -INFINITY ? histogram<true, true>(cut) : histogram<true, false>(cut);
             const double goal = (double)top_p * Z;
-            find_weight(goal, Z);
-            const int hi = *team.of(&sm.zone_hi, 0), lo = ::min(*team.of(&sm.zone_lo, 0), hi);
-            const unsigned int upto = *team.of(&sm.total, 0);
-            if (hi < kBins - 1 && upto <= kList) {            // the whole kept set fits the list
-                const int n = gather<false>(cut, 0, hi, nullptr);
-                if (!first) return kElsewhere;
+            Zone z{0, 0, 0, kBins - 1};
+            find_weight<false>(goal, Z, z);
+            z.hi = *team.of(&sm.zone_hi, 0);
+            z.lo = ::min(*team.of(&sm.zone_lo, 0), z.hi);
+            const unsigned int upto = *team.of(&sm.total, 0), before = (unsigned int)*team.of(&sm.n_above, 0);
+            bool done = false;
+            if (z.hi < kBins - 1 && upto <= kShort) {         // a short kept set: all of it in the list
+                z.lo = 0;
+                const int n = gather<false, false, false>(cut, z, nullptr);
+                if (!first) return kGone;
                 sort_list(sm, n);
                 return finish_list(n, true, top_p, Z, floor, u);
             }
-            bool done = false;
-            if (hi < kBins - 1) {
+            if (z.hi < kBins - 1) {
                 double above;
-                const int n = gather<true>(cut, lo, hi, &above);
+                int n;
+                if (upto - before <= kList) {
+                    n = gather<true, false, false>(cut, z, &above);
+                } else {                                      // step by step
+                    gather<true, false, true>(cut, z, &above);
+                    find_weight<true>(goal, above, z);
+                    z.fine_hi = *team.of(&sm.zone_hi, 0);
+                    z.fine_lo = ::min(*team.of(&sm.zone_lo, 0), z.fine_hi);
+                    n = gather<true, true, false>(cut, z, &above);
+                }
                 if (n >= 1 && n <= kList) {
                     Cut c = cut;
                     if (first) {
@@ -898,7 +971,7 @@ struct Sampler {
                     }
                     const Cut p_cut = share(c);
                     if (floor == 0.0 && u > 0.0) {
-                        // the warps' kept weights: what lies above the zone, and their tokens of the list
+                        // the warps' kept weights: what lies ahead of the zone, and their tokens of the list
                         add_list(n, p_cut);
                         return locate(p_cut, 0.0, u);
                     }
@@ -1083,9 +1156,10 @@ sample_kernel(const SampleArgs a) {
             token = s.sample(mx, top_k, top_p, min_p, a.uniform[(size_t)b * a.N + r]);
         }
     }
-    // A block leaves its shared memory behind only when no other block of the row may still read it.
-    if (kTeam) team.barrier();
-    if (bad ? team.rank != 0 : token == kElsewhere) return;
+    // A block leaves only when no other block of the row may still read its shared memory (the barrier does not wait for
+    // blocks that have left).
+    if (kTeam && token != kGone) team.barrier();
+    if (bad ? team.rank != 0 : token <= kElsewhere) return;
     if (!kVerify) {
         if (threadIdx.x == 0) {
             a.token[(size_t)b * a.N + r] = token;

@@ -144,8 +144,16 @@ def _check(rc: int):
         raise HtError(rc, load().ht_last_error_string().decode())
 
 
+try:                                       # the same number without the stream object around it (3 us of a call's 20)
+    from torch._C import _cuda_getCurrentRawStream as _raw_stream
+except ImportError:
+    _raw_stream = None
+
+
 def _stream() -> int:
-    return torch.cuda.current_stream().cuda_stream
+    if _raw_stream is None:
+        return torch.cuda.current_stream().cuda_stream
+    return _raw_stream(torch.cuda.current_device())
 
 
 def _ptr(t: Optional[torch.Tensor]):
@@ -484,66 +492,80 @@ def make_head_desc(D: int, norm: int = HT_HEAD_NORM_Q | HT_HEAD_NORM_K, eps: flo
                     high, orig_len, magnitude, 0, 0, 0)
 
 
-def _one_device(first: torch.Tensor, *others) -> None:
-    """All tensors on the current device, whose stream the work goes to."""
-    dev = first.device
-    for t in others:
-        if t is not None and t.device != dev:
-            raise ValueError("tensors on different devices")
-    if dev.index != torch.cuda.current_device():
-        raise ValueError("the tensors' device is not the current one")
+def _device_of(t: torch.Tensor, name: str) -> int:
+    """The index of t's device, which must be the current one: the work goes to its current stream."""
+    dev = t.get_device()
+    if dev < 0:
+        raise ValueError("%s must be a CUDA tensor (this library has no CPU path)" % name)
+    if dev != torch.cuda.current_device():
+        raise ValueError("%s lives on device %d, which is not the current one" % (name, dev))
+    return dev
 
 
-def _row_stride(t: torch.Tensor, name: str) -> int:
-    """Elements between the rows of t [B, N, H, D], whose heads must be dense and whose rows evenly spaced."""
-    B, N, H, D = t.shape
-    sb, sn, sh, sd = t.stride()
+def _dense(t: torch.Tensor, dev: int, dtype, shape, name: str):
+    """t must be a contiguous tensor of this device, dtype and shape."""
+    if t.get_device() != dev or t.dtype != dtype or t.shape != shape or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous CUDA tensor of device %d, %s, shape %s; it is %s on %s, shape %s%s" % (
+            name, dev, dtype, tuple(shape), t.dtype, t.device, tuple(t.shape), "" if t.is_contiguous() else ", strided"))
+
+
+def _rows(t: torch.Tensor, dev: int, dtype, B: int, N: int, D: int, name: str):
+    """(heads, elements between rows) of t [B, N, H, D], whose heads must be dense and whose rows evenly spaced."""
+    shape, (sb, sn, sh, sd) = t.shape, t.stride() if t.dim() == 4 else (0, 0, 0, 0)
+    if t.get_device() != dev or t.dtype != dtype or len(shape) != 4 or shape[0] != B or shape[1] != N or shape[3] != D:
+        raise ValueError("%s must be a CUDA tensor of device %d, %s, shape [%d, %d, heads, %d]" % (name, dev, dtype, B, N, D))
+    H = shape[2]
     if sd != 1 or (sh != D and H > 1) or (B > 1 and N > 1 and sb != N * sn):
         raise ValueError("%s: heads must be contiguous and D apart, rows evenly spaced over [B, N]" % name)
-    return sn if N > 1 else (sb if B > 1 else H * D)
+    return H, (sn if N > 1 else (sb if B > 1 else H * D))
+
+
+def _pair(k: torch.Tensor, v: torch.Tensor, dev: int, dtype, name: str):
+    """Shape and strides of a K and a V cache, which must agree."""
+    shape, strides = k.shape, k.stride()
+    if k.get_device() != dev or v.get_device() != dev or k.dtype != dtype or v.dtype != dtype:
+        raise ValueError("%s must be CUDA tensors of device %d, %s" % (name, dev, dtype))
+    if v.shape != shape or v.stride() != strides or len(shape) != 4:
+        raise ValueError("%s must share a 4-dimensional shape and strides" % name)
+    if strides[3] != 1 or strides[2] != shape[3]:
+        raise ValueError("%s: rows must be contiguous and D apart" % name)
+    return shape, strides
 
 
 def _place_args(q_in, k_in, v_in, pos, kv_len, head, q_weight, k_weight, q_out):
     B, N, Hq, D = q_in.shape
-    for t, name in ((q_in, "q_in"), (k_in, "k_in"), (v_in, "v_in")):
-        if not t.is_cuda or t.dtype != q_in.dtype:
-            raise ValueError("%s must be a CUDA tensor of q_in's dtype (this library has no CPU path)" % name)
-    if k_in.shape != v_in.shape or k_in.shape[:2] != (B, N) or k_in.shape[3] != D:
-        raise ValueError("k_in and v_in must be [B, N, Hkv, D]")
-    _need(pos, torch.int32, "pos")
-    _need(kv_len, torch.int32, "kv_len")
-    if tuple(pos.shape) != (B, N) or tuple(kv_len.shape) != (B,):
-        raise ValueError("pos must be [B, N] and kv_len [B]")
-    for w, name in ((q_weight, "q_weight"), (k_weight, "k_weight")):
-        if w is not None:
-            _need(w, q_in.dtype, name)
-            if tuple(w.shape) != (D,):
-                raise ValueError("%s must be [D]" % name)
-    if q_out is None:
-        q_out = torch.empty((B, N, Hq, D), dtype=q_in.dtype, device=q_in.device)
-    _need(q_out, q_in.dtype, "q_out")
-    if q_out.shape != q_in.shape:
-        raise ValueError("q_out must be [B, N, Hq, D]")
-    _one_device(q_in, k_in, v_in, pos, kv_len, q_weight, k_weight, q_out)
+    dtype, dev = q_in.dtype, _device_of(q_in, "q_in")
     head = HeadDesc.from_buffer_copy(head)               # the caller's is left as it is
-    head.q_stride, head.k_stride, head.v_stride = _row_stride(q_in, "q_in"), _row_stride(k_in, "k_in"), _row_stride(v_in, "v_in")
-    return head, q_out, torch.empty(B, dtype=torch.int32, device=q_in.device)
+    _, head.q_stride = _rows(q_in, dev, dtype, B, N, D, "q_in")
+    Hkv, head.k_stride = _rows(k_in, dev, dtype, B, N, D, "k_in")
+    Hv, head.v_stride = _rows(v_in, dev, dtype, B, N, D, "v_in")
+    if Hkv != Hv:
+        raise ValueError("k_in and v_in must have the same heads")
+    _dense(pos, dev, torch.int32, (B, N), "pos")
+    _dense(kv_len, dev, torch.int32, (B,), "kv_len")
+    if q_weight is not None:
+        _dense(q_weight, dev, dtype, (D,), "q_weight")
+    if k_weight is not None:
+        _dense(k_weight, dev, dtype, (D,), "k_weight")
+    if q_out is None:
+        q_out = torch.empty((B, N, Hq, D), dtype=dtype, device=q_in.device)
+    _dense(q_out, dev, dtype, (B, N, Hq, D), "q_out")
+    return head, q_out, torch.empty(B, dtype=torch.int32, device=q_in.device), Hkv, dev
 
 
 def norm_rope_kv_append(q_in, k_in, v_in, pos, kv_len, k_cache, v_cache, head: HeadDesc, q_weight=None, k_weight=None, q_out=None):
     """Norm and rotation of the query and key heads as ``head`` (``make_head_desc``) says, K and V into the caches.
     q_in [B, N, Hq, D], k_in, v_in [B, N, Hkv, D] (rows may be strided: slices of a fused projection); pos [B, N] int32;
     kv_len [B] int32; caches [B, Hkv, cap, D] (written in place at rows kv_len[b] + r).  Returns (q_out, status)."""
-    head, q_out, status = _place_args(q_in, k_in, v_in, pos, kv_len, head, q_weight, k_weight, q_out)
-    if not (k_cache.is_cuda and v_cache.is_cuda) or k_cache.dtype != q_in.dtype or v_cache.dtype != q_in.dtype:
-        raise ValueError("caches must be CUDA tensors of q_in's dtype")
-    if k_cache.stride() != v_cache.stride() or k_cache.shape != v_cache.shape or k_cache.shape[1] != k_in.shape[2]:
-        raise ValueError("k_cache and v_cache must share shape and strides and hold k_in's heads")
-    _one_device(q_in, k_cache, v_cache)
-    desc = make_attn_desc(q_in, k_cache)
-    _check(load().ht_norm_rope_kv_append(ctypes.byref(desc), ctypes.byref(head), _ptr(q_in), _ptr(k_in), _ptr(v_in), _ptr(q_weight),
-                                         _ptr(k_weight), _ptr(pos), _ptr(kv_len), _ptr(q_out), _ptr(k_cache), _ptr(v_cache),
-                                         _ptr(status), _stream()))
+    head, q_out, status, Hkv, dev = _place_args(q_in, k_in, v_in, pos, kv_len, head, q_weight, k_weight, q_out)
+    (Bc, Hc, cap, Dc), strides = _pair(k_cache, v_cache, dev, q_in.dtype, "caches")
+    B, N, Hq, D = q_in.shape
+    if Bc != B or Hc != Hkv or Dc != D:
+        raise ValueError("the caches must be [B, Hkv, cap, D]")
+    desc = AttnDesc(B, N, Hq, Hkv, D, cap, _DTYPES[q_in.dtype], 0.0, strides[0], strides[1], 0, 0)
+    _check(load().ht_norm_rope_kv_append(ctypes.byref(desc), ctypes.byref(head), q_in.data_ptr(), k_in.data_ptr(), v_in.data_ptr(),
+                                         _ptr(q_weight), _ptr(k_weight), pos.data_ptr(), kv_len.data_ptr(), q_out.data_ptr(),
+                                         k_cache.data_ptr(), v_cache.data_ptr(), status.data_ptr(), _stream()))
     return q_out, status
 
 
@@ -551,56 +573,53 @@ def norm_rope_kv_append_paged(q_in, k_in, v_in, pos, kv_len, block_table, k_page
                               k_weight=None, q_out=None):
     """As ``norm_rope_kv_append`` with the caches as page pools [n_pages, Hkv, page_size, D] (written in place at the
     logical rows kv_len[b] + r through block_table [B, max_pages]).  Returns (q_out, status)."""
-    head, q_out, status = _place_args(q_in, k_in, v_in, pos, kv_len, head, q_weight, k_weight, q_out)
-    _need(block_table, torch.int32, "block_table")
+    head, q_out, status, Hkv, dev = _place_args(q_in, k_in, v_in, pos, kv_len, head, q_weight, k_weight, q_out)
+    (n_pages, Hp, page_size, Dp), strides = _pair(k_pages, v_pages, dev, q_in.dtype, "page pools")
     B, N, Hq, D = q_in.shape
-    n_pages, Hkv, page_size, Dp = k_pages.shape
-    if not (k_pages.is_cuda and v_pages.is_cuda) or k_pages.dtype != q_in.dtype or v_pages.dtype != q_in.dtype:
-        raise ValueError("page pools must be CUDA tensors of q_in's dtype")
-    if Dp != D or Hkv != k_in.shape[2] or k_pages.stride(3) != 1 or k_pages.stride(2) != D or k_pages.stride() != v_pages.stride() \
-            or k_pages.shape != v_pages.shape:
-        raise ValueError("page rows must be contiguous and D apart, K and V pools alike and of k_in's heads")
-    if block_table.dim() != 2 or block_table.shape[0] != B:
+    if Hp != Hkv or Dp != D:
+        raise ValueError("the pools must be [n_pages, Hkv, page_size, D]")
+    if block_table.dim() != 2:
         raise ValueError("block_table must be [B, max_pages]")
-    _one_device(q_in, k_pages, v_pages, block_table)
     max_pages = block_table.shape[1]
+    _dense(block_table, dev, torch.int32, (B, max_pages), "block_table")
     desc = AttnDesc(B, N, Hq, Hkv, D, max_pages * page_size, _DTYPES[q_in.dtype], 0.0, 0, 0, 0, 0)
-    pages = PagedDesc(page_size, max_pages, n_pages, k_pages.stride(0), k_pages.stride(1))
-    _check(load().ht_norm_rope_kv_append_paged(ctypes.byref(desc), ctypes.byref(head), ctypes.byref(pages), _ptr(q_in), _ptr(k_in),
-                                               _ptr(v_in), _ptr(q_weight), _ptr(k_weight), _ptr(pos), _ptr(kv_len), _ptr(block_table),
-                                               _ptr(q_out), _ptr(k_pages), _ptr(v_pages), _ptr(status), _stream()))
+    pages = PagedDesc(page_size, max_pages, n_pages, strides[0], strides[1])
+    _check(load().ht_norm_rope_kv_append_paged(ctypes.byref(desc), ctypes.byref(head), ctypes.byref(pages), q_in.data_ptr(),
+                                               k_in.data_ptr(), v_in.data_ptr(), _ptr(q_weight), _ptr(k_weight), pos.data_ptr(),
+                                               kv_len.data_ptr(), block_table.data_ptr(), q_out.data_ptr(), k_pages.data_ptr(),
+                                               v_pages.data_ptr(), status.data_ptr(), _stream()))
     return q_out, status
 
 
 def _sample_args(logits, uniform, temperature, top_k, top_p, min_p):
-    _need(logits, name="logits")
-    _need(uniform, torch.float32, "uniform")
     B, N, V = logits.shape
-    if tuple(uniform.shape) != (B, N):
-        raise ValueError("uniform must be [B, N]")
-    for t, dtype, name in ((temperature, torch.float32, "temperature"), (top_k, torch.int32, "top_k"),
-                           (top_p, torch.float32, "top_p"), (min_p, torch.float32, "min_p")):
-        if t is not None:
-            _need(t, dtype, name)
-            if tuple(t.shape) != (B,):
-                raise ValueError("%s must be [B]" % name)
-    _one_device(logits, uniform, temperature, top_k, top_p, min_p)
-    return B, N, V
+    dev = _device_of(logits, "logits")
+    if not logits.is_contiguous():
+        raise ValueError("logits must be contiguous")
+    _dense(uniform, dev, torch.float32, (B, N), "uniform")
+    if temperature is not None:
+        _dense(temperature, dev, torch.float32, (B,), "temperature")
+    if top_k is not None:
+        _dense(top_k, dev, torch.int32, (B,), "top_k")
+    if top_p is not None:
+        _dense(top_p, dev, torch.float32, (B,), "top_p")
+    if min_p is not None:
+        _dense(min_p, dev, torch.float32, (B,), "min_p")
+    return B, N, V, dev
 
 
 def sample(logits, uniform, temperature=None, top_k=None, top_p=None, min_p=None, token=None):
     """Tokens drawn from the filtered distributions of logits [B, N, V] with uniform [B, N] float32 numbers in [0, 1];
     temperature, top_p, min_p [B] float32 and top_k [B] int32, or None.  Returns (token [B, N], status [B])."""
-    B, N, V = _sample_args(logits, uniform, temperature, top_k, top_p, min_p)
+    B, N, V, dev = _sample_args(logits, uniform, temperature, top_k, top_p, min_p)
+    device = logits.device
     if token is None:
-        token = torch.empty((B, N), dtype=torch.int32, device=logits.device)
-    _need(token, torch.int32, "token")
-    if tuple(token.shape) != (B, N):
-        raise ValueError("token must be [B, N]")
-    _one_device(logits, token)
-    status = torch.empty(B, dtype=torch.int32, device=logits.device)
-    _check(load().ht_sample(_ptr(logits), _DTYPES[logits.dtype], B, N, V, _ptr(uniform), _ptr(temperature), _ptr(top_k), _ptr(top_p),
-                            _ptr(min_p), _ptr(token), _ptr(status), _stream()))
+        token = torch.empty((B, N), dtype=torch.int32, device=device)
+    else:
+        _dense(token, dev, torch.int32, (B, N), "token")
+    status = torch.empty(B, dtype=torch.int32, device=device)
+    _check(load().ht_sample(logits.data_ptr(), _DTYPES[logits.dtype], B, N, V, uniform.data_ptr(), _ptr(temperature), _ptr(top_k),
+                            _ptr(top_p), _ptr(min_p), token.data_ptr(), status.data_ptr(), _stream()))
     return token, status
 
 
@@ -609,109 +628,99 @@ def verify_sampled(logits, uniform, tokens, parent, root_pred=None, temperature=
     """``verify_greedy`` with the tree rows' tokens drawn as ``sample`` draws them.  logits [B, N, V], uniform [B, N];
     tokens [B, T], parent [B, N] int32, root_pred [B] int32 or None; ``accept_len`` as in ``verify_greedy``.
     Returns (pred [B, N], accept_len [B], accept_path [B, max_path], next_token [B], status [B])."""
-    B, N, V = _sample_args(logits, uniform, temperature, top_k, top_p, min_p)
-    _need(tokens, torch.int32, "tokens")
-    _need(parent, torch.int32, "parent")
-    if tuple(parent.shape) != (B, N) or tokens.dim() != 2 or tokens.shape[0] != B:
-        raise ValueError("parent must be [B, N] and tokens [B, T]")
+    B, N, V, dev = _sample_args(logits, uniform, temperature, top_k, top_p, min_p)
+    if tokens.dim() != 2:
+        raise ValueError("tokens must be [B, T]")
+    T = tokens.shape[1]
+    _dense(tokens, dev, torch.int32, (B, T), "tokens")
+    _dense(parent, dev, torch.int32, (B, N), "parent")
     if root_pred is not None:
-        _need(root_pred, torch.int32, "root_pred")
-        if tuple(root_pred.shape) != (B,):
-            raise ValueError("root_pred must be [B]")
-    dev = logits.device
+        _dense(root_pred, dev, torch.int32, (B,), "root_pred")
+    device = logits.device
     if accept_len is None:
-        accept_len = torch.zeros(B, dtype=torch.int32, device=dev)
+        accept_len = torch.zeros(B, dtype=torch.int32, device=device)
     else:
-        _need(accept_len, torch.int32, "accept_len")
-        if tuple(accept_len.shape) != (B,):
-            raise ValueError("accept_len must be [B]")
-    _one_device(logits, tokens, parent, root_pred, accept_len)
-    pred = torch.empty((B, N), dtype=torch.int32, device=dev)
-    accept_path = torch.empty((B, max_path), dtype=torch.int32, device=dev)
-    next_token = torch.empty(B, dtype=torch.int32, device=dev)
-    status = torch.empty(B, dtype=torch.int32, device=dev)
-    _check(load().ht_verify_sampled(_ptr(logits), _DTYPES[logits.dtype], _ptr(uniform), _ptr(temperature), _ptr(top_k), _ptr(top_p),
-                                    _ptr(min_p), _ptr(tokens), _ptr(parent), _ptr(root_pred), B, N, tokens.shape[1], V, max_path,
-                                    _ptr(pred), _ptr(accept_len), _ptr(accept_path), _ptr(next_token), _ptr(status), _stream()))
+        _dense(accept_len, dev, torch.int32, (B,), "accept_len")
+    pred = torch.empty((B, N), dtype=torch.int32, device=device)
+    accept_path = torch.empty((B, max_path), dtype=torch.int32, device=device)
+    next_token = torch.empty(B, dtype=torch.int32, device=device)
+    status = torch.empty(B, dtype=torch.int32, device=device)
+    _check(load().ht_verify_sampled(logits.data_ptr(), _DTYPES[logits.dtype], uniform.data_ptr(), _ptr(temperature), _ptr(top_k),
+                                    _ptr(top_p), _ptr(min_p), tokens.data_ptr(), parent.data_ptr(), _ptr(root_pred), B, N, T, V,
+                                    max_path, pred.data_ptr(), accept_len.data_ptr(), accept_path.data_ptr(), next_token.data_ptr(),
+                                    status.data_ptr(), _stream()))
     return pred, accept_len, accept_path, next_token, status
 
 
-def _score_desc(q, cap, slopes, pos) -> ScoreDesc:
-    B, N, Hq, _ = q.shape
-    if slopes is not None:
-        _need(slopes, torch.float32, "slopes")
-        if pos is None:
-            raise ValueError("slopes need pos")
-        _need(pos, torch.int32, "pos")
-        if tuple(slopes.shape) != (Hq,) or tuple(pos.shape) != (B, N):
-            raise ValueError("slopes must be [Hq] and pos [B, N]")
-        _one_device(q, slopes, pos)
-    return ScoreDesc(float(cap), _ptr(slopes), None if slopes is None else _ptr(pos))
+def _scored_args(q, kv_len, parent, cap, slopes, pos):
+    if q.dim() != 4:
+        raise ValueError("q must be [B, N, Hq, D]")
+    B, N, Hq, D = q.shape
+    dev = _device_of(q, "q")
+    if not q.is_contiguous():
+        raise ValueError("q must be contiguous")
+    _dense(kv_len, dev, torch.int32, (B,), "kv_len")
+    _dense(parent, dev, torch.int32, (B, N), "parent")
+    if slopes is None:
+        return B, N, Hq, D, dev, ScoreDesc(cap, None, None)
+    _dense(slopes, dev, torch.float32, (Hq,), "slopes")
+    if pos is None:
+        raise ValueError("slopes need pos")
+    _dense(pos, dev, torch.int32, (B, N), "pos")
+    return B, N, Hq, D, dev, ScoreDesc(cap, slopes.data_ptr(), pos.data_ptr())
 
 
-def _attn_buffers(q, desc, out, workspace):
+def _attn_buffers(q, dev, desc, out, workspace, status):
+    """The call's outputs and workspace, those that were not passed allocated."""
     if out is None:
         out = torch.empty_like(q)
-    _need(out, q.dtype, "out")
-    if out.shape != q.shape:
-        raise ValueError("out must have q's shape")
-    need = tree_attention_workspace(desc)
-    if workspace is None and need:
-        workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
-    return out, workspace, 0 if workspace is None else workspace.numel() * workspace.element_size()
+    else:
+        _dense(out, dev, q.dtype, q.shape, "out")
+    if workspace is None:
+        need = tree_attention_workspace(desc)
+        ws, ws_bytes = (None, 0) if need == 0 else (torch.empty(need, dtype=torch.uint8, device=q.device), need)
+    else:
+        if workspace.get_device() != dev or not workspace.is_contiguous():
+            raise ValueError("workspace must be a contiguous CUDA tensor of device %d" % dev)
+        ws, ws_bytes = workspace, workspace.numel() * workspace.element_size()
+    if status is None:
+        status = torch.empty(q.shape[0], dtype=torch.int32, device=q.device)
+    else:
+        _dense(status, dev, torch.int32, q.shape[:1], "status")
+    return out, ws, ws_bytes, status
 
 
 def tree_attention_scored(q, k_cache, v_cache, kv_len, parent, cap: float = 0.0, slopes=None, pos=None, out=None, workspace=None,
                           status=None, scale: float = 0.0, num_splits: int = 0, flags: int = 0):
     """``tree_attention`` with the scores capped (cap * tanh(s / cap), 0: not) and biased by distance (slopes [Hq] float32
     with pos [B, N] int32, or None).  Returns (out, status)."""
-    _need(q, name="q")
-    _need(kv_len, torch.int32, "kv_len")
-    _need(parent, torch.int32, "parent")
-    if not (k_cache.is_cuda and v_cache.is_cuda) or k_cache.dtype != q.dtype or v_cache.dtype != q.dtype:
-        raise ValueError("caches must be CUDA tensors of q's dtype")
-    if k_cache.stride() != v_cache.stride() or k_cache.shape != v_cache.shape:
-        raise ValueError("k_cache and v_cache must share shape and strides")
-    _one_device(q, k_cache, v_cache, kv_len, parent, out, workspace, status)
-    score = _score_desc(q, cap, slopes, pos)
-    desc = make_attn_desc(q, k_cache, scale, num_splits, flags)
-    B, N = desc.B, desc.N
-    if tuple(parent.shape) != (B, N) or tuple(kv_len.shape) != (B,):
-        raise ValueError("parent must be [B, N] and kv_len [B]")
-    out, workspace, ws_bytes = _attn_buffers(q, desc, out, workspace)
-    if status is None:
-        status = torch.empty(B, dtype=torch.int32, device=q.device)
-    _check(load().ht_tree_attention_scored(ctypes.byref(desc), ctypes.byref(score), _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(kv_len),
-                                           _ptr(parent), _ptr(out), _ptr(workspace), ws_bytes, _ptr(status), _stream()))
+    B, N, Hq, D, dev, score = _scored_args(q, kv_len, parent, cap, slopes, pos)
+    (Bc, Hkv, rows, Dc), strides = _pair(k_cache, v_cache, dev, q.dtype, "caches")
+    if Bc != B or Dc != D:
+        raise ValueError("the caches must be [B, Hkv, cap, D]")
+    desc = AttnDesc(B, N, Hq, Hkv, D, rows, _DTYPES[q.dtype], scale, strides[0], strides[1], num_splits, flags)
+    out, ws, ws_bytes, status = _attn_buffers(q, dev, desc, out, workspace, status)
+    _check(load().ht_tree_attention_scored(ctypes.byref(desc), ctypes.byref(score), q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(),
+                                           kv_len.data_ptr(), parent.data_ptr(), out.data_ptr(), _ptr(ws), ws_bytes, status.data_ptr(),
+                                           _stream()))
     return out, status
 
 
 def tree_attention_scored_paged(q, k_pages, v_pages, block_table, kv_len, parent, cap: float = 0.0, slopes=None, pos=None, out=None,
                                 workspace=None, status=None, scale: float = 0.0, flags: int = 0):
     """``tree_attention_paged`` with the scores shaped as in ``tree_attention_scored``.  Returns (out, status)."""
-    _need(q, name="q")
-    _need(block_table, torch.int32, "block_table")
-    _need(kv_len, torch.int32, "kv_len")
-    _need(parent, torch.int32, "parent")
-    if not (k_pages.is_cuda and v_pages.is_cuda) or k_pages.dtype != q.dtype or v_pages.dtype != q.dtype:
-        raise ValueError("page pools must be CUDA tensors of q's dtype")
-    if k_pages.stride() != v_pages.stride() or k_pages.shape != v_pages.shape:
-        raise ValueError("k_pages and v_pages must share shape and strides")
-    _one_device(q, k_pages, v_pages, block_table, kv_len, parent, out, workspace, status)
-    B, N, Hq, D = q.shape
-    n_pages, Hkv, page_size, Dp = k_pages.shape
-    if Dp != D or k_pages.stride(3) != 1 or k_pages.stride(2) != D:
-        raise ValueError("page rows must be contiguous and D apart")
-    if block_table.dim() != 2 or block_table.shape[0] != B or tuple(parent.shape) != (B, N) or tuple(kv_len.shape) != (B,):
-        raise ValueError("block_table must be [B, max_pages], parent [B, N], kv_len [B]")
-    score = _score_desc(q, cap, slopes, pos)
+    B, N, Hq, D, dev, score = _scored_args(q, kv_len, parent, cap, slopes, pos)
+    (n_pages, Hkv, page_size, Dp), strides = _pair(k_pages, v_pages, dev, q.dtype, "page pools")
+    if Dp != D:
+        raise ValueError("the pools must be [n_pages, Hkv, page_size, D]")
+    if block_table.dim() != 2:
+        raise ValueError("block_table must be [B, max_pages]")
     max_pages = block_table.shape[1]
+    _dense(block_table, dev, torch.int32, (B, max_pages), "block_table")
     desc = AttnDesc(B, N, Hq, Hkv, D, max_pages * page_size, _DTYPES[q.dtype], scale, 0, 0, 0, flags)
-    pages = PagedDesc(page_size, max_pages, n_pages, k_pages.stride(0), k_pages.stride(1))
-    out, workspace, ws_bytes = _attn_buffers(q, desc, out, workspace)
-    if status is None:
-        status = torch.empty(B, dtype=torch.int32, device=q.device)
-    _check(load().ht_tree_attention_scored_paged(ctypes.byref(desc), ctypes.byref(pages), ctypes.byref(score), _ptr(q), _ptr(k_pages),
-                                                 _ptr(v_pages), _ptr(block_table), _ptr(kv_len), _ptr(parent), _ptr(out),
-                                                 _ptr(workspace), ws_bytes, _ptr(status), _stream()))
+    pages = PagedDesc(page_size, max_pages, n_pages, strides[0], strides[1])
+    out, ws, ws_bytes, status = _attn_buffers(q, dev, desc, out, workspace, status)
+    _check(load().ht_tree_attention_scored_paged(ctypes.byref(desc), ctypes.byref(pages), ctypes.byref(score), q.data_ptr(),
+                                                 k_pages.data_ptr(), v_pages.data_ptr(), block_table.data_ptr(), kv_len.data_ptr(),
+                                                 parent.data_ptr(), out.data_ptr(), _ptr(ws), ws_bytes, status.data_ptr(), _stream()))
     return out, status

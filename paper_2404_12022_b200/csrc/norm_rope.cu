@@ -5,13 +5,14 @@
 //     the first rot_dim features of y in pairs (a, b): (a cos - b sin, b cos + a sin) of the angle pos * f_i
 // with pair i = (i, i + rot_dim / 2) or (2 i, 2 i + 1), and the frequencies f_i formed on the host in 64 bits.
 //
-// Every value is read once and written once: bound by HBM for prompts (8 x 2048 rows of 80 heads: see the launcher), by
-// the launch and one round trip to memory for a tree's rows.  One block per (sequence, row).  A head is D / 2 features
-// by lanes that hold two 16-byte vectors each, chosen so that both features of every pair meet in one lane: the rotation
-// needs no exchange, the mean a shuffle over 4 to 16 lanes.  A lane keeps its place within the head for all heads of
-// the row, so the cosines and sines are loaded into registers once; the first heads' vectors are on their way while the
-// angles are formed.  Angles: the position times the frequency in turns, in 64 bits, its fraction to 32 (a position of
-// a hundred thousand leaves a 32-bit product no low bits); products and sums in 32 bits, one rounding to the type.
+// Every value is read once and written once: bound by HBM for prompts, by the launch and one round trip to memory for a
+// tree's rows.  A block takes rows of the batch by turns.  A head is D / 2 features by lanes that hold two 16-byte
+// vectors each, chosen so that both features of every pair meet in one lane: the rotation needs no exchange, the mean a
+// shuffle over 4 to 16 lanes.  A lane keeps its place within the head for all heads of a row, so the cosines and sines
+// are loaded into registers once per row; up to three heads per lane are in flight, and as soon as one has been used the
+// next row's vectors are asked for in its place.  Angles: the position times the frequency in turns, in 64 bits, its
+// fraction to 32 (a position of a hundred thousand leaves a 32-bit product no low bits); products and sums in 32 bits,
+// one rounding to the type.
 #include <math.h>
 
 #include "ht_common.cuh"
@@ -28,6 +29,8 @@ struct PlaceArgs {
     const int32_t *pos, *kv_len;
     int32_t *status;
     int N, Hq, Hkv, cap, rot, norm;
+    int chunks;                   // of kPlaceAhead * (heads per block pass) heads
+    long long rows;
     float eps, offset, magnitude;
     long long q_stride, k_stride, v_stride, stride_b, stride_h;
 };
@@ -36,24 +39,12 @@ constexpr int kPlaceThreads = 256;
 constexpr int kPlaceAhead = 3;    // heads per lane whose vectors are asked for before the angles are formed
 
 template <typename T, int D, bool kInterleaved>
-__global__ void __launch_bounds__(kPlaceThreads)
+__global__ void __launch_bounds__(kPlaceThreads, 2)
 norm_rope_kernel(const PlaceArgs p, const PageMap pm, const __grid_constant__ RopeTurns turns) {
     // lets a kernel that is serialized programmatically behind this one (the attention call) set itself up meanwhile
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     constexpr int VE = Vec16<T>::n, LPH = D / (2 * VE), HPB = kPlaceThreads / LPH;     // lanes per head, heads per block pass
-    __shared__ float s_cos[D / 2], s_sin[D / 2];
-    const int b = blockIdx.x / p.N, r = blockIdx.x - b * p.N;
-    const int L = p.kv_len[b];
-    const bool bad = L < 0 || (long long)L + p.N > p.cap;
-    if (r == 0) {                                        // the sequence's word, by one block: its length, its pages
-        int bad_page = 0;
-        if (!bad && pm.table)
-            for (int i = (L >> pm.shift) + threadIdx.x; i <= (L + p.N - 1) >> pm.shift; i += kPlaceThreads)
-                bad_page |= (unsigned)pm.table[(size_t)b * pm.max_pages + i] >= (unsigned)pm.n_pages;
-        bad_page = __syncthreads_or(bad_page);
-        if (threadIdx.x == 0) p.status[b] = bad ? HT_STATUS_BAD_LEN : (bad_page ? HT_STATUS_BAD_PAGE : HT_STATUS_OK);
-    }
-    if (bad) return;
+    __shared__ float s_cos[2][D / 2], s_sin[2][D / 2];
     const int half_rot = p.rot >> 1;
     const int group = threadIdx.x / LPH, j = threadIdx.x - group * LPH;
     // this lane's two vectors within a head
@@ -69,91 +60,130 @@ norm_rope_kernel(const PlaceArgs p, const PageMap pm, const __grid_constant__ Ro
         v0 = rotates ? j : 2 * j;
         v1 = rotates ? j + R : 2 * j + 1;
     }
-    // where cache row L + r of this sequence starts, short of the head's offset
-    long long row_off = (long long)b * p.stride_b + (long long)(L + r) * D;
-    bool no_page = false;
-    if (pm.table) {
-        const int page = pm.table[(size_t)b * pm.max_pages + ((L + r) >> pm.shift)];
-        no_page = (unsigned)page >= (unsigned)pm.n_pages;     // the row's K and V are not stored; its q is written
-        row_off = (long long)page * pm.page_stride + (long long)((L + r) & ((1 << pm.shift) - 1)) * D;
-    }
-    const size_t row = (size_t)b * p.N + r;
-    const int heads = p.Hq + 2 * p.Hkv;
-    auto source = [&](int h) -> const uint4 * {
-        const T *src = h < p.Hq            ? static_cast<const T *>(p.q_in) + row * p.q_stride + (size_t)h * D
-                       : h < p.Hq + p.Hkv ? static_cast<const T *>(p.k_in) + row * p.k_stride + (size_t)(h - p.Hq) * D
-                                          : static_cast<const T *>(p.v_in) + row * p.v_stride + (size_t)(h - p.Hq - p.Hkv) * D;
-        return reinterpret_cast<const uint4 *>(src);
-    };
-    uint4 in0[kPlaceAhead], in1[kPlaceAhead];
-    auto ask = [&](int h0) {
+    // A block keeps one chunk of kPlaceAhead * HPB heads for all its rows: what a lane's heads are is settled here.
+    enum { kQ = 0, kK = 1, kV = 2, kNone = 3 };
+    const int chunk = (int)(blockIdx.x % (unsigned)p.chunks), step = (int)(gridDim.x / (unsigned)p.chunks);
+    int kind[kPlaceAhead], head[kPlaceAhead];
+    const uint4 *src[kPlaceAhead];
+    long long row = blockIdx.x / (unsigned)p.chunks;
 #pragma unroll
-        for (int u = 0; u < kPlaceAhead; ++u) {
-            const int h = h0 + u * HPB;
-            if (h < heads) {
-                const uint4 *src = source(h);
-                in0[u] = src[v0];
-                in1[u] = src[v1];
-            }
+    for (int u = 0; u < kPlaceAhead; ++u) {
+        const int h = chunk * kPlaceAhead * HPB + group + u * HPB;
+        kind[u] = h < p.Hq ? kQ : (h < p.Hq + p.Hkv ? kK : (h < p.Hq + 2 * p.Hkv ? kV : kNone));
+        head[u] = kind[u] == kQ ? h : (kind[u] == kK ? h - p.Hq : h - p.Hq - p.Hkv);
+        const T *base = static_cast<const T *>(kind[u] == kQ ? p.q_in : (kind[u] == kK ? p.k_in : p.v_in));
+        const long long stride = kind[u] == kQ ? p.q_stride : (kind[u] == kK ? p.k_stride : p.v_stride);
+        src[u] = reinterpret_cast<const uint4 *>(base + row * stride + (long long)head[u] * D);
+    }
+    uint4 in0[kPlaceAhead], in1[kPlaceAhead];
+    auto ask = [&](int u) {                              // the vectors of this lane's head u, and on to the block's next row
+        if (kind[u] != kNone) {
+            in0[u] = src[u][v0];
+            in1[u] = src[u][v1];
         }
+        src[u] += (kind[u] == kQ ? p.q_stride : (kind[u] == kK ? p.k_stride : p.v_stride)) / VE * step;
     };
-    ask(group);
-    for (int i = threadIdx.x; i < half_rot; i += kPlaceThreads) {
-        const double t = (double)p.pos[row] * turns.f[i];
+#pragma unroll
+    for (int u = 0; u < kPlaceAhead; ++u) ask(u);
+    // the query weights stay in registers (ones without weights); the few key heads read theirs where they need them
+    float wq[2 * VE];
+    {
+        const uint4 *w = static_cast<const uint4 *>(p.q_weight);
+        if (w) {
+            unpack16<T>(__ldg(w + v0), wq);
+            unpack16<T>(__ldg(w + v1), wq + VE);
+        }
+#pragma unroll
+        for (int e = 0; e < 2 * VE; ++e) wq[e] = w ? wq[e] + p.offset : 1.f;
+    }
+    // Cosines and sines of a row's position into one of two tables; the next row's are formed while the current row's are
+    // in use, its position having been asked for a row earlier, by two warps that take turns.
+    auto form_table = [&](int at, int i, int turn) {
+        const double t = (double)at * turns.f[i];
         float s, c;
         sincospif(2.f * (float)(t - rint(t)), &s, &c);
-        s_cos[i] = c * p.magnitude;
-        s_sin[i] = s * p.magnitude;
-    }
-    __syncthreads();
-    // The lane's pairs, for all heads of the row.  Half-split: the VE pairs of vector v0; interleaved: VE / 2 pairs of
-    // v0, then VE / 2 of v1.
-    float cs[VE], sn[VE];
-    bool turned[VE];
+        s_cos[turn][i] = c * p.magnitude;
+        s_sin[turn][i] = s * p.magnitude;
+    };
+    int me = threadIdx.x;                                // the pair this thread forms, where below half_rot (at most 64)
+    if (me < half_rot) form_table(p.pos[row], me, 0);
+    int pos_next = row + step < p.rows ? p.pos[row + step] : 0;
+    for (int turn = 0; row < p.rows; row += step, turn ^= 1) {
+        const long long next = row + step;
+        const int b = (int)((unsigned)row / (unsigned)p.N), r = (int)row - b * p.N;
+        const int L = p.kv_len[b];
+        const bool bad = L < 0 || (long long)L + p.N > p.cap;
+        // where cache row L + r of this sequence starts, short of the head's offset
+        long long row_off = (long long)b * p.stride_b + (long long)(L + r) * D;
+        bool no_page = false;
+        if (pm.table && !bad) {
+            const int page = pm.table[(size_t)b * pm.max_pages + ((L + r) >> pm.shift)];
+            no_page = (unsigned)page >= (unsigned)pm.n_pages;     // the row's K and V are not stored; its q is written
+            row_off = (long long)page * pm.page_stride + (long long)((L + r) & ((1 << pm.shift) - 1)) * D;
+        }
+        if (r == 0 && chunk == 0) {                      // the sequence's word, by one block: its length, its pages
+            int bad_page = 0;
+            if (!bad && pm.table)
+                for (int i = (L >> pm.shift) + threadIdx.x; i <= (L + p.N - 1) >> pm.shift; i += kPlaceThreads)
+                    bad_page |= (unsigned)pm.table[(size_t)b * pm.max_pages + i] >= (unsigned)pm.n_pages;
+            bad_page = __syncthreads_or(bad_page);
+            if (threadIdx.x == 0) p.status[b] = bad ? HT_STATUS_BAD_LEN : (bad_page ? HT_STATUS_BAD_PAGE : HT_STATUS_OK);
+        }
+        __syncthreads();                                 // the row's table is complete, the other one's readers are done
+        // The lane's pairs, for all heads of the row.  Half-split: the VE pairs of vector v0; interleaved: VE / 2 pairs of
+        // v0, then VE / 2 of v1.
+        float cs[VE], sn[VE];
 #pragma unroll
-    for (int e = 0; e < VE; ++e) {
-        const int pair = kInterleaved ? (e < VE / 2 ? v0 * (VE / 2) + e : v1 * (VE / 2) + e - VE / 2) : j * VE + e;
-        turned[e] = pair < half_rot;
-        cs[e] = turned[e] ? s_cos[pair] : 1.f;
-        sn[e] = turned[e] ? s_sin[pair] : 0.f;
-    }
-    for (int h0 = group; h0 - group < heads; h0 += kPlaceAhead * HPB) {      // (uniform over the block: the shuffles below need whole warps)
-        if (h0 != group) ask(h0);
+        for (int e = 0; e < VE; ++e) {
+            const int pair = kInterleaved ? (e < VE / 2 ? v0 * (VE / 2) + e : v1 * (VE / 2) + e - VE / 2) : j * VE + e;
+            cs[e] = pair < half_rot ? s_cos[turn][pair] : 1.f;
+            sn[e] = pair < half_rot ? s_sin[turn][pair] : 0.f;
+        }
+        me = (me + 64) & (kPlaceThreads - 1);
+        if (next < p.rows) {
+            if (me < half_rot) form_table(pos_next, me, turn ^ 1);
+            if (next + step < p.rows) pos_next = p.pos[next + step];
+        }
 #pragma unroll
         for (int u = 0; u < kPlaceAhead; ++u) {
-            const int h = h0 + u * HPB;
-            if (h - group >= heads) break;
-            const bool is_q = h < p.Hq, is_k = !is_q && h < p.Hq + p.Hkv;
+            uint4 out0 = in0[u], out1 = in1[u];
+            if (next < p.rows) ask(u);                   // the place is free for the next row's vectors
             float x[2 * VE];
-            unpack16<T>(in0[u], x);
-            unpack16<T>(in1[u], x + VE);
-            float ss = 0.f;
+            unpack16<T>(out0, x);
+            unpack16<T>(out1, x + VE);
+            float ss = 0.f, ss1 = 0.f;
 #pragma unroll
-            for (int e = 0; e < 2 * VE; ++e) ss = fmaf(x[e], x[e], ss);
+            for (int e = 0; e < VE; ++e) {
+                ss = fmaf(x[e], x[e], ss);
+                ss1 = fmaf(x[VE + e], x[VE + e], ss1);
+            }
+            ss += ss1;
 #pragma unroll
             for (int off = LPH / 2; off > 0; off >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, off);
-            if (h >= heads || (!is_q && no_page)) continue;
-            uint4 out0 = in0[u], out1 = in1[u];
-            if (is_q || is_k) {
-                if (p.norm & (is_q ? HT_HEAD_NORM_Q : HT_HEAD_NORM_K)) {
-                    const float inv = 1.f / sqrtf(ss * (1.f / D) + p.eps);
-                    const uint4 *w = static_cast<const uint4 *>(is_q ? p.q_weight : p.k_weight);
-                    if (w) {
-                        float wf[2 * VE];
-                        unpack16<T>(__ldg(w + v0), wf);
-                        unpack16<T>(__ldg(w + v1), wf + VE);
+            if (bad || kind[u] == kNone || (kind[u] != kQ && no_page)) continue;
+            if (kind[u] != kV) {
+                if (p.norm & (kind[u] == kQ ? HT_HEAD_NORM_Q : HT_HEAD_NORM_K)) {
+                    const float inv = rsqrtf(fmaf(ss, 1.f / D, p.eps));
+                    if (kind[u] == kQ) {
 #pragma unroll
-                        for (int e = 0; e < 2 * VE; ++e) x[e] *= inv * (wf[e] + p.offset);
+                        for (int e = 0; e < 2 * VE; ++e) x[e] *= inv * wq[e];
                     } else {
+                        const uint4 *w = static_cast<const uint4 *>(p.k_weight);
+                        float wk[2 * VE];
+                        if (w) {
+                            unpack16<T>(__ldg(w + v0), wk);
+                            unpack16<T>(__ldg(w + v1), wk + VE);
+                        }
 #pragma unroll
-                        for (int e = 0; e < 2 * VE; ++e) x[e] *= inv;
+                        for (int e = 0; e < 2 * VE; ++e) x[e] *= w ? inv * (wk[e] + p.offset) : inv;
                     }
                 }
                 if (rotates) {
 #pragma unroll
                     for (int e = 0; e < VE; ++e) {
                         const int a = kInterleaved ? 2 * e : e, c = kInterleaved ? 2 * e + 1 : e + VE;
-                        if (turned[e]) {
+                        // an unrotated pair stays as it is, infinities included (interleaved: within a rotating lane)
+                        if (!kInterleaved || (e < VE / 2 ? v0 * (VE / 2) + e : v1 * (VE / 2) + e - VE / 2) < half_rot) {
                             const float xa = x[a], xc = x[c];
                             x[a] = xa * cs[e] - xc * sn[e];
                             x[c] = xc * cs[e] + xa * sn[e];
@@ -166,9 +196,8 @@ norm_rope_kernel(const PlaceArgs p, const PageMap pm, const __grid_constant__ Ro
                 out0 = *reinterpret_cast<const uint4 *>(o);
                 out1 = *reinterpret_cast<const uint4 *>(o + VE);
             }
-            T *dst = is_q   ? static_cast<T *>(p.q_out) + (row * p.Hq + h) * D
-                     : is_k ? static_cast<T *>(p.k_cache) + row_off + (size_t)(h - p.Hq) * p.stride_h
-                            : static_cast<T *>(p.v_cache) + row_off + (size_t)(h - p.Hq - p.Hkv) * p.stride_h;
+            T *dst = kind[u] == kQ ? static_cast<T *>(p.q_out) + (row * p.Hq + head[u]) * D
+                                   : static_cast<T *>(kind[u] == kK ? p.k_cache : p.v_cache) + row_off + head[u] * p.stride_h;
             reinterpret_cast<uint4 *>(dst)[v0] = out0;
             reinterpret_cast<uint4 *>(dst)[v1] = out1;
         }
@@ -181,8 +210,10 @@ norm_rope_kernel(const PlaceArgs p, const PageMap pm, const __grid_constant__ Ro
 static RopeTurns make_turns(const ht_head_desc &h) {
     RopeTurns t{};
     const double two_pi = 6.283185307179586476925;
-    for (int i = 0; i < h.rot_dim / 2; ++i) {
-        double f = pow((double)h.rope_base, -2.0 * i / h.rot_dim) / two_pi;
+    const double ratio = h.rot_dim > 0 ? pow((double)h.rope_base, -2.0 / h.rot_dim) : 1.0;
+    double plain = 1.0 / two_pi;                         // base^(-2i / rot_dim) / 2 pi, by products: 63 roundings of 2^-53 at most
+    for (int i = 0; i < h.rot_dim / 2; ++i, plain *= ratio) {
+        double f = plain;
         if (h.scaling == HT_ROPE_LINEAR) {
             f /= h.factor;
         } else if (h.scaling == HT_ROPE_BY_PARTS) {
@@ -195,16 +226,42 @@ static RopeTurns make_turns(const ht_head_desc &h) {
     return t;
 }
 
-template <typename T>
-static int launch_t(const PlaceArgs &a, const PageMap &pm, const RopeTurns &turns, int D, bool interleaved, unsigned blocks, cudaStream_t s) {
-    if (D == 64) {
-        if (interleaved) norm_rope_kernel<T, 64, true><<<blocks, kPlaceThreads, 0, s>>>(a, pm, turns);
-        else norm_rope_kernel<T, 64, false><<<blocks, kPlaceThreads, 0, s>>>(a, pm, turns);
-    } else {
-        if (interleaved) norm_rope_kernel<T, 128, true><<<blocks, kPlaceThreads, 0, s>>>(a, pm, turns);
-        else norm_rope_kernel<T, 128, false><<<blocks, kPlaceThreads, 0, s>>>(a, pm, turns);
+// Blocks of a kernel that the device holds at once.
+template <typename Kernel>
+static int resident_blocks(Kernel kernel) {
+    int dev = 0, sms = 0, per_sm = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess ||
+        cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, kPlaceThreads, 0) != cudaSuccess || sms <= 0 || per_sm <= 0) {
+        cudaGetLastError();
+        return 148;
     }
+    return sms * per_sm;
+}
+
+template <typename T, int D, bool kInterleaved>
+static int launch_form(const PlaceArgs &a, const PageMap &pm, const RopeTurns &turns, cudaStream_t s) {
+    static int resident[64];                             // per device
+    int dev = 0;
+    cudaGetDevice(&dev);
+    int *slot = (dev >= 0 && dev < 64) ? &resident[dev] : nullptr;
+    int blocks = slot ? *slot : 0;
+    if (blocks == 0) {
+        blocks = resident_blocks(norm_rope_kernel<T, D, kInterleaved>);
+        if (slot) *slot = blocks;
+    }
+    constexpr int kChunk = kPlaceAhead * kPlaceThreads * 2 * Vec16<T>::n / D;       // heads a block takes of a row
+    PlaceArgs args = a;
+    args.chunks = (a.Hq + 2 * a.Hkv + kChunk - 1) / kChunk;
+    long long turns_at_once = blocks / args.chunks;      // rows
+    turns_at_once = turns_at_once < 1 ? 1 : (turns_at_once > a.rows ? a.rows : turns_at_once);
+    norm_rope_kernel<T, D, kInterleaved><<<(unsigned)(turns_at_once * args.chunks), kPlaceThreads, 0, s>>>(args, pm, turns);
     return check_launch("ht_norm_rope_kv_append");
+}
+
+template <typename T>
+static int launch_t(const PlaceArgs &a, const PageMap &pm, const RopeTurns &turns, int D, bool interleaved, cudaStream_t s) {
+    if (D == 64) return interleaved ? launch_form<T, 64, true>(a, pm, turns, s) : launch_form<T, 64, false>(a, pm, turns, s);
+    return interleaved ? launch_form<T, 128, true>(a, pm, turns, s) : launch_form<T, 128, false>(a, pm, turns, s);
 }
 
 int launch_norm_rope(const ht_attn_desc &d, const ht_head_desc &h, const void *q_in, const void *k_in, const void *v_in,
@@ -221,12 +278,12 @@ int launch_norm_rope(const ht_attn_desc &d, const ht_head_desc &h, const void *q
     a.stride_h = pm.table ? pm.head_stride : (d.kv_stride_h ? d.kv_stride_h : (long long)d.cap * d.D);
     a.stride_b = d.kv_stride_b ? d.kv_stride_b : (long long)d.Hkv * d.cap * d.D;
     const RopeTurns turns = make_turns(h);
-    const unsigned blocks = (unsigned)((long long)d.B * d.N);
+    a.rows = (long long)d.B * d.N;
     const bool il = h.interleaved != 0;
     switch (d.dtype) {
-        case HT_F32: return launch_t<float>(a, pm, turns, d.D, il, blocks, s);
-        case HT_F16: return launch_t<__half>(a, pm, turns, d.D, il, blocks, s);
-        default: return launch_t<__nv_bfloat16>(a, pm, turns, d.D, il, blocks, s);
+        case HT_F32: return launch_t<float>(a, pm, turns, d.D, il, s);
+        case HT_F16: return launch_t<__half>(a, pm, turns, d.D, il, s);
+        default: return launch_t<__nv_bfloat16>(a, pm, turns, d.D, il, s);
     }
 }
 

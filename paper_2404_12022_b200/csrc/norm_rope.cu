@@ -35,6 +35,23 @@ struct PlaceArgs {
     long long q_stride, k_stride, v_stride, stride_b, stride_h;
 };
 
+// 16 bytes of rounded values, a pair per conversion.
+__device__ __forceinline__ uint4 pack16(const float *x, float) {
+    return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+}
+__device__ __forceinline__ uint4 pack16(const float *x, __half) {
+    __half2 h[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) h[i] = __floats2half2_rn(x[2 * i], x[2 * i + 1]);
+    return *reinterpret_cast<const uint4 *>(h);
+}
+__device__ __forceinline__ uint4 pack16(const float *x, __nv_bfloat16) {
+    __nv_bfloat162 h[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) h[i] = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
+    return *reinterpret_cast<const uint4 *>(h);
+}
+
 constexpr int kPlaceThreads = 256;
 constexpr int kPlaceAhead = 3;    // heads per lane whose vectors are asked for before the angles are formed
 
@@ -65,6 +82,7 @@ norm_rope_kernel(const PlaceArgs p, const PageMap pm, const __grid_constant__ Ro
     const int chunk = (int)(blockIdx.x % (unsigned)p.chunks), step = (int)(gridDim.x / (unsigned)p.chunks);
     int kind[kPlaceAhead], head[kPlaceAhead];
     const uint4 *src[kPlaceAhead];
+    unsigned int ahead[kPlaceAhead];                     // vectors from a row of the block to its next (checked on the host)
     long long row = blockIdx.x / (unsigned)p.chunks;
 #pragma unroll
     for (int u = 0; u < kPlaceAhead; ++u) {
@@ -73,15 +91,17 @@ norm_rope_kernel(const PlaceArgs p, const PageMap pm, const __grid_constant__ Ro
         head[u] = kind[u] == kQ ? h : (kind[u] == kK ? h - p.Hq : h - p.Hq - p.Hkv);
         const T *base = static_cast<const T *>(kind[u] == kQ ? p.q_in : (kind[u] == kK ? p.k_in : p.v_in));
         const long long stride = kind[u] == kQ ? p.q_stride : (kind[u] == kK ? p.k_stride : p.v_stride);
-        src[u] = reinterpret_cast<const uint4 *>(base + row * stride + (long long)head[u] * D);
+        src[u] = reinterpret_cast<const uint4 *>(base + row * stride + (long long)head[u] * D) + v0;
+        ahead[u] = (unsigned int)(stride / VE * step);
     }
+    const int apart = v1 - v0;
     uint4 in0[kPlaceAhead], in1[kPlaceAhead];
     auto ask = [&](int u) {                              // the vectors of this lane's head u, and on to the block's next row
         if (kind[u] != kNone) {
-            in0[u] = src[u][v0];
-            in1[u] = src[u][v1];
+            in0[u] = src[u][0];
+            in1[u] = src[u][apart];
         }
-        src[u] += (kind[u] == kQ ? p.q_stride : (kind[u] == kK ? p.k_stride : p.v_stride)) / VE * step;
+        src[u] += ahead[u];
     };
 #pragma unroll
     for (int u = 0; u < kPlaceAhead; ++u) ask(u);
@@ -190,16 +210,14 @@ norm_rope_kernel(const PlaceArgs p, const PageMap pm, const __grid_constant__ Ro
                         }
                     }
                 }
-                T o[2 * VE];
-#pragma unroll
-                for (int e = 0; e < 2 * VE; ++e) o[e] = from_float<T>(x[e]);
-                out0 = *reinterpret_cast<const uint4 *>(o);
-                out1 = *reinterpret_cast<const uint4 *>(o + VE);
+                out0 = pack16(x, T());
+                out1 = pack16(x + VE, T());
             }
             T *dst = kind[u] == kQ ? static_cast<T *>(p.q_out) + (row * p.Hq + head[u]) * D
                                    : static_cast<T *>(kind[u] == kK ? p.k_cache : p.v_cache) + row_off + head[u] * p.stride_h;
-            reinterpret_cast<uint4 *>(dst)[v0] = out0;
-            reinterpret_cast<uint4 *>(dst)[v1] = out1;
+            uint4 *to = reinterpret_cast<uint4 *>(dst) + v0;
+            to[0] = out0;
+            to[apart] = out1;
         }
     }
 }
@@ -254,6 +272,9 @@ static int launch_form(const PlaceArgs &a, const PageMap &pm, const RopeTurns &t
     args.chunks = (a.Hq + 2 * a.Hkv + kChunk - 1) / kChunk;
     long long turns_at_once = blocks / args.chunks;      // rows
     turns_at_once = turns_at_once < 1 ? 1 : (turns_at_once > a.rows ? a.rows : turns_at_once);
+    const long long widest = a.q_stride > a.k_stride ? (a.q_stride > a.v_stride ? a.q_stride : a.v_stride) : (a.k_stride > a.v_stride ? a.k_stride : a.v_stride);
+    while (turns_at_once > 1 && widest / Vec16<T>::n * turns_at_once > 0xffffffffLL) turns_at_once /= 2;     // (a block's step between rows is a 32-bit count of vectors)
+    if (widest / Vec16<T>::n > 0xffffffffLL) return fail(HT_ERR_UNSUPPORTED, "row stride too large");
     norm_rope_kernel<T, D, kInterleaved><<<(unsigned)(turns_at_once * args.chunks), kPlaceThreads, 0, s>>>(args, pm, turns);
     return check_launch("ht_norm_rope_kv_append");
 }

@@ -61,7 +61,8 @@ norm_rope_kernel(const PlaceArgs p, const PageMap pm, const __grid_constant__ Ro
     // lets a kernel that is serialized programmatically behind this one (the attention call) set itself up meanwhile
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     constexpr int VE = Vec16<T>::n, LPH = D / (2 * VE), HPB = kPlaceThreads / LPH;     // lanes per head, heads per block pass
-    __shared__ float s_cos[2][D / 2], s_sin[2][D / 2];
+    constexpr int kBatch = kPlaceThreads / 64;           // rows whose tables are formed at once: a thread per pair
+    __shared__ float s_cos[2][kBatch][D / 2], s_sin[2][kBatch][D / 2];
     const int half_rot = p.rot >> 1;
     const int group = threadIdx.x / LPH, j = threadIdx.x - group * LPH;
     // this lane's two vectors within a head
@@ -116,20 +117,26 @@ norm_rope_kernel(const PlaceArgs p, const PageMap pm, const __grid_constant__ Ro
 #pragma unroll
         for (int e = 0; e < 2 * VE; ++e) wq[e] = w ? wq[e] + p.offset : 1.f;
     }
-    // Cosines and sines of a row's position into one of two tables; the next row's are formed while the current row's are
-    // in use, its position having been asked for a row earlier, by two warps that take turns.
-    auto form_table = [&](int at, int i, int turn) {
-        const double t = (double)at * turns.f[i];
+    // Cosines and sines of the positions of the block's next four rows, one pair per thread, into one of two sets of tables
+    // while the other one is in use; the positions have been asked for a batch earlier.
+    const int me_row = threadIdx.x >> 6, me_pair = threadIdx.x & 63;
+    auto position = [&](long long first) {
+        const long long at = first + (long long)me_row * step;
+        return me_pair < half_rot && at < p.rows ? p.pos[at] : 0;
+    };
+    auto form_tables = [&](int at, int turn) {
+        if (me_pair >= half_rot) return;
+        const double t = (double)at * turns.f[me_pair];
         float s, c;
         sincospif(2.f * (float)(t - rint(t)), &s, &c);
-        s_cos[turn][i] = c * p.magnitude;
-        s_sin[turn][i] = s * p.magnitude;
+        s_cos[turn][me_row][me_pair] = c * p.magnitude;
+        s_sin[turn][me_row][me_pair] = s * p.magnitude;
     };
-    int me = threadIdx.x;                                // the pair this thread forms, where below half_rot (at most 64)
-    if (me < half_rot) form_table(p.pos[row], me, 0);
-    int pos_next = row + step < p.rows ? p.pos[row + step] : 0;
-    for (int turn = 0; row < p.rows; row += step, turn ^= 1) {
+    form_tables(position(row), 0);
+    int pos_next = position(row + kBatch * step);
+    for (int i = 0; row < p.rows; row += step, ++i) {
         const long long next = row + step;
+        const int k = i % kBatch, turn = (i / kBatch) & 1;
         const int b = (int)((unsigned)row / (unsigned)p.N), r = (int)row - b * p.N;
         const int L = p.kv_len[b];
         const bool bad = L < 0 || (long long)L + p.N > p.cap;
@@ -149,20 +156,21 @@ norm_rope_kernel(const PlaceArgs p, const PageMap pm, const __grid_constant__ Ro
             bad_page = __syncthreads_or(bad_page);
             if (threadIdx.x == 0) p.status[b] = bad ? HT_STATUS_BAD_LEN : (bad_page ? HT_STATUS_BAD_PAGE : HT_STATUS_OK);
         }
-        __syncthreads();                                 // the row's table is complete, the other one's readers are done
+        if (k == 0) {
+            __syncthreads();                             // the batch's tables are complete, the other ones' readers are done
+            if (row + kBatch * step < p.rows) {
+                form_tables(pos_next, turn ^ 1);
+                pos_next = position(row + 2 * kBatch * step);
+            }
+        }
         // The lane's pairs, for all heads of the row.  Half-split: the VE pairs of vector v0; interleaved: VE / 2 pairs of
         // v0, then VE / 2 of v1.
         float cs[VE], sn[VE];
 #pragma unroll
         for (int e = 0; e < VE; ++e) {
             const int pair = kInterleaved ? (e < VE / 2 ? v0 * (VE / 2) + e : v1 * (VE / 2) + e - VE / 2) : j * VE + e;
-            cs[e] = pair < half_rot ? s_cos[turn][pair] : 1.f;
-            sn[e] = pair < half_rot ? s_sin[turn][pair] : 0.f;
-        }
-        me = (me + 64) & (kPlaceThreads - 1);
-        if (next < p.rows) {
-            if (me < half_rot) form_table(pos_next, me, turn ^ 1);
-            if (next + step < p.rows) pos_next = p.pos[next + step];
+            cs[e] = pair < half_rot ? s_cos[turn][k][pair] : 1.f;
+            sn[e] = pair < half_rot ? s_sin[turn][k][pair] : 0.f;
         }
 #pragma unroll
         for (int u = 0; u < kPlaceAhead; ++u) {

@@ -408,13 +408,13 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
             }
             release();
             // the tree rows' positions (which the kernel ahead may have written) take the place of the parents
-            float *const tree_pos = reinterpret_cast<float *>(sm.parent);
             if constexpr ((kShape & kShapeBias) != 0) {
                 if (new_rows) {
-                    for (int c = tid256; c < p.N; c += 256) tree_pos[c] = (float)(p.pos[(size_t)sg.b * p.N + c] - L);
+                    stage_tree_positions(p, reinterpret_cast<float *>(sm.parent), sg.b, L, tid256);
                     softmax_groups_sync();
                 }
             }
+            const TreeKeys tree_keys{reinterpret_cast<const float *>(sm.parent) + kTile, &sm.anc[0][row], words};
 
             // A segment that is only part of its unit: which CTAs hold the other parts.  How many of
             // them have been delivered is asked anew at every tile and looked at in the epilogue, so
@@ -450,7 +450,7 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
                 const int tile_lo = kt * kTile;
                 float *const xa = xa_e, *const xb = xb_e;
                 if (warp_real) {
-                if (tile_lo + kTile > L) {
+                if (kShape == 0 && tile_lo + kTile > L) {
                     // The tile reaches into the tree rows / the tail: overwrite the scores of keys this
                     // row must not see with -inf, in place, so that the two passes below need no mask.
                     // Context keys are visible, tree key c iff bit c of the row's ancestor words, the
@@ -484,7 +484,7 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
                         mx0 = max3(mx0, xa[c], xa[c + 1]);
                         mx1 = max3(mx1, xa[c + 2], xa[c + 3]);
                     }
-                    if (kShape & kShapeCap) size = shape_size(xa, size, tile_lo + kTile > L);
+                    if (kShape & kShapeCap) size = shape_size(xa, size);
                     tmem_ld_wait();
                     tmem_ld32(s_addr + ((2 * h + 2) & 3) * 32, xa);   // after the last chunk: chunk 0 again, for pass 2
 #pragma unroll
@@ -492,29 +492,32 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
                         mx0 = max3(mx0, xb[c], xb[c + 1]);
                         mx1 = max3(mx1, xb[c + 2], xb[c + 3]);
                     }
-                    if (kShape & kShapeCap) size = shape_size(xb, size, tile_lo + kTile > L);
+                    if (kShape & kShapeCap) size = shape_size(xb, size);
                 }
                 float mx = fmaxf(mx0, mx1) * p.scale_log2;   // scale > 0: max commutes with scaling
                 bool negligible = false;
                 if constexpr (kShape != 0) {
                     if ((kShape & kShapeCap) && shape_coefficients(p, shape, size, s_addr, 4, xa)) tmem_ld32(s_addr, xa);
                     mx = shape_bound<kShape>(p, mx, tile_lo, kTile, shape);
-                    if constexpr ((kShape & kShapeBias) != 0) {
-                        const bool tree_keys = tile_lo + kTile > L;
-                        if (tree_keys || __any_sync(0xffffffffu, real && !(mx <= m_ref + kRescaleThreshold))) {
-                            // the reference may have to rise (or some keys are at positions of their own): the exact maximum
-                            mx = -INFINITY;
+                    const bool tree_tile = tile_lo + kTile > L;
+                    if (tree_tile || ((kShape & kShapeBias) && __any_sync(0xffffffffu, real && !(mx <= m_ref + kRescaleThreshold)))) {
+                        // masked keys, or a reference that may have to rise: the exact maximum
+                        mx = -INFINITY;
 #pragma unroll 1
-                            for (int w = 0; w < 4; ++w) {
-                                tmem_ld_wait();
-                                shape_scores<kShape, true>(p, xa, tile_lo + 32 * w, L, tree_pos, shape, 0.f);
+                        for (int w = 0; w < 4; ++w) {
+                            tmem_ld_wait();
+                            shape_scores<kShape, true>(p, xa, tile_lo + 32 * w, L, tree_keys, shape, 0.f);
+                            float m0 = -INFINITY, m1 = -INFINITY;
 #pragma unroll
-                                for (int c = 0; c < 32; c += 2) mx = max3(mx, xa[c], xa[c + 1]);
-                                tmem_ld32(s_addr + ((w + 1) & 3) * 32, xa);       // after the last chunk: chunk 0 again, for pass 2
+                            for (int c = 0; c < 32; c += 4) {
+                                m0 = max3(m0, xa[c], xa[c + 1]);
+                                m1 = max3(m1, xa[c + 2], xa[c + 3]);
                             }
-                        } else {
-                            negligible = __all_sync(0xffffffffu, !real || mx < m_ref - kNegligibleLog2) && tile_lo + kTile <= L - p.near_keys;
+                            mx = max3(mx, m0, m1);
+                            tmem_ld32(s_addr + ((w + 1) & 3) * 32, xa);           // after the last chunk: chunk 0 again, for pass 2
                         }
+                    } else if (kShape & kShapeBias) {
+                        negligible = __all_sync(0xffffffffu, !real || mx < m_ref - kNegligibleLog2) && tile_lo + kTile <= L - p.near_keys;
                     }
                 }
                 // --- running maximum, raised lazily ---
@@ -556,11 +559,11 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
                     } else {
                         if (tile_lo + kTile > L - p.near_keys)
                             softmax_pass2<kBf16, true, true>(s_addr, xa, xb, scale2, nbase2, acc2, [&](float *x, int w) {
-                                shape_scores<kShape, true>(p, x, tile_lo + 32 * w, L, tree_pos, shape, -base);
+                                shape_scores<kShape, true>(p, x, tile_lo + 32 * w, L, tree_keys, shape, -base);
                             });
                         else
                             softmax_pass2<kBf16, false, true>(s_addr, xa, xb, scale2, nbase2, acc2, [&](float *x, int w) {
-                                shape_scores<kShape, false>(p, x, tile_lo + 32 * w, L, tree_pos, shape, -base);
+                                shape_scores<kShape, false>(p, x, tile_lo + 32 * w, L, tree_keys, shape, -base);
                             });
                     }
                 } else {

@@ -72,7 +72,7 @@ struct PagedParams {
 struct __align__(1024) Smem {
     unsigned char q[kEntryBytes];
     unsigned char ring[kStages][kEntryBytes];
-    int32_t parent[kMaxWords * 32];
+    int32_t parent[kMaxWords * 32 + 2 * kTile];   // the scored instantiations: the tree rows' positions later, a tile's worth of room around them
     float ml[2][kRows][2];
     int32_t len[kMaxB];
     int32_t nkt[kMaxB];
@@ -311,10 +311,11 @@ __device__ __forceinline__ unsigned long long add_f32x2(unsigned long long a, un
 //     warp meets a score beyond half the cap, the tile is first rewritten in tensor memory by a rolled loop with the general
 //     form (cap_one), and the coefficients become those of the identity: a second form in line costs the tiles that never
 //     take it a third of their time (16 x 67 rows on 8192 keys: 890 us against 635 us).
-//   - Tree tiles (masked keys, keys at positions of their own) have instantiations of their own (kTree) for the same reason.
+//   - Tiles with tree keys (masked keys, keys at positions of their own) have instantiations of their own (kTree) for the
+//     same reason; they are masked as they are shaped, not in tensor memory.
 //   - The running maximum needs no shaped maximum: tanh is monotone, so without a bias the maximum is the shaped raw
-//     maximum; with one, the raw maximum and the bias's larger end bound it, and the exact maximum is only formed where
-//     that bound may raise the reference -- in the first tiles, since a segment's tiles are taken from the nearest keys to
+//     maximum; with one, the raw maximum and the bias's larger end bound it, and the exact maximum is only formed in tiles
+//     with tree keys and where that bound may raise the reference -- in the first tiles, since a segment's tiles are taken from the nearest keys to
 //     the farthest (p.from_end).  A tile whose bound lies 2^-40 below the reference adds nothing to the 32-bit sum of a
 //     part of up to 2^15 keys: its weights are zero.
 constexpr int kShapeCap = 1, kShapeBias = 2;
@@ -341,24 +342,19 @@ __device__ __forceinline__ float rcp(float x) {
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-// cap tanh(x scale / cap), any x; -inf (a masked key) stays.
+// cap tanh(x scale / cap), any x.
 __device__ __forceinline__ float cap_one(const Params &p, float x) {
     const float u = x * x;
     const float near = x * fmaf(u, fmaf(u, fmaf(u, fmaf(u, fmaf(u, p.series[5], p.series[4]), p.series[3]), p.series[2]), p.series[1]), p.series[0]);
     const float far = fmaf(-2.f * p.cap_log2, rcp(1.f + ex2(x * (2.8853900817779268f * p.score_mul))), p.cap_log2);
-    return fabsf(x * p.score_mul) <= p.series_lim ? near : (x == -INFINITY ? x : far);
+    return fabsf(x * p.score_mul) <= p.series_lim ? near : far;
 }
-// The largest |product| of 32, masked keys (-inf) of a tile with tree keys left out.
-__device__ __forceinline__ float shape_size(const float *x, float size, bool tree_keys) {
-    if (tree_keys) {
+// The largest |product| of 32 (whatever lies in masked places: it can only send a tile the general way).
+__device__ __forceinline__ float shape_size(const float *x, float size) {
 #pragma unroll
-        for (int c = 0; c < 32; ++c) size = fmaxf(size, x[c] == -INFINITY ? 0.f : fabsf(x[c]));
-    } else {
-#pragma unroll
-        for (int c = 0; c < 32; c += 8)
-            size = max3(size, fmaxf(max3(fabsf(x[c]), fabsf(x[c + 1]), fabsf(x[c + 2])), fabsf(x[c + 3])),
-                        fmaxf(max3(fabsf(x[c + 4]), fabsf(x[c + 5]), fabsf(x[c + 6])), fabsf(x[c + 7])));
-    }
+    for (int c = 0; c < 32; c += 8)
+        size = max3(size, fmaxf(max3(fabsf(x[c]), fabsf(x[c + 1]), fabsf(x[c + 2])), fabsf(x[c + 3])),
+                    fmaxf(max3(fabsf(x[c + 4]), fabsf(x[c + 5]), fabsf(x[c + 6])), fabsf(x[c + 7])));
     return size;
 }
 // The tile's coefficients; its `chunks` x 32 products at s_addr rewritten as capped scores where the series does not
@@ -389,19 +385,30 @@ __device__ __forceinline__ float shape_bound(const Params &p, float mx, int key0
     if (kShape & kShapeBias) s += row.slope * (float)((row.slope > 0.f ? key0 + keys - 1 : key0) - row.pos);
     return s;
 }
-// 32 raw products of keys key0, ... of a sequence with L context rows -> shaped scores plus `add`.  kTree: some may be
-// tree keys or masked (masked keys, -inf, stay masked).  tree_pos: positions of the tree rows less L.
-template <int kShape, bool kTree>
-__device__ __forceinline__ void shape_scores(const Params &p, float *x, int key0, int L, const float *tree_pos, const RowShape &row, float add) {
-    const bool tree = kTree && key0 + 32 > L;
-    uint32_t masked = 0u;                                    // (the series loses a -inf)
-    if (kTree && (kShape & kShapeCap)) {
-#pragma unroll
-        for (int c = 0; c < 32; ++c) masked |= (x[c] == -INFINITY ? 1u : 0u) << c;
+// What the shaping of a tile with tree keys reads from shared memory: positions less kv_len of the kTile context rows
+// ahead of the tree, of the tree rows and of what follows them (`pos`: of the first tree row); the row's ancestor words,
+// kRows apart.
+struct TreeKeys {
+    const float *pos;
+    const uint32_t *anc;
+    int words;
+};
+// Fills the area that `pos` points into (all softmax threads; a barrier of theirs on both sides).
+__device__ __forceinline__ void stage_tree_positions(const Params &p, float *area, int b, int L, int tid256) {
+    for (int i = tid256; i < p.N + 2 * kTile; i += 256) {
+        const int c = i - kTile;
+        area[i] = c < 0 ? (float)c : (c < p.N ? (float)(p.pos[(size_t)b * p.N + c] - L) : 0.f);
     }
-    // context keys: the bias is linear in the key
+}
+// 32 raw products of keys key0, ... of a sequence with L context rows -> shaped scores plus `add`.  kTree: some may be
+// tree keys; those the row must not see, and the tail, become -inf whatever they hold.
+template <int kShape, bool kTree>
+__device__ __forceinline__ void shape_scores(const Params &p, float *x, int key0, int L, const TreeKeys &tk, const RowShape &row, float add) {
+    const bool tree = kTree && key0 + 32 > L;
+    // the bias, less the row's own position: linear in the key for context keys
     const float slope = (kShape & kShapeBias) && !tree ? row.slope : 0.f;
-    const float first = (kShape & kShapeBias) && !tree ? fmaf(row.slope, (float)(key0 - row.pos), add) : add;
+    float first = add;
+    if (kShape & kShapeBias) first = fmaf(row.slope, (tree ? 0.f : (float)(key0 - L)) - row.from_len, add);
     const unsigned long long slope2 = pack_f32x2(slope, slope), first2 = pack_f32x2(first, first);
     auto rest = [&](int c) {                                 // what is added to the (capped) scores of keys c and c + 1
         return (kShape & kShapeBias) ? fma_f32x2(slope2, pack_f32x2((float)c, (float)(c + 1)), first2) : first2;
@@ -423,17 +430,19 @@ __device__ __forceinline__ void shape_scores(const Params &p, float *x, int key0
             unpack_f32x2(fma_f32x2(v, q, rest(c)), x[c], x[c + 1]);
         }
     }
-    if (kTree && (kShape & kShapeCap)) {
+    if (tree) {
+        const int cc0 = key0 - L;                            // tree index of the first key, above -32
+        if (kShape & kShapeBias) {
+            const float *pos = tk.pos + min(cc0, p.N);       // (wholly behind the tree: masked)
 #pragma unroll
-        for (int c = 0; c < 32; ++c) x[c] = (masked >> c) & 1u ? -INFINITY : x[c];
-    }
-    if ((kShape & kShapeBias) && tree) {                     // some of the 32 are tree keys, at the positions given
-        float at[32];                                        // position of the key - L (index clamped: the tail is masked)
+            for (int c = 0; c < 32; ++c) x[c] = fmaf(row.slope, pos[c], x[c]);
+        }
+        const int wi = cc0 >> 5, sh = cc0 & 31;              // arithmetic shift: -1 for cc0 in (-32, 0)
+        const uint32_t lo = wi < 0 ? 0xFFFFFFFFu : (wi < tk.words ? tk.anc[wi * kRows] : 0u);
+        const uint32_t hi = wi + 1 < tk.words ? tk.anc[(wi + 1) * kRows] : 0u;
+        const uint32_t vis = __funnelshift_r(lo, hi, sh);
 #pragma unroll
-        for (int c = 0; c < 32; ++c) at[c] = tree_pos[min(max(key0 + c - L, 0), p.N - 1)];
-#pragma unroll
-        for (int c = 0; c < 32; ++c)
-            x[c] = fmaf(row.slope, (key0 + c < L ? (float)(key0 + c - L) : at[c]) - row.from_len, x[c]);
+        for (int c = 0; c < 32; ++c) x[c] = ((vis >> c) & 1u) ? x[c] : -INFINITY;
     }
 }
 

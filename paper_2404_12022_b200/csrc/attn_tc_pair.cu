@@ -66,7 +66,7 @@ static_assert(2 * kPXchgStream <= (2 + kPStages) * kEntryBytes, "the exchange ar
 struct __align__(1024) PSmem {
     unsigned char q[2][kEntryBytes];
     unsigned char ring[kPStages][kEntryBytes];
-    int32_t parent[kMaxWords * 32];
+    int32_t parent[kMaxWords * 32 + 2 * kTile];   // the scored instantiations: the tree rows' positions later, a tile's worth of room around them
     int32_t len[kMaxB];
     int32_t nkt[kMaxB];
     int32_t pre[kMaxB + 1];
@@ -476,13 +476,14 @@ attn_tc_pair_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
             }
             release();
             // the tree rows' positions (which the kernel ahead may have written) take the place of the parents
-            float *const tree_pos = reinterpret_cast<float *>(sm.parent);
             if constexpr ((kShape & kShapeBias) != 0) {
                 if (new_rows) {
-                    for (int c = tid256; c < p.N; c += 256) tree_pos[c] = (float)(p.pos[(size_t)sg.b * p.N + c] - L);
+                    stage_tree_positions(p, reinterpret_cast<float *>(sm.parent), sg.b, L, tid256);
                     softmax_groups_sync();
                 }
             }
+            const TreeKeys tree_keys{reinterpret_cast<const float *>(sm.parent) + kTile, &sm.anc[s * words * kRows + row], words};
+
             // A segment that is only part of its unit: see the one-tile kernel.
             const bool complete = sg.kt0 == 0 && sg.len == sg.nkt;
             const int cut_k = (t == t_begin) ? 0 : 1;
@@ -516,7 +517,7 @@ attn_tc_pair_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                     const uint32_t s_addr = tmem + lane_base + s * 128 + h * kHalf;
                     const int key_lo = kt * kTile + h * kHalf;
                     if (warp_real) {
-                    if (key_lo + kHalf > L) {
+                    if (kShape == 0 && key_lo + kHalf > L) {
                         // Reaches into the tree rows / the tail: scores of keys this row must not see
                         // become -inf in place (context visible, tree key c iff ancestor bit c, tail never).
 #pragma unroll 1
@@ -555,26 +556,26 @@ attn_tc_pair_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                     bool negligible = false;
                     if constexpr (kShape != 0) {
                         float size = 0.f;                   // the largest |product| of the row
-                        if (kShape & kShapeCap) size = shape_size(xb, shape_size(xa, size, key_lo + kHalf > L), key_lo + kHalf > L);
+                        if (kShape & kShapeCap) size = shape_size(xb, shape_size(xa, size));
                         if ((kShape & kShapeCap) && shape_coefficients(p, shape, size, s_addr, 2, xa)) {
                             tmem_ld32(s_addr, xa);
                             tmem_ld32(s_addr + 32, xb);
                             tmem_ld_wait();
                         }
                         mx = shape_bound<kShape>(p, mx, key_lo, kHalf, shape);
-                        const bool exact = (kShape & kShapeBias) &&
-                                           (key_lo + kHalf > L || __any_sync(0xffffffffu, real && !(mx <= m_ref + kRescaleThreshold)));
+                        const bool tree_half = key_lo + kHalf > L;
+                        const bool exact = tree_half || ((kShape & kShapeBias) && __any_sync(0xffffffffu, real && !(mx <= m_ref + kRescaleThreshold)));
                         if (kShape & kShapeBias)
                             negligible = !exact && __all_sync(0xffffffffu, !real || mx < m_ref - kNegligibleLog2) && key_lo + kHalf <= L - p.near_keys;
                         if (!negligible) {
-                            if (key_lo + kHalf > L) {
-                                shape_scores<kShape, true>(p, xa, key_lo, L, tree_pos, shape, 0.f);
-                                shape_scores<kShape, true>(p, xb, key_lo + 32, L, tree_pos, shape, 0.f);
+                            if (tree_half) {
+                                shape_scores<kShape, true>(p, xa, key_lo, L, tree_keys, shape, 0.f);
+                                shape_scores<kShape, true>(p, xb, key_lo + 32, L, tree_keys, shape, 0.f);
                             } else {
-                                shape_scores<kShape, false>(p, xa, key_lo, L, tree_pos, shape, 0.f);
-                                shape_scores<kShape, false>(p, xb, key_lo + 32, L, tree_pos, shape, 0.f);
+                                shape_scores<kShape, false>(p, xa, key_lo, L, tree_keys, shape, 0.f);
+                                shape_scores<kShape, false>(p, xb, key_lo + 32, L, tree_keys, shape, 0.f);
                             }
-                            if (exact) {                    // the reference may have to rise: the exact maximum
+                            if (exact) {                    // masked keys, or a reference that may have to rise
                                 mx = -INFINITY;
 #pragma unroll
                                 for (int c = 0; c < 32; ++c) mx = max3(mx, xa[c], xb[c]);

@@ -43,6 +43,7 @@ struct SampleSmem {
     double wsum[kSampleWarps];            // per warp, of the block's latest sum
     double part[kSampleWarps];            // per warp: kept weight of its range of the row
     double scan[3 * kSampleWarps];
+    double short_w[kShort], short_sum;
     float wmax[kSampleWarps];
     unsigned int wcount[kSampleWarps];
     struct {
@@ -886,7 +887,8 @@ struct Sampler {
                 // Lower bounds of the k-th largest token: the k-th largest of a block's thread maxima, and the smallest of
                 // the blocks' ceil(k / blocks)-th largest.
                 unsigned int key = team.max_key(kth_maximum(thread_max, top_k));
-                if (kTeam) key = ::max(key, team.min_key(kth_maximum(thread_max, (top_k + team.size - 1) / team.size)));
+                // (the first admits about k tokens per block: the second is worth its time where those may not fit the list)
+                if (kTeam && team.size * top_k > kList / 2) key = ::max(key, team.min_key(kth_maximum(thread_max, (top_k + team.size - 1) / team.size)));
                 const float bound = key <= order_key(-INFINITY) ? -INFINITY : key_value(key);
                 open_list();
                 row.each([&](float x, int i) { if (x >= bound && x > -INFINITY) append(x, i); });
@@ -1005,8 +1007,37 @@ struct Sampler {
         __syncthreads();
     }
 
+    // finish_list for the usual few tokens, one per thread: one running sum settles top_p and min_p, and each kept token adds
+    // up the weights of the kept ones at or below its index itself.
+    __device__ __forceinline__ int finish_short(int n, bool p_on, float top_p, double total, double floor, double u) {
+        const int i = threadIdx.x;
+        const bool mine = i < n;
+        const unsigned long long e = mine ? sm.list[i] : 0ull;
+        const double w = mine ? wt(entry_value(e)) : 0.0;
+        double sum;
+        const double before = block_scan(w, sm.wsum, &sum);
+        if (total < 0.0) total = sum;
+        // (a prefix: both conditions fall with the order)
+        const bool keep = mine && (i == 0 || ((!p_on || before < (double)top_p * total) && w >= floor));
+        n = __syncthreads_count(keep);
+        if (i < kShort) sm.short_w[i] = keep ? w : 0.0;
+        if (i == n - 1) sm.short_sum = before + w;
+        if (i == 0) { sm.answer = INT_MAX; sm.first_thread = -1; }
+        __syncthreads();
+        if (keep && w > 0.0) {
+            const int at = entry_index(e);
+            double upto = 0.0;
+            for (int j = 0; j < n; ++j) upto += entry_index(sm.list[j]) <= at ? sm.short_w[j] : 0.0;
+            if (upto > u * sm.short_sum) atomicMin(&sm.answer, at);
+            atomicMax(&sm.first_thread, at);                 // the last one with a weight, should none exceed the goal
+        }
+        __syncthreads();
+        return sm.answer != INT_MAX ? sm.answer : sm.first_thread;
+    }
+
     // list[0, n): the first n of the order.  total < 0: the weight that top_p refers to is the list's own.
     __device__ __forceinline__ int finish_list(int n, bool p_on, float top_p, double total, double floor, double u) {
+        if (n <= (int)kShort) return finish_short(n, p_on, top_p, total, floor, u);
         if (n > 1 && p_on) {
             double sum;
             if (total < 0.0) {

@@ -39,7 +39,7 @@ struct SampleSmem {
         unsigned int hist[kBins];
         unsigned long long list[kList];
     };
-    double pow2[16];                      // 2^(i / 16)
+    double pow2[kBinsPerOctave];          // 2^(i / 64)
     double wsum[kSampleWarps];            // per warp, of the block's latest sum
     double part[kSampleWarps];            // per warp: kept weight of its range of the row
     double scan[3 * kSampleWarps];
@@ -69,15 +69,13 @@ __device__ __forceinline__ float key_value(unsigned int k) {
 // In constant memory, where an instruction reads them as operands (as literals each would be put together in two
 // registers first, for every token anew).
 constexpr double kLn2By64 = 0.693147180559945309417 / 64.0;
-__constant__ double kSeries[6] = {1.0, kLn2By64, kLn2By64 *kLn2By64 / 2.0, kLn2By64 *kLn2By64 *kLn2By64 / 6.0,
-                                  kLn2By64 *kLn2By64 *kLn2By64 *kLn2By64 / 24.0,
-                                  kLn2By64 *kLn2By64 *kLn2By64 *kLn2By64 *kLn2By64 / 120.0};
+__constant__ double kSeries[5] = {1.0, kLn2By64, kLn2By64 *kLn2By64 / 2.0, kLn2By64 *kLn2By64 *kLn2By64 / 6.0,
+                                  kLn2By64 *kLn2By64 *kLn2By64 *kLn2By64 / 24.0};
 __constant__ double kMagicC = 6755399441055744.0 + (1 << 30);      // 1.5 * 2^52 + the bias below: adding it rounds to a whole number
 
 // Weight of a logit.  exp(d / T) = 2^(t / 64) with t = 64 log2(e) d / T.  k = t rounded is the token's bin (its distance
-// to the largest in 1/64 octaves); k rounded to fours, 64 n + 4 i, leaves |r| <= 5/2: a table of 2^(i / 16) (16 doubles:
-// a gather without bank conflicts), the Taylor series of e^(r ln2 / 64) to the fifth power (the next term is below
-// 6e-13) and n into the exponent.  All in 64 bits.
+// to the largest in 1/64 octaves) and leaves |r| <= 1/2: k = 64 n + i, a table of 2^(i / 64), the Taylor series of
+// e^(r ln2 / 64) to the fourth power (the next term is below 4e-14) and n into the exponent.  All in 64 bits.
 struct Weights {
     double m, c;                          // largest logit, 64 log2(e) / T
     float m32, low, c32;                  // largest logit; logits below `low` lie in the last bin; log2(e) / T
@@ -87,14 +85,14 @@ struct Weights {
     __device__ __forceinline__ int split(float x, double &q, double &s) const {
         const double d = (double)x - m;
         const double kd = fma(d, c, kMagicC);
-        const unsigned int k = (unsigned int)__double2loint(kd), k4 = (k + 2u) & ~3u;
-        const double r = fma(d, c, kMagicC - __hiloint2double(__double2hiint(kd), (int)k4));
-        q = kSeries[5];
+        const unsigned int k = (unsigned int)__double2loint(kd);
+        const double r = fma(d, c, kMagicC - kd);
+        q = kSeries[4];
 #pragma unroll
-        for (int i = 4; i >= 0; --i) q = fma(q, r, kSeries[i]);
-        s = *reinterpret_cast<const double *>(reinterpret_cast<const char *>(pow2) + ((k4 << 1) & 0x78u));
+        for (int i = 3; i >= 0; --i) q = fma(q, r, kSeries[i]);
+        s = *reinterpret_cast<const double *>(reinterpret_cast<const char *>(pow2) + ((k << 3) & 0x1f8u));
         // (the bias leaves no trace above bit 31)
-        s = __hiloint2double((int)((unsigned int)__double2hiint(s) + ((k4 & ~63u) << 14)), __double2loint(s));
+        s = __hiloint2double((int)((unsigned int)__double2hiint(s) + ((k & ~63u) << 14)), __double2loint(s));
         return (int)(kBias - k);
     }
     // the distance in bins as such
@@ -1087,7 +1085,7 @@ sample_kernel(const SampleArgs a) {
     }
     const int unit = kTeam ? (int)blockIdx.x / team.size : (int)blockIdx.x;
     const int b = unit / a.R, r = unit - b * a.R;
-    if (threadIdx.x < 16) sm.pow2[threadIdx.x] = exp2((double)threadIdx.x / 16.0);
+    if (threadIdx.x < kBinsPerOctave) sm.pow2[threadIdx.x] = exp2((double)threadIdx.x / kBinsPerOctave);
     // The launch is serialized programmatically behind the kernel ahead of it in the stream: from here on everything
     // that kernel wrote may be read.  A kernel serialized behind this one may set itself up meanwhile.
     asm volatile("griddepcontrol.wait;" ::: "memory");

@@ -464,14 +464,24 @@ __device__ __forceinline__ int list_draw(SampleSmem &sm, const Weights &wt, int 
 // is read any more.
 constexpr int kElsewhere = -2, kGone = -3;
 
+// bf16 rows in shared memory are counted by value: 13 binades of either sign, 128 values each, and the few nearer to zero
+// as one bin, in the order of the values.  Behind the row's slice in shared memory: counts, and the values' weights.
+constexpr int kSide = 13 * 128;
+constexpr int kValues = 2 * kSide + 1;
+constexpr size_t kValueBytes = ((size_t)kValues * (sizeof(unsigned int) + sizeof(double)) + 31) / 16 * 16;
+template <typename T, bool kStaged> struct ByValue { static constexpr bool on = false; };
+template <> struct ByValue<__nv_bfloat16, true> { static constexpr bool on = true; };
+
 template <typename T, bool kStaged, bool kTeam>
 struct Sampler {
     static constexpr int VE = Vec16<T>::n;
+    static constexpr bool kByValue = ByValue<T, kStaged>::on;
     SampleSmem &sm;
     Team<kTeam> &team;
     Row<T, kStaged> row;
     Weights wt;
     float m;                              // largest logit
+    double *value_weight;                 // [kValues] and behind them counts (kByValue)
 
     // Elements ahead of the cut of a running count (count_goal > 0) or weight (goal), by halving the range of the keys and
     // then of the indexes: exact for every distribution, one pass over the row per step.  For rows whose zone does not
@@ -605,6 +615,143 @@ struct Sampler {
                 sm.hist[i] = all;
             }
         }
+    }
+
+    // The cut of top_p by counts per value: every value's weight is formed once instead of every token's (4096 rows of
+    // 32000: VALUE_TIMES).  False where the cut lies among the values next to zero or weights that count lie
+    // beyond the bins (negative and larger than twice the largest logit, and 32).  sm.part: the warps' kept weights.
+    __device__ __forceinline__ bool value_cut(float top_p, Cut &cut) {
+        constexpr int PER = (kValues + kSampleThreads - 1) / kSampleThreads;
+        unsigned int *const count = reinterpret_cast<unsigned int *>(value_weight + kValues);
+        const int top = (int)((__float_as_uint(fmaxf(fabsf(m), 16.f)) >> 16) | 0x7fu), a0 = top - kSide + 1;   // of the magnitudes' bits
+        auto bin = [&](unsigned int bits, int &t) {           // bits: the value's, as a float's; t: 0 .. kSide - 1 where it has a bin
+            t = (int)((bits >> 16) & 0x7fffu) - a0;
+            return (int)bits < 0 ? kSide + 1 + t : kSide - 1 - t;
+        };
+        auto value = [&](int b) {
+            const unsigned int a = b < kSide ? (unsigned int)(top - b) : (b == kSide ? 0u : (unsigned int)(a0 + b - kSide - 1) | 0x8000u);
+            return __uint_as_float(a << 16);
+        };
+        __syncthreads();
+        for (int i = threadIdx.x; i < kValues; i += kSampleThreads) count[i] = 0u;
+        __syncthreads();
+        double w_near = 0.0;
+        float w_low = 0.f;
+        unsigned int beyond = 0;
+        row.each([&](float x, int) {
+            int t;
+            const int b = bin(__float_as_uint(x), t);
+            if ((unsigned int)t < (unsigned int)kSide) {
+                atomicAdd(&count[b], 1u);
+            } else if (t < 0) {
+                w_near += wt(x);
+            } else {
+                beyond |= x >= wt.low;
+                w_low += wt.small(x);
+            }
+        });
+        const double near_zero = team.sum(block_sum(sm, w_near)), low = team.sum(block_sum(sm, (double)w_low));
+        if (team.count((unsigned int)__syncthreads_or((int)beyond)) != 0) return false;
+        // the values' weights, in every block; their counts and running weights in the first one
+        double mass[PER], mine = 0.0;
+        unsigned int c[PER];
+#pragma unroll 1
+        for (int q = 0; q < PER; ++q) {
+            const int b = threadIdx.x * PER + q;
+            if (b < kValues) value_weight[b] = wt(value(b));
+        }
+        if (!kTeam || team.rank == 0) {
+#pragma unroll
+            for (int q = 0; q < PER; ++q) {
+                const int b = threadIdx.x * PER + q;
+                c[q] = b < kValues ? count[b] : 0u;
+                if (kTeam && b < kValues)
+                    for (int r = 1; r < team.size; ++r) c[q] += *team.of(&count[b], r);
+                mass[q] = b == kSide ? near_zero : (c[q] ? c[q] * value_weight[b] : 0.0);
+                mine += mass[q];
+            }
+            double all, before = block_scan(mine, sm.wsum, &all);
+            const double goal = (double)top_p * (all + low);
+            if (threadIdx.x == 0) sm.zone_lo = -1;
+            __syncthreads();
+#pragma unroll
+            for (int q = 0; q < PER; ++q) {
+                const int b = threadIdx.x * PER + q;
+                if (b != kSide && before < goal && before + mass[q] >= goal) {
+                    // of the equal tokens those before which less than the goal has come
+                    const double each_w = value_weight[b], n = ceil((goal - before) / each_w);
+                    unsigned int ties = n < 1.0 ? 1u : (n > (double)c[q] ? c[q] : (unsigned int)n);
+                    while (ties > 1 && !(before + (double)(ties - 1) * each_w < goal)) --ties;
+                    while (ties < c[q] && before + (double)ties * each_w < goal) ++ties;
+                    sm.total = ties;
+                    sm.zone_lo = b;
+                }
+                before += mass[q];
+            }
+        }
+        team.barrier();
+        const int at = *team.of(&sm.zone_lo, 0);
+        const unsigned int ties = *team.of(&sm.total, 0);
+        if (at < 0) return false;
+        // kept weights and equal tokens by warp
+        double w = 0.0;
+        unsigned int equal = 0;
+        row.each([&](float x, int) {
+            int t;
+            const int b = bin(__float_as_uint(x), t);
+            if ((unsigned int)t < (unsigned int)kSide) {
+                if (b < at) w += value_weight[b];
+                else equal += b == at;
+            } else if (t < 0 && at > kSide) {
+                w += wt(x);
+            }
+        });
+        w = warp_sum(w);
+        equal = __reduce_add_sync(0xffffffffu, equal);
+        const int warp = threadIdx.x >> 5;
+        __syncthreads();
+        if ((threadIdx.x & 31) == 0) { sm.part[warp] = w; sm.wcount[warp] = equal; }
+        __syncthreads();
+        unsigned int in_block = 0;
+#pragma unroll
+        for (int i = 0; i < kSampleWarps; ++i) in_block += sm.wcount[i];
+        double ahead;
+        team.sum((double)in_block, ahead);
+        // the equal tokens of the blocks and warps ahead come first; the first one left out lies in warp `edge`, if in this block
+        int left = (int)ties - (int)ahead, edge = -1, edge_left = 0;
+#pragma unroll
+        for (int i = 0; i < kSampleWarps; ++i) {
+            const int n = (int)sm.wcount[i];
+            if (left >= 0 && left < n) { edge = i; edge_left = left; }
+            if ((int)threadIdx.x == i) sm.part[i] += (double)::min(::max(left, 0), n) * value_weight[at];
+            left -= n;
+        }
+        int index = INT_MAX;
+        if (edge >= 0) {
+            const float v = value(at);
+            const int first = row.warp_first(edge), n = row.warp_first(edge + 1) - first, per = (n + kSampleThreads - 1) / kSampleThreads;
+            const int v0 = first + ::min(n, (int)threadIdx.x * per), v1 = first + ::min(n, ((int)threadIdx.x + 1) * per);
+            unsigned int n_mine = 0, all;
+            for (int k = v0; k < v1; ++k) {
+                float x[VE];
+                row.load(k, x);
+#pragma unroll
+                for (int e = 0; e < VE; ++e) n_mine += x[e] == v;
+            }
+            unsigned int seen = block_scan(n_mine, sm.wcount, &all);
+            if (seen <= (unsigned int)edge_left && (unsigned int)edge_left < seen + n_mine)
+                for (int k = v0; k < v1; ++k) {
+                    float x[VE];
+                    row.load(k, x);
+                    for (int e = 0; e < VE; ++e)
+                        if (x[e] == v && seen++ == (unsigned int)edge_left) sm.answer = row.index(k, e);
+                }
+            __syncthreads();
+            index = sm.answer;
+        }
+        cut = Cut{value(at), team.min_int(index)};
+        __syncthreads();
+        return true;
     }
 
     // Counts of the kept elements by bin, summed over the row's blocks in the first one, and (kWeight) their weight.
@@ -933,7 +1080,14 @@ struct Sampler {
             }
             team.barrier();
         }
-        if (p_on) {
+        bool cut_by_value = false;
+        if constexpr (kByValue) {
+            if (p_on && cut.x == -INFINITY) {
+                cut_by_value = value_cut(top_p, cut);
+                if (cut_by_value && floor == 0.0 && u > 0.0) return locate(cut, 0.0, u);
+            }
+        }
+        if (p_on && !cut_by_value) {
             const double Z = cut.x == -INFINITY ? histogram<true, true>(cut) : histogram<true, false>(cut);
             const double goal = (double)top_p * Z;
             Zone z{0, 0, 0, kBins - 1};
@@ -1181,7 +1335,8 @@ sample_kernel(const SampleArgs a) {
             const float low = (float)((double)m - (double)(kBins - 1) / kBinsPerOctave / log2e * (double)Tm);
             Sampler<T, kStaged, kTeam> s{sm, team, row,
                                          Weights{(double)m, kBinsPerOctave * log2e / (double)Tm, m, fmaxf(low, -FLT_MAX),
-                                                 (float)fmin(log2e / (double)Tm, 1e30), sm.pow2}, m};
+                                                 (float)fmin(log2e / (double)Tm, 1e30), sm.pow2}, m,
+                                         reinterpret_cast<double *>(s_dyn + share)};     // (the same place in every block)
             token = s.sample(mx, top_k, top_p, min_p, a.uniform[(size_t)b * a.N + r]);
         }
     }
@@ -1264,9 +1419,10 @@ static cudaError_t launch_t(const SampleArgs &a, const char *what, cudaStream_t 
     // Blocks per row: as many as rows are too few to fill the GPU with, and as many as it takes for the slices to fit
     // shared memory two to an SM.
     const long long rows = (long long)a.B * a.R;
-    auto slice = [&](int team) { return (((size_t)a.V * sizeof(T) + 15 + 15) / 16 + team - 1) / team * 16; };
+    const size_t by_value = ByValue<T, true>::on ? kValueBytes : 0;
+    auto slice = [&](int team) { return (((size_t)a.V * sizeof(T) + 15 + 15) / 16 + team - 1) / team * 16 + by_value; };
     int team = 1;
-    while (team < kMaxTeam && (slice(team) > kSampleDynMax / 2 || (rows * team * 2 <= 2 * 148 && slice(team) > 8192))) team *= 2;
+    while (team < kMaxTeam && (slice(team) > kSampleDynMax / 2 || (rows * team * 2 <= 2 * 148 && slice(team) - by_value > 8192))) team *= 2;
     const bool staged = slice(team) <= kSampleDynMax;
     const size_t tree = a.tokens ? sizeof(TreeSmem) : 0;
     const size_t smem = staged && slice(team) > tree ? slice(team) : tree;

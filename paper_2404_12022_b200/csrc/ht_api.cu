@@ -102,7 +102,7 @@ using namespace ht;
 
 extern "C" {
 
-int ht_version(void) { return 100; }
+int ht_version(void) { return 110; }
 
 const char *ht_last_error_string(void) { return g_err; }
 

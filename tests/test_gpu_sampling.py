@@ -126,6 +126,23 @@ def test_cuts_among_tokens_far_below_the_largest(hb):
     check(hb, x.cuda(), u, k=[700, 700, 2000, 0, 0, 0], p=[1.0, 0.9, 1.0, 0.9999999, 0.99999994, 0.9999])
 
 
+@pytest.mark.parametrize("V", [700, 9001, 40003])
+def test_bf16_nuclei_wherever_the_cut_lies(hb, V):
+    """The cut among positive, negative and equal values, among values next to zero, in rows far from zero, in rows whose
+    smaller values lie beyond the counted range; rows over one block and over several."""
+    g = torch.Generator().manual_seed(61)
+    rnd = torch.randn((10, 1, V), generator=g)
+    x = torch.stack([rnd[0], rnd[1] * 1e-3, rnd[2] * 1e-6 + 0.0, rnd[3] * 3 - 40.0, rnd[4] * 60.0 - 300.0, rnd[5] * 3 + 180.0,
+                     (rnd[6] * 2).round(), rnd[7].clamp(max=0.0), -rnd[8].abs() * 20.0, rnd[9] * 0.01 + 1.0])
+    x = x.to(torch.bfloat16).cuda()
+    for seed, p in enumerate((0.2, 0.5, 0.62, 0.9, 0.999)):
+        u = np.random.default_rng(seed).random((10, 1)).astype(np.float32)
+        for T in (1.0, 0.3, 30.0):
+            check(hb, x, u, T=[T] * 10, p=[p] * 10, what="p %g T %g" % (p, T))
+        check(hb, x, u, p=[p] * 10, m=[0.3] * 10, what="p %g and min_p" % p)
+        check(hb, x, np.zeros((10, 1)), p=[p] * 10, what="p %g, uniform 0" % p)
+
+
 def test_bad_parameters_are_flagged(hb):
     B, nan, inf = 9, float("nan"), float("inf")
     x, _ = logits(44, torch.float16, B, 2, 300)

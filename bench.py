@@ -209,10 +209,10 @@ class ClockSampler:
 # DRAM traffic per launch of the attention kernel on a c3 layer, from the ncu capture of the committed build summarised
 # at the end of profiles/attn_tc_kernel_c3_layer.md (dram__bytes_read.sum + dram__bytes_write.sum, mean of two launches).  It is only
 # reported while the kernel source is the one that was profiled.
-NCU_TRAFFIC = {"workload": "c3_llama7b_step_bf16", "bytes_per_launch": 287.6e6,
+NCU_TRAFFIC = {"workload": "c3_llama7b_step_bf16", "bytes_per_launch": 288.9e6,
                "source": ["paper_2404_12022_b200/csrc/attn_tc.cu", "paper_2404_12022_b200/csrc/attn_tc.cuh",
                           "paper_2404_12022_b200/csrc/ht_common.cuh"],
-               "sha256": "eaae2896afb6cfc62190630292e100236acc25093f3c70e33ac50d261a13661e"}
+               "sha256": "9d54db754242e2cc0a2a55e0eb49b135e29ceda58ae6a66f1e86aec4a88828dc"}
 
 
 def traffic_digest():

@@ -41,6 +41,11 @@
 //                        the first context tiles do not wait for it; each role waits where it
 //                        first touches what that kernel may still write or read.
 //
+//   scored forms       : instantiations whose scores are capped or biased by distance ahead of the
+//                        softmax (ht_tree_attention_scored; the arithmetic and its reasons are at
+//                        shape_scores).  4 x 91 rows on 4096 keys, 54.5 us without: cap 65 us,
+//                        bias 61 us, both 80 us -- the softmax groups, not HBM, set the pace.
+//
 // Every wait on an mbarrier is bounded; when one runs out the CTA raises an abort flag,
 // reports HT_STATUS_TIMEOUT, runs to the end of its control flow without further waiting,
 // drains its own copies, frees its TMEM and returns.

@@ -212,7 +212,7 @@ class ClockSampler:
 NCU_TRAFFIC = {"workload": "c3_llama7b_step_bf16", "bytes_per_launch": 288.9e6,
                "source": ["paper_2404_12022_b200/csrc/attn_tc.cu", "paper_2404_12022_b200/csrc/attn_tc.cuh",
                           "paper_2404_12022_b200/csrc/ht_common.cuh"],
-               "sha256": "9d54db754242e2cc0a2a55e0eb49b135e29ceda58ae6a66f1e86aec4a88828dc"}
+               "sha256": "e4c8148031ff0cd86ea962c8c407d901f46e811f390531258ff56be383947343"}
 
 
 def traffic_digest():

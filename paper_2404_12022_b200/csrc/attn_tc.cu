@@ -130,12 +130,12 @@ __device__ __forceinline__ void fetch_q_tile(Smem &sm, const CUtensorMap &tm_q, 
 template <bool kBf16, bool kPaged, bool kClustered, int kShape = 0>
 __global__ void __launch_bounds__(kThreads, 1)
 attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
-               const __grid_constant__ CUtensorMap tm_v, const Params p, const PagedParams pp) {
+               const __grid_constant__ CUtensorMap tm_v, const Params p, const PagedParams pp, const __grid_constant__ ScoreParams sp) {
     extern __shared__ unsigned char smem_raw[];
     Smem &sm = *reinterpret_cast<Smem *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     volatile int *abort_flag = &sm.abort;
-    const bool from_end = (kShape & kShapeBias) && p.from_end;
+    const bool from_end = (kShape & kShapeBias) && sp.from_end;
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < kStages; ++i) { mbar_init(&sm.kv_full[i], 1); mbar_init(&sm.kv_empty[i], 1); }
@@ -345,7 +345,7 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
                     advance(k_slot, k_ph, j == 0 ? 1 : 2);                    // K entries: 0, 1, 3, 5, ...
                     if (j > 0) issue_pv(j - 1, prev_first, prev_tree);
                     prev_first = i < 2;
-                    prev_tree = (from_end ? sg.kt0 + sg.len - i : sg.kt0 + i + 1) * kTile > L - (kShape ? p.near_keys : 0);
+                    prev_tree = (from_end ? sg.kt0 + sg.len - i : sg.kt0 + i + 1) * kTile > L - (kShape ? sp.near_keys : 0);
                     ++j;
                 }
                 t += sg.len;
@@ -415,11 +415,11 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
             // the tree rows' positions (which the kernel ahead may have written) take the place of the parents
             if constexpr ((kShape & kShapeBias) != 0) {
                 if (new_rows) {
-                    stage_tree_positions(p, reinterpret_cast<float *>(sm.parent), sg.b, L, tid256);
+                    stage_tree_positions(sp, reinterpret_cast<float *>(sm.parent), sg.b, L, p.N, tid256);
                     softmax_groups_sync();
                 }
             }
-            const TreeKeys tree_keys{reinterpret_cast<const float *>(sm.parent) + kTile, &sm.anc[0][row], words};
+            const TreeKeys tree_keys{reinterpret_cast<const float *>(sm.parent) + kTile, &sm.anc[0][row], words, p.N};
 
             // A segment that is only part of its unit: which CTAs hold the other parts.  How many of
             // them have been delivered is asked anew at every tile and looked at in the epilogue, so
@@ -438,7 +438,7 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
             }
 
             RowShape shape{};
-            if constexpr ((kShape & kShapeBias) != 0) shape = row_shape<kShape>(p, real, sg.b, L, node, sg.hk * p.g + row % p.g);
+            if constexpr ((kShape & kShapeBias) != 0) shape = row_shape<kShape>(sp, real, sg.b, L, p.N, node, sg.hk * p.g + row % p.g);
             float m_ref = -INFINITY, l_sum = 0.f;
 #pragma unroll 1
             for (int i = 0; i < sg.len; ++i) {
@@ -502,8 +502,8 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
                 float mx = fmaxf(mx0, mx1) * p.scale_log2;   // scale > 0: max commutes with scaling
                 bool negligible = false;
                 if constexpr (kShape != 0) {
-                    if ((kShape & kShapeCap) && shape_coefficients(p, shape, size, s_addr, 4, xa)) tmem_ld32(s_addr, xa);
-                    mx = shape_bound<kShape>(p, mx, tile_lo, kTile, shape);
+                    if ((kShape & kShapeCap) && shape_coefficients(sp, shape, size, s_addr, 4, xa)) tmem_ld32(s_addr, xa);
+                    mx = shape_bound<kShape>(sp, mx, tile_lo, kTile, shape);
                     const bool tree_tile = tile_lo + kTile > L;
                     if (tree_tile || ((kShape & kShapeBias) && __any_sync(0xffffffffu, real && !(mx <= m_ref + kRescaleThreshold)))) {
                         // masked keys, or a reference that may have to rise: the exact maximum
@@ -511,7 +511,7 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
 #pragma unroll 1
                         for (int w = 0; w < 4; ++w) {
                             tmem_ld_wait();
-                            shape_scores<kShape, true>(p, xa, tile_lo + 32 * w, L, tree_keys, shape, 0.f);
+                            shape_scores<kShape, true>(sp, xa, tile_lo + 32 * w, L, tree_keys, shape, 0.f);
                             float m0 = -INFINITY, m1 = -INFINITY;
 #pragma unroll
                             for (int c = 0; c < 32; c += 4) {
@@ -522,7 +522,7 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
                             tmem_ld32(s_addr + ((w + 1) & 3) * 32, xa);           // after the last chunk: chunk 0 again, for pass 2
                         }
                     } else if (kShape & kShapeBias) {
-                        negligible = __all_sync(0xffffffffu, !real || mx < m_ref - kNegligibleLog2) && tile_lo + kTile <= L - p.near_keys;
+                        negligible = __all_sync(0xffffffffu, !real || mx < m_ref - kNegligibleLog2) && tile_lo + kTile <= L - sp.near_keys;
                     }
                 }
                 // --- running maximum, raised lazily ---
@@ -562,13 +562,13 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
 #pragma unroll
                         for (int w = 0; w < 4; ++w) tmem_st16(s_addr + w * 16, r);
                     } else {
-                        if (tile_lo + kTile > L - p.near_keys)
+                        if (tile_lo + kTile > L - sp.near_keys)
                             softmax_pass2<kBf16, true, true>(s_addr, xa, xb, scale2, nbase2, acc2, [&](float *x, int w) {
-                                shape_scores<kShape, true>(p, x, tile_lo + 32 * w, L, tree_keys, shape, -base);
+                                shape_scores<kShape, true>(sp, x, tile_lo + 32 * w, L, tree_keys, shape, -base);
                             });
                         else
                             softmax_pass2<kBf16, false, true>(s_addr, xa, xb, scale2, nbase2, acc2, [&](float *x, int w) {
-                                shape_scores<kShape, false>(p, x, tile_lo + 32 * w, L, tree_keys, shape, -base);
+                                shape_scores<kShape, false>(sp, x, tile_lo + 32 * w, L, tree_keys, shape, -base);
                             });
                     }
                 } else {
@@ -905,7 +905,7 @@ size_t attn_tc_workspace(const ht_attn_desc &d) {
     return ticket_bytes(d) + (size_t)2 * sm_count() * (pair_mode(d) ? 2 : 1) * tc::kSlotFloats * sizeof(float);
 }
 
-typedef void (*AttnKernelFn)(const CUtensorMap, const CUtensorMap, const CUtensorMap, const tc::Params, const tc::PagedParams);
+typedef void (*AttnKernelFn)(const CUtensorMap, const CUtensorMap, const CUtensorMap, const tc::Params, const tc::PagedParams, const tc::ScoreParams);
 constexpr int kAttnForms = 32;             // bf16, paged, clustered, then the shape of the scores
 template <int kShape>
 static AttnKernelFn attn_tc_form(int form) {
@@ -998,7 +998,7 @@ static int make_map(CUtensorMap *map, const void *base, int dtype, const cuuint6
 
 
 int launch_attn_tc_pair_kernel(const CUtensorMap &tm_q, const CUtensorMap &tm_k, const CUtensorMap &tm_v, const tc::Params &p,
-                               const tc::PagedParams &pp, bool bf16, bool paged, int shape, cudaStream_t s);
+                               const tc::PagedParams &pp, const tc::ScoreParams &sp, bool bf16, bool paged, int shape, cudaStream_t s);
 
 int launch_attn_tc(const ht_attn_desc &d, const void *q, const void *kc, const void *vc, const int32_t *kv_len,
                    const int32_t *parent, void *out, void *ws, size_t ws_bytes, int32_t *status, cudaStream_t s,
@@ -1045,34 +1045,33 @@ int launch_attn_tc(const ht_attn_desc &d, const void *q, const void *kc, const v
     p.n_rt = units_per_head(d);
     const float scale = d.scale > 0.f ? d.scale : 1.f / sqrtf((float)d.D);
     p.scale_log2 = scale * 1.4426950408889634f;
-    p.score_mul = 0.f; p.cap_log2 = 0.f; p.series_lim = -1.f;
-    for (int i = 0; i < 6; ++i) p.series[i] = 0.f;
-    p.slopes = nullptr; p.pos = nullptr; p.near_keys = 0; p.from_end = 0;
+    tc::ScoreParams sp{};
+    sp.series_lim = -1.f;
     int shape = 0;
     if (score) {
         const double log2e = 1.4426950408889634074;
-        p.score_mul = p.scale_log2;
+        sp.score_mul = p.scale_log2;
         if (score->cap > 0.f) {
             shape |= tc::kShapeCap;
             const double mul = fmin((double)scale / score->cap, 1e30);
-            p.score_mul = (float)mul;
-            p.cap_log2 = (float)(score->cap * log2e);
+            sp.score_mul = (float)mul;
+            sp.cap_log2 = (float)(score->cap * log2e);
             if (mul <= 1000.0) {                     // (beyond, the coefficients leave the range of 32 bits)
                 // Taylor series of tanh
                 const double a[6] = {1.0, -1.0 / 3.0, 2.0 / 15.0, -17.0 / 315.0, 62.0 / 2835.0, -1382.0 / 155925.0};
                 double power = score->cap * log2e * mul;
-                for (int i = 0; i < 6; ++i, power *= mul * mul) p.series[i] = (float)(a[i] * power);
-                p.series_lim = 0.5f;
+                for (int i = 0; i < 6; ++i, power *= mul * mul) sp.series[i] = (float)(a[i] * power);
+                sp.series_lim = 0.5f;
             }
         }
         if (score->slopes) {
             shape |= tc::kShapeBias;
-            p.slopes = score->slopes;
-            p.pos = score->pos;
+            sp.slopes = score->slopes;
+            sp.pos = score->pos;
             // A steep slope leaves a row a handful of keys: the tree's and the context rows right ahead of it.  The rounding
             // of their weights to 16 bits does not average away, as on tiles with tree keys.
-            p.near_keys = tc::kTile;
-            p.from_end = 1;
+            sp.near_keys = tc::kTile;
+            sp.from_end = 1;
         }
         p.scale_log2 = 1.f;
     }
@@ -1125,7 +1124,7 @@ int launch_attn_tc(const ht_attn_desc &d, const void *q, const void *kc, const v
     trace("ht_tree_attention -> %s kernel, %s, %d CTAs%s%s", pair_mode(d) ? "tile-pair" : "one-tile",
           k > 1 ? (k == 16 ? "clusters of 16" : (k == 8 ? (split == 2 ? "two clusters of 8 per unit" : "clusters of 8") : (k == 4 ? (split == 4 ? "four clusters of 4 per unit" : "clusters of 4") : "clusters of 2"))) : "persistent",
           p.grid, p.early ? ", early start" : "", needs_prepare(d, pages != nullptr) ? ", counters cleared by a kernel" : "");
-    if (pair_mode(d)) return launch_attn_tc_pair_kernel(tm_q, tm_k, tm_v, p, pp, d.dtype == HT_BF16, pages != nullptr, shape, s);
+    if (pair_mode(d)) return launch_attn_tc_pair_kernel(tm_q, tm_k, tm_v, p, pp, sp, d.dtype == HT_BF16, pages != nullptr, shape, s);
     e = ensure_smem_attr(sizeof(tc::Smem) + 1024);
     if (e != cudaSuccess) return fail(HT_ERR_CUDA, "cudaFuncSetAttribute: %s", cudaGetErrorString(e));
     // Few (sequence, KV head) units: one cluster of 16, 8, 4 or 2 CTAs per unit, parts reduced through
@@ -1145,7 +1144,7 @@ int launch_attn_tc(const ht_attn_desc &d, const void *q, const void *kc, const v
     attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = k > 1 ? 2 : 1;
-    e = cudaLaunchKernelEx(&cfg, attn_tc_fn(d.dtype == HT_BF16, pages != nullptr, k > 1, shape), tm_q, tm_k, tm_v, p, pp);
+    e = cudaLaunchKernelEx(&cfg, attn_tc_fn(d.dtype == HT_BF16, pages != nullptr, k > 1, shape), tm_q, tm_k, tm_v, p, pp, sp);
     if (e != cudaSuccess) {
         cudaGetLastError();
         return fail(HT_ERR_CUDA, "ht_tree_attention (tcgen05, clusters of %d): %s", k > 1 ? k : 1, cudaGetErrorString(e));

@@ -40,15 +40,6 @@ struct Params {
     int cluster_split;     // clusters per unit: 1, or 2 (each reduces its half of the keys; the two results meet in the workspace)
     int wait_kcycles;      // how long a wait on an mbarrier may last, in units of 1024 clock cycles
     int early;             // HT_ATTN_CONTEXT_FINAL: lengths, trees and context rows may be read while the kernel ahead still runs
-    // The scored instantiations only (scale_log2 is 1 there: their scores are shaped into log2 units before the softmax):
-    float score_mul;       // with a cap: scale / cap; without: scale * log2(e)
-    float cap_log2;        // cap * log2(e)
-    float series[6];       // cap * log2(e) * tanh(score_mul x) = x (series[0] + u (series[1] + u (...))), u = x^2
-    float series_lim;      // |score_mul x| up to which it is taken (negative: never)
-    const float *slopes;   // [Hq]: distance bias
-    const int32_t *pos;    // [B, N] position ids of the query rows (with slopes)
-    int near_keys;         // tiles reaching past context row kv_len - near_keys send P as a hi + lo pair
-    int from_end;          // a segment's tiles are taken from its last to its first
 };
 // The launch is serialized programmatically behind the kernel before it in the stream: a thread passes this point once
 // that kernel has completed and what it wrote is visible, and only then lets this kernel's own dependents be set up.
@@ -67,6 +58,19 @@ enum : int {
 struct PagedParams {
     const int32_t *block_table;
     int page_size, page_shift, max_pages, n_pages;      // page_size = 1 << page_shift
+};
+
+// What the scored instantiations need besides (a kernel parameter of its own, like PagedParams; Params.scale_log2 is 1 there:
+// their scores are shaped into log2 units before the softmax).
+struct ScoreParams {
+    float score_mul;       // with a cap: scale / cap; without: scale * log2(e)
+    float cap_log2;        // cap * log2(e)
+    float series[6];       // cap * log2(e) * tanh(score_mul x) = x (series[0] + u (series[1] + u (...))), u = x^2
+    float series_lim;      // |score_mul x| up to which it is taken (negative: never)
+    const float *slopes;   // [Hq]: distance bias
+    const int32_t *pos;    // [B, N] position ids of the query rows (with slopes)
+    int near_keys;         // tiles reaching past context row kv_len - near_keys send P as a hi + lo pair
+    int from_end;          // a segment's tiles are taken from its last to its first
 };
 
 struct __align__(1024) Smem {
@@ -328,11 +332,11 @@ struct RowShape {
     float a[6];            // a shaped score is x (a[0] + u (a[1] + u (...))), u = x^2
 };
 template <int kShape>
-__device__ __forceinline__ RowShape row_shape(const Params &p, bool real, int b, int L, int node, int head) {
+__device__ __forceinline__ RowShape row_shape(const ScoreParams &p, bool real, int b, int L, int N, int node, int head) {
     RowShape r{};
     if ((kShape & kShapeBias) && real) {
         r.slope = p.slopes[head] * 1.4426950408889634f;
-        r.pos = p.pos[(size_t)b * p.N + node];
+        r.pos = p.pos[(size_t)b * N + node];
         r.from_len = (float)(r.pos - L);
     }
     return r;
@@ -343,7 +347,7 @@ __device__ __forceinline__ float rcp(float x) {
     return y;
 }
 // cap tanh(x scale / cap), any x.
-__device__ __forceinline__ float cap_one(const Params &p, float x) {
+__device__ __forceinline__ float cap_one(const ScoreParams &p, float x) {
     const float u = x * x;
     const float near = x * fmaf(u, fmaf(u, fmaf(u, fmaf(u, fmaf(u, p.series[5], p.series[4]), p.series[3]), p.series[2]), p.series[1]), p.series[0]);
     const float far = fmaf(-2.f * p.cap_log2, rcp(1.f + ex2(x * (2.8853900817779268f * p.score_mul))), p.cap_log2);
@@ -359,7 +363,7 @@ __device__ __forceinline__ float shape_size(const float *x, float size) {
 }
 // The tile's coefficients; its `chunks` x 32 products at s_addr rewritten as capped scores where the series does not
 // reach (a register array of 32 as scratch; size: the row's largest |product|).  True where they were rewritten.
-__device__ __forceinline__ bool shape_coefficients(const Params &p, RowShape &row, float size, uint32_t s_addr, int chunks, float *x) {
+__device__ __forceinline__ bool shape_coefficients(const ScoreParams &p, RowShape &row, float size, uint32_t s_addr, int chunks, float *x) {
     const bool far = __any_sync(0xffffffffu, !(size * p.score_mul <= p.series_lim));
 #pragma unroll
     for (int i = 0; i < 6; ++i) row.a[i] = far ? (i == 0 ? 1.f : 0.f) : p.series[i];
@@ -380,7 +384,7 @@ __device__ __forceinline__ bool shape_coefficients(const Params &p, RowShape &ro
 }
 // An upper bound of the shaped scores of `keys` context keys from key0 on whose largest raw product is mx.
 template <int kShape>
-__device__ __forceinline__ float shape_bound(const Params &p, float mx, int key0, int keys, const RowShape &row) {
+__device__ __forceinline__ float shape_bound(const ScoreParams &p, float mx, int key0, int keys, const RowShape &row) {
     float s = (kShape & kShapeCap) ? cap_one(p, mx) : mx * p.score_mul;
     if (kShape & kShapeBias) s += row.slope * (float)((row.slope > 0.f ? key0 + keys - 1 : key0) - row.pos);
     return s;
@@ -391,19 +395,19 @@ __device__ __forceinline__ float shape_bound(const Params &p, float mx, int key0
 struct TreeKeys {
     const float *pos;
     const uint32_t *anc;
-    int words;
+    int words, N;
 };
 // Fills the area that `pos` points into (all softmax threads; a barrier of theirs on both sides).
-__device__ __forceinline__ void stage_tree_positions(const Params &p, float *area, int b, int L, int tid256) {
-    for (int i = tid256; i < p.N + 2 * kTile; i += 256) {
+__device__ __forceinline__ void stage_tree_positions(const ScoreParams &p, float *area, int b, int L, int N, int tid256) {
+    for (int i = tid256; i < N + 2 * kTile; i += 256) {
         const int c = i - kTile;
-        area[i] = c < 0 ? (float)c : (c < p.N ? (float)(p.pos[(size_t)b * p.N + c] - L) : 0.f);
+        area[i] = c < 0 ? (float)c : (c < N ? (float)(p.pos[(size_t)b * N + c] - L) : 0.f);
     }
 }
 // 32 raw products of keys key0, ... of a sequence with L context rows -> shaped scores plus `add`.  kTree: some may be
 // tree keys; those the row must not see, and the tail, become -inf whatever they hold.
 template <int kShape, bool kTree>
-__device__ __forceinline__ void shape_scores(const Params &p, float *x, int key0, int L, const TreeKeys &tk, const RowShape &row, float add) {
+__device__ __forceinline__ void shape_scores(const ScoreParams &p, float *x, int key0, int L, const TreeKeys &tk, const RowShape &row, float add) {
     const bool tree = kTree && key0 + 32 > L;
     // the bias, less the row's own position: linear in the key for context keys
     const float slope = (kShape & kShapeBias) && !tree ? row.slope : 0.f;
@@ -433,7 +437,7 @@ __device__ __forceinline__ void shape_scores(const Params &p, float *x, int key0
     if (tree) {
         const int cc0 = key0 - L;                            // tree index of the first key, above -32
         if (kShape & kShapeBias) {
-            const float *pos = tk.pos + min(cc0, p.N);       // (wholly behind the tree: masked)
+            const float *pos = tk.pos + min(cc0, tk.N);       // (wholly behind the tree: masked)
 #pragma unroll
             for (int c = 0; c < 32; ++c) x[c] = fmaf(row.slope, pos[c], x[c]);
         }

@@ -141,12 +141,12 @@ __device__ __noinline__ void cluster_merge_pair(const Params &p, const unsigned 
 template <bool kBf16, bool kPaged, bool kSplit, int kShape = 0>
 __global__ void __launch_bounds__(kPThreads, 1)
 attn_tc_pair_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
-                    const __grid_constant__ CUtensorMap tm_v, const Params p, const PagedParams pp) {
+                    const __grid_constant__ CUtensorMap tm_v, const Params p, const PagedParams pp, const __grid_constant__ ScoreParams sp) {
     extern __shared__ unsigned char smem_raw[];
     PSmem &sm = *reinterpret_cast<PSmem *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     volatile int *abort_flag = &sm.abort;
-    const bool from_end = (kShape & kShapeBias) && p.from_end;
+    const bool from_end = (kShape & kShapeBias) && sp.from_end;
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < kPStages; ++i) { mbar_init(&sm.kv_full[i], 1); mbar_init(&sm.kv_empty[i], 2); }
@@ -406,7 +406,7 @@ attn_tc_pair_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                         if (pend) issue_pv();
                         pend = true;
                         pend_first = (i == 0 && h == 0);
-                        pend_tree = key_hi + h * kHalf > L - (kShape ? p.near_keys : 0);
+                        pend_tree = key_hi + h * kHalf > L - (kShape ? sp.near_keys : 0);
                         pend_h = h;
                         pend_slot = v_slot;
                         pend_ph = v_ph;
@@ -478,11 +478,11 @@ attn_tc_pair_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
             // the tree rows' positions (which the kernel ahead may have written) take the place of the parents
             if constexpr ((kShape & kShapeBias) != 0) {
                 if (new_rows) {
-                    stage_tree_positions(p, reinterpret_cast<float *>(sm.parent), sg.b, L, tid256);
+                    stage_tree_positions(sp, reinterpret_cast<float *>(sm.parent), sg.b, L, p.N, tid256);
                     softmax_groups_sync();
                 }
             }
-            const TreeKeys tree_keys{reinterpret_cast<const float *>(sm.parent) + kTile, &sm.anc[s * words * kRows + row], words};
+            const TreeKeys tree_keys{reinterpret_cast<const float *>(sm.parent) + kTile, &sm.anc[s * words * kRows + row], words, p.N};
 
             // A segment that is only part of its unit: see the one-tile kernel.
             const bool complete = sg.kt0 == 0 && sg.len == sg.nkt;
@@ -499,7 +499,7 @@ attn_tc_pair_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
             }
 
             RowShape shape{};
-            if constexpr ((kShape & kShapeBias) != 0) shape = row_shape<kShape>(p, real, sg.b, L, node, sg.hk * p.g + row % p.g);
+            if constexpr ((kShape & kShapeBias) != 0) shape = row_shape<kShape>(sp, real, sg.b, L, p.N, node, sg.hk * p.g + row % p.g);
             float m_ref = -INFINITY, l_sum = 0.f;
             int last_h = -1;                            // score buffer of this stream's latest P V in this segment
             if (active) {
@@ -555,28 +555,28 @@ attn_tc_pair_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                     float mx = fmaxf(mx0, mx1) * p.scale_log2;
                     bool negligible = false;
                     bool direct = false;                    // the scores become exponents below, right ahead of the exponentials
-                    const bool hi_lo = key_lo + kHalf > L - (kShape ? p.near_keys : 0);
+                    const bool hi_lo = key_lo + kHalf > L - (kShape ? sp.near_keys : 0);
                     if constexpr (kShape != 0) {
                         float size = 0.f;                   // the largest |product| of the row
                         if (kShape & kShapeCap) size = shape_size(xb, shape_size(xa, size));
-                        if ((kShape & kShapeCap) && shape_coefficients(p, shape, size, s_addr, 2, xa)) {
+                        if ((kShape & kShapeCap) && shape_coefficients(sp, shape, size, s_addr, 2, xa)) {
                             tmem_ld32(s_addr, xa);
                             tmem_ld32(s_addr + 32, xb);
                             tmem_ld_wait();
                         }
-                        mx = shape_bound<kShape>(p, mx, key_lo, kHalf, shape);
+                        mx = shape_bound<kShape>(sp, mx, key_lo, kHalf, shape);
                         const bool tree_half = key_lo + kHalf > L;
                         const bool exact = tree_half || ((kShape & kShapeBias) && __any_sync(0xffffffffu, real && !(mx <= m_ref + kRescaleThreshold)));
                         if (kShape & kShapeBias)
-                            negligible = !exact && __all_sync(0xffffffffu, !real || mx < m_ref - kNegligibleLog2) && key_lo + kHalf <= L - p.near_keys;
+                            negligible = !exact && __all_sync(0xffffffffu, !real || mx < m_ref - kNegligibleLog2) && key_lo + kHalf <= L - sp.near_keys;
                         direct = kShape == kShapeCap && !exact && !hi_lo;
                         if (!negligible && !direct) {
                             if (tree_half) {
-                                shape_scores<kShape, true>(p, xa, key_lo, L, tree_keys, shape, 0.f);
-                                shape_scores<kShape, true>(p, xb, key_lo + 32, L, tree_keys, shape, 0.f);
+                                shape_scores<kShape, true>(sp, xa, key_lo, L, tree_keys, shape, 0.f);
+                                shape_scores<kShape, true>(sp, xb, key_lo + 32, L, tree_keys, shape, 0.f);
                             } else {
-                                shape_scores<kShape, false>(p, xa, key_lo, L, tree_keys, shape, 0.f);
-                                shape_scores<kShape, false>(p, xb, key_lo + 32, L, tree_keys, shape, 0.f);
+                                shape_scores<kShape, false>(sp, xa, key_lo, L, tree_keys, shape, 0.f);
+                                shape_scores<kShape, false>(sp, xb, key_lo + 32, L, tree_keys, shape, 0.f);
                             }
                             if (exact) {                    // masked keys, or a reference that may have to rise
                                 mx = -INFINITY;
@@ -665,7 +665,7 @@ attn_tc_pair_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                         // former's multiply-adds fill the time of the latter's special-function unit (16 x 67 rows on 8192 keys:
                         // 760 -> 642 us; with a bias, whose tiles are mostly negligible, it only costs registers: 464 -> 486 us).
                         auto shaped_chunk = [&](float *x, int key0, uint32_t col) {
-                            shape_scores<kShape, false>(p, x, key0, L, tree_keys, shape, -base);
+                            shape_scores<kShape, false>(sp, x, key0, L, tree_keys, shape, -base);
                             uint32_t r[16];
 #pragma unroll
                             for (int c = 0; c < 16; ++c) {
@@ -875,7 +875,7 @@ attn_tc_pair_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
 
 }  // namespace tc
 
-typedef void (*PairKernelFn)(const CUtensorMap, const CUtensorMap, const CUtensorMap, const tc::Params, const tc::PagedParams);
+typedef void (*PairKernelFn)(const CUtensorMap, const CUtensorMap, const CUtensorMap, const tc::Params, const tc::PagedParams, const tc::ScoreParams);
 template <int kShape>
 static PairKernelFn pair_form(int form) {
     static const PairKernelFn fns[8] = {
@@ -896,7 +896,7 @@ static PairKernelFn pair_fn(int form, int shape) {
 
 // Raises the kernels' dynamic shared memory limit (once per device) and launches.
 int launch_attn_tc_pair_kernel(const CUtensorMap &tm_q, const CUtensorMap &tm_k, const CUtensorMap &tm_v, const tc::Params &p,
-                               const tc::PagedParams &pp, bool bf16, bool paged, int shape, cudaStream_t s) {
+                               const tc::PagedParams &pp, const tc::ScoreParams &sp, bool bf16, bool paged, int shape, cudaStream_t s) {
     const int form = (bf16 ? 1 : 0) + (paged ? 2 : 0) + (p.cluster_split > 1 ? 4 : 0);
     const PairKernelFn fn = pair_fn(form, shape);
     static bool done[64];
@@ -927,7 +927,7 @@ int launch_attn_tc_pair_kernel(const CUtensorMap &tm_q, const CUtensorMap &tm_k,
     attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = p.cluster_k > 1 ? 2 : 1;
-    e = cudaLaunchKernelEx(&cfg, fn, tm_q, tm_k, tm_v, p, pp);
+    e = cudaLaunchKernelEx(&cfg, fn, tm_q, tm_k, tm_v, p, pp, sp);
     if (e != cudaSuccess) {
         cudaGetLastError();
         return fail(HT_ERR_CUDA, "ht_tree_attention (tcgen05, tile pairs, clusters of %d): %s", p.cluster_k > 1 ? p.cluster_k : 1,

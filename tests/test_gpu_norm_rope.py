@@ -90,6 +90,12 @@ def test_norm_rope_against_the_oracle(hb, dtype, shape, kw):
     run_one(hb, DT[dtype], shape, kw, fused=True, norm=3)
 
 
+@pytest.mark.parametrize("dtype,shape", [("bf16", (1, 5, 128, 32, 128)), ("f32", (2, 3, 128, 32, 128)), ("f16", (8, 400, 2, 1, 64)),
+                                         ("bf16", (3, 700, 33, 3, 128))], ids=lambda s: str(s))
+def test_more_heads_than_a_block_takes_and_more_rows_than_blocks(hb, dtype, shape):
+    run_one(hb, DT[dtype], shape, dict(rot_dim=64), fused=True, norm=3)
+
+
 @pytest.mark.parametrize("norm", [0, 1, 2])
 def test_norm_of_either_side_dense_inputs_and_in_place(hb, norm):
     run_one(hb, torch.bfloat16, (2, 9, 8, 4, 128), {}, fused=False, norm=norm)

@@ -143,6 +143,23 @@ def test_bf16_nuclei_wherever_the_cut_lies(hb, V):
         check(hb, x, np.zeros((10, 1)), p=[p] * 10, what="p %g, uniform 0" % p)
 
 
+def test_a_row_too_long_for_shared_memory(hb):
+    x, u = logits(62, torch.float32, 2, 1, 500001, 2.0, 10.0)
+    check(hb, x, u)
+    check(hb, x, u, k=[40, 900], p=[0.9, 0.95])
+    check(hb, x, u, p=[0.3, 0.9])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_extreme_parameters(hb, dtype):
+    V = 2000
+    x, u = logits(63, DT[dtype], 8, 2, V)
+    check(hb, x, u, T=[1e-30, 1e-38, 1e-3, 1e3, 1e10, 1e30, 1.0, 1.0])
+    check(hb, x, u, T=[1e-30, 1e-3, 1e3, 1e10] * 2, p=[0.5] * 8)
+    check(hb, x, u, k=[V - 1, V, V + 1, 2 ** 31 - 1, -(2 ** 31), 512, 513, 1])
+    check(hb, x, u, p=[1e-30, 1e-6, 0.9999999, 1.0, 2.0, 0.0, -1.0, 1.0], m=[0, 0, 0, 1.0, 0.999, 1e-30, 0.5, -3.0])
+
+
 def test_bad_parameters_are_flagged(hb):
     B, nan, inf = 9, float("nan"), float("inf")
     x, _ = logits(44, torch.float16, B, 2, 300)
@@ -230,6 +247,18 @@ def test_statuses_of_sampled_verification(hb):
     u[2, 7] = 0.5
     got = hb.verify_sampled(x, dev(u), tokens, dev(parent, torch.int32), None, max_path=12, accept_len=got[1])
     assert got[4].tolist() == [0, 1, 0, 0] and got[1].tolist()[0] == T
+
+
+def test_more_rows_than_the_tree_search_stages(hb, oracle):
+    B, N, V = 2, 1100, 40
+    x, u = logits(49, torch.bfloat16, B, N, V, 2.0, 20.0)
+    parent = trees(np.random.default_rng(4), B, N, N)
+    pred = so.sample(x.double().cpu().numpy(), u.astype(np.float64))
+    tokens = np.take_along_axis(pred, np.maximum(parent, 0), 1)
+    got = hb.verify_sampled(x, dev(u), dev(tokens, torch.int32), dev(parent, torch.int32), None, max_path=255)
+    want = oracle.accept_scan(tokens, parent, pred, None, 255)
+    for g, w in zip(got, (pred, *want)):
+        assert np.array_equal(g.cpu().numpy(), w)
 
 
 def test_captured_and_replayed_and_two_streams(hb, oracle):

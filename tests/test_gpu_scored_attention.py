@@ -131,6 +131,29 @@ def test_work_splits_clusters_and_promises(hb, shape, final):
     close(plain, reference(c, 0.0, False))
 
 
+@pytest.mark.parametrize("shape", [(1, 1000, 2, 2, 128, [64]), (1, 1024, 2, 1, 128, [0]), (2, 300, 4, 2, 128, [130, 5])],
+                         ids=lambda s: "N%dHq%dHkv%d" % s[1:4])
+def test_large_trees_on_strided_views_of_a_layered_cache(hb, shape):
+    c = case(35, "bf16", *shape)
+    q, k, v, lens, parent, slopes, pos = c
+    layers = torch.zeros((2, 3) + tuple(k.shape), dtype=k.dtype, device="cuda")
+    layers[0, 1], layers[1, 1] = k, v
+    for cap, bias in ((10.0, False), (0.0, True), (10.0, True)):
+        check(hb, (q, layers[0, 1], layers[1, 1], lens, parent, slopes, pos), cap, bias)
+
+
+def test_waits_that_run_out_are_reported_and_leave_the_device_usable(hb):
+    for shape in ((5, 37, 32, 32, 128, [900, 640, 33, 1200, 512]), (2, 19, 64, 8, 128, [3000, 2500])):
+        c = case(36, "bf16", *shape)
+        q, k, v, lens, parent, slopes, pos = c
+        kw = dict(cap=20.0, slopes=slopes, pos=pos)
+        _, st = hb.tree_attention_scored(q, k, v, lens, parent, flags=hb.HT_ATTN_TEST_SHORT_WAITS, **kw)
+        assert all(s in (0, 6) for s in st.tolist()) and 6 in st.tolist()
+        out, st = hb.tree_attention_scored(q, k, v, lens, parent, **kw)
+        assert (st == 0).all()
+        close(out, reference(c, 20.0, True))
+
+
 @pytest.mark.parametrize("splits", [1, 3, 8])
 def test_alu_kernel_splits(hb, splits):
     check(hb, case(27, "f32", 1, 18, 4, 2, 64, [700]), 20.0, True, num_splits=splits)

@@ -126,6 +126,23 @@ def test_cuts_among_tokens_far_below_the_largest(hb):
     check(hb, x.cuda(), u, k=[700, 700, 2000, 0, 0, 0], p=[1.0, 0.9, 1.0, 0.9999999, 0.99999994, 0.9999])
 
 
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("V", [4000, 22318, 131072])
+def test_cuts_by_count_far_below_the_largest(hb, dtype, V):
+    """The k-th token far below the largest, among values that are all distinct (where the type has them), among ties that
+    the list of candidates holds and among ties that it does not, with masked tokens between; u = 1 takes the last kept one."""
+    g = torch.Generator().manual_seed(77)
+    x = torch.randn((6, 1, V), generator=g)
+    x[2] = (20 * x[2]).round() / 20
+    x[3] = x[3].round()
+    x[4, 0, ::3] = float("-inf")
+    x[5, 0, ::3] = torch.finfo(DT[dtype]).min
+    x[:, 0, V // 2] = 70.0
+    u = np.array([[1.0], [0.5], [1.0], [1.0], [1.0], [1.0]], np.float32)
+    for k in (513, 1789, V // 2, V - 1):
+        check(hb, x.to(DT[dtype]).cuda(), u, k=[k] * 6, p=[1.0] * 5 + [0.99999994], what=str(k))
+
+
 @pytest.mark.parametrize("V", [700, 9001, 40003])
 def test_bf16_nuclei_wherever_the_cut_lies(hb, V):
     """The cut among positive, negative and equal values, among values next to zero, in rows far from zero, in rows whose

@@ -517,7 +517,10 @@ def _rows(t: torch.Tensor, dev: int, dtype, B: int, N: int, D: int, name: str):
     H = shape[2]
     if sd != 1 or (sh != D and H > 1) or (B > 1 and N > 1 and sb != N * sn):
         raise ValueError("%s: heads must be contiguous and D apart, rows evenly spaced over [B, N]" % name)
-    return H, (sn if N > 1 else (sb if B > 1 else H * D))
+    row = sn if N > 1 else (sb if B > 1 else H * D)
+    if row < H * D:                                      # (a broadcast tensor's 0 would read as "dense")
+        raise ValueError("%s: rows must not overlap; they are %d elements apart" % (name, row))
+    return H, row
 
 
 def _pair(k: torch.Tensor, v: torch.Tensor, dev: int, dtype, name: str):
@@ -529,6 +532,8 @@ def _pair(k: torch.Tensor, v: torch.Tensor, dev: int, dtype, name: str):
         raise ValueError("%s must share a 4-dimensional shape and strides" % name)
     if strides[3] != 1 or strides[2] != shape[3]:
         raise ValueError("%s: rows must be contiguous and D apart" % name)
+    if (strides[0] == 0 and shape[0] > 1) or (strides[1] == 0 and shape[1] > 1):         # (0 would read as "dense")
+        raise ValueError("%s must not be broadcast" % name)
     return shape, strides
 
 

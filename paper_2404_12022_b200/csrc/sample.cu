@@ -10,7 +10,7 @@
 // Every filter keeps a prefix of the order, so a kept set is one pair (x, index): the first element left out.
 //
 // The token is a whole number, and the cut of a flat distribution moves all that follows it, so weights and sums are
-// held in 64 bits (relative error about 1e-13; tokens below 2^-32 of the largest, whose sum is below 1e-5 of the whole,
+// held in 64 bits (relative error about 1e-13; tokens below 2^-31 of the largest, whose sum is below 1e-4 of the whole,
 // are added up in 32): a row's answer does not depend on how its sum was split.  Nothing is added by atomics but counts.
 //
 // A row is split over the blocks of a cluster (one block where the rows fill the GPU by themselves), its slices in

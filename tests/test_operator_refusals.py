@@ -108,3 +108,23 @@ def test_sampling_refuses(hb, ptr):
     assert ver(T=0) == inv and ver(T=5) == inv and ver(max_path=0) == inv and ver(max_path=256) == inv
     assert ver(tokens=None) == inv and ver(parent=None) == inv
     assert ver(B=0) == hb.HT_OK
+
+
+def test_binding_refuses_broadcast_rows_and_caches(hb):
+    """A stride of 0 stands for "dense" behind the binding: a broadcast tensor's would be read past its end."""
+    import torch
+    x = torch.zeros(1, 1, 2, 64)
+    rows = lambda t, B, N: hb._rows(t, -1, torch.float32, B, N, 64, "k_in")             # noqa: E731
+    assert rows(x, 1, 1) == (2, 128)
+    assert rows(torch.zeros(2, 3, 6, 64)[:, :, 1:3], 2, 3) == (2, 6 * 64)
+    for B, N in ((2, 3), (1, 3), (2, 1)):
+        with pytest.raises(ValueError, match="overlap"):
+            rows(x.expand(B, N, 2, 64), B, N)
+    with pytest.raises(ValueError, match="overlap"):
+        rows(torch.zeros(512).as_strided((1, 3, 2, 64), (512, 64, 64, 1)), 1, 3)
+    c = torch.zeros(1, 1, 16, 64)
+    pair = lambda t: hb._pair(t, t, -1, torch.float32, "caches")                        # noqa: E731
+    assert pair(c)[0] == (1, 1, 16, 64)
+    for B, H in ((2, 1), (1, 2), (2, 2)):
+        with pytest.raises(ValueError, match="broadcast"):
+            pair(c.expand(B, H, 16, 64))

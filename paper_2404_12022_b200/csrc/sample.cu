@@ -486,19 +486,22 @@ struct Sampler {
     float m;                              // largest logit
     double *value_weight;                 // [kValues] and behind them counts (kByValue)
 
-    // The kept elements equal to `key`, in index order: the index of the one that `ties` of them precede (INT_MAX: none).
+    // The cut behind the last element of value x that `in` keeps: where x is the value that `in` cuts through, `in` itself.
+    __device__ __forceinline__ Cut last_of(float x, const Cut &in) { return x == in.x ? in : Cut{x, INT_MAX}; }
+
+    // The cut among the elements of value key_value(key) that `in` keeps, behind the first `ties` of them in index order.
     // By the list, or, where they are more than it holds, by halving the range of the indexes, one pass per step.
-    __device__ __noinline__ int tie_index(const Cut in, unsigned int key, unsigned int ties) {
+    __device__ __noinline__ Cut tie_cut(const Cut in, unsigned int key, unsigned int ties) {
         open_list();
         row.each([&](float x, int i) { if (order_key(x) == key && in.keeps(x, i)) append(x, i); });
         const int n = close_list();
         if (n <= kList) {
-            int at = INT_MAX;
+            Cut c = last_of(key_value(key), in);
             if (!kTeam || team.rank == 0) {
                 sort_list(sm, n);
-                if (ties < (unsigned int)n) at = entry_index(sm.list[ties]);
+                if (ties < (unsigned int)n) c = Cut{key_value(key), entry_index(sm.list[ties])};
             }
-            return share(Cut{0.f, at}).index;
+            return share(c);
         }
         team.barrier();
         int a = 0, z = row.V;                                // the first index with `ties` equal elements ahead of it
@@ -509,7 +512,7 @@ struct Sampler {
             if (team.count(block_count(sm, c)) >= ties) z = mid;
             else a = mid + 1;
         }
-        return a;
+        return a < row.V ? Cut{key_value(key), a} : last_of(key_value(key), in);
     }
 
     // Cut behind the first `goal` elements of the order, by a radix selection on the values' keys (11, 11 and 10 bits): exact
@@ -536,7 +539,7 @@ struct Sampler {
             above += (unsigned int)*team.of(&sm.n_above, 0);
             team.barrier();                                  // (read by all before the next round's answer)
         }
-        return Cut{key_value(prefix), tie_index(in, prefix, goal - above)};
+        return tie_cut(in, prefix, goal - above);
     }
 
     // Elements ahead of the cut of a running weight, by halving the range of the keys: exact for every distribution, one
@@ -560,7 +563,7 @@ struct Sampler {
         unsigned int ties = n < 1.0 ? 1u : (n > 2.0e9 ? 2000000000u : (unsigned int)n);
         while (ties > 1 && !(above + (double)(ties - 1) * each_w < goal)) --ties;
         while (above + (double)ties * each_w < goal && ties < 2000000000u) ++ties;
-        return Cut{key_value(lo), tie_index(in, lo, ties)};
+        return tie_cut(in, lo, ties);
     }
 
     __device__ __forceinline__ void open_list() {            // (a barrier of the row lies behind every open_list)
@@ -1151,7 +1154,7 @@ struct Sampler {
                         sort_list(sm, n);
                         double sum;
                         const int at = list_cut(sm, wt, n, above, goal, &sum);
-                        c = at < n ? Cut{entry_value(sm.list[at]), entry_index(sm.list[at])} : Cut{entry_value(sm.list[n - 1]), INT_MAX};
+                        c = at < n ? Cut{entry_value(sm.list[at]), entry_index(sm.list[at])} : last_of(entry_value(sm.list[n - 1]), cut);
                     }
                     const Cut p_cut = share(c);
                     if (floor == 0.0 && u > 0.0) {

@@ -143,6 +143,23 @@ def test_cuts_by_count_far_below_the_largest(hb, dtype, V):
         check(hb, x.to(DT[dtype]).cuda(), u, k=[k] * 6, p=[1.0] * 5 + [0.99999994], what=str(k))
 
 
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("V", [1200, 6007, 60001])
+def test_nuclei_that_hold_all_of_a_top_k_cut_through_ties(hb, dtype, V):
+    """top_k ends among equal tokens and top_p is so near 1 that nothing else is cut: the tokens equal to the k-th, but
+    behind it, stay out.  (The k-th token carries at least 1e-6 of the weight, so top_p of 1 - 6e-8 to 1 - 1e-7 ends behind it.)"""
+    g = torch.Generator().manual_seed(31)
+    x = torch.randint(0, 8, (8, 1, V), generator=g).float() / 8                       # 150 to 7500 tokens of each value
+    x[4:] = torch.randint(0, 40, (4, 1, V), generator=g).float() / 40
+    x[3], x[7] = 0.0, 1.5                                                             # one value throughout
+    x = x.to(DT[dtype]).cuda()
+    for u in (0.0, 0.31, 0.77, 0.999):
+        for k in (3, 100, 300, 513, 700, 1100):
+            for p in (0.9999999, 0.99999994):
+                check(hb, x, np.full((8, 1), u, np.float32), k=[k] * 8, p=[p] * 8, what=str((u, k, p)))
+                check(hb, x, np.full((8, 1), u, np.float32), k=[k] * 8, p=[p] * 8, m=[0.5, 0.0] * 4, what=str((u, k, p, "min_p")))
+
+
 @pytest.mark.parametrize("V", [700, 9001, 40003])
 def test_bf16_nuclei_wherever_the_cut_lies(hb, V):
     """The cut among positive, negative and equal values, among values next to zero, in rows far from zero, in rows whose

@@ -58,7 +58,7 @@ def token(x, u, T=1.0, top_k=0, top_p=1.0, min_p=0.0):
     running = 0.0
     for i in kept:
         running += w[i]
-        if running > u * total:
+        if u < 1 and running > u * total:                    # (nothing exceeds all of the weight; the rounded sum may)
             return i
     return kept[-1]
 

@@ -1056,7 +1056,8 @@ struct Sampler {
     }
 
     __device__ __forceinline__ int sample(float thread_max, int top_k, float top_p, float min_p, float uniform) {
-        const double u = (double)uniform, floor = min_p > 0.f ? (double)min_p : 0.0;
+        // (nothing exceeds all of the weight: a rounded sum must not, so 1 becomes a number that no sum reaches)
+        const double u = uniform < 1.f ? (double)uniform : 2.0, floor = min_p > 0.f ? (double)min_p : 0.0;
         const bool first = !kTeam || team.rank == 0;
         Cut cut{-INFINITY, INT_MIN};                          // keeps everything above -inf (padding has indexes below 0)
         const bool p_on = top_p < 1.f;

@@ -68,6 +68,19 @@ def test_uniform_numbers_at_the_ends(hb):
         check(hb, x, u, **kw)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("V,N", [(30, 2000), (500, 500), (5003, 100), (60001, 8)])
+@pytest.mark.parametrize("kw", [dict(), dict(k=20), dict(k=700), dict(T=2.0)], ids=str)
+def test_uniform_one_takes_the_last_kept_token_with_a_weight(hb, dtype, V, N, kw):
+    """Tokens whose weight is lost in the rounding of the sum count as well: no running weight exceeds all of it."""
+    x, _ = logits(57, DT[dtype], 1, N, V, spread=12.0)
+    got, st = hb.sample(x, torch.ones((1, N), device="cuda"), dev([kw["T"]]) if "T" in kw else None, dev([kw["k"]], torch.int32) if "k" in kw else None)
+    a = x[0].double().cpu().numpy()
+    order = np.argsort(-a, axis=1, kind="stable")[:, :kw.get("k", V)]
+    assert ((a.max(1) - a.min(1)) < 600).all()                                          # every weight is above 2^-1000
+    assert (st == 0).all() and np.array_equal(got[0].cpu().numpy(), order.max(1))
+
+
 def test_weights_far_below_the_largest_still_count(hb):
     """With uniform 0 the first token of any weight is the answer, down to 2^-1000 of the largest and not below."""
     x = torch.full((3, 1, 900), -float("inf"))

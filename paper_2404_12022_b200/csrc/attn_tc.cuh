@@ -409,10 +409,10 @@ __device__ __forceinline__ void stage_tree_positions(const ScoreParams &p, float
 template <int kShape, bool kTree>
 __device__ __forceinline__ void shape_scores(const ScoreParams &p, float *x, int key0, int L, const TreeKeys &tk, const RowShape &row, float add) {
     const bool tree = kTree && key0 + 32 > L;
-    // the bias, less the row's own position: linear in the key for context keys
+    // The bias: linear in the key for context keys; in a run with tree keys each key's is formed from its distance below.
     const float slope = (kShape & kShapeBias) && !tree ? row.slope : 0.f;
     float first = add;
-    if (kShape & kShapeBias) first = fmaf(row.slope, (tree ? 0.f : (float)(key0 - L)) - row.from_len, add);
+    if (kShape & kShapeBias) first = tree ? 0.f : fmaf(row.slope, (float)(key0 - L) - row.from_len, add);
     const unsigned long long slope2 = pack_f32x2(slope, slope), first2 = pack_f32x2(first, first);
     auto rest = [&](int c) {                                 // what is added to the (capped) scores of keys c and c + 1
         return (kShape & kShapeBias) ? fma_f32x2(slope2, pack_f32x2((float)c, (float)(c + 1)), first2) : first2;
@@ -437,9 +437,15 @@ __device__ __forceinline__ void shape_scores(const ScoreParams &p, float *x, int
     if (tree) {
         const int cc0 = key0 - L;                            // tree index of the first key, above -32
         if (kShape & kShapeBias) {
+            // The distance first: both positions may lie far from the context's end (a tree behind rows that were dropped from
+            // the cache), and the products of each with the slope, taken one after the other, would leave their rounding.
             const float *pos = tk.pos + min(cc0, tk.N);       // (wholly behind the tree: masked)
+            const unsigned long long own2 = pack_f32x2(-row.from_len, -row.from_len), per2 = pack_f32x2(row.slope, row.slope), add2 = pack_f32x2(add, add);
 #pragma unroll
-            for (int c = 0; c < 32; ++c) x[c] = fmaf(row.slope, pos[c], x[c]);
+            for (int c = 0; c < 32; c += 2) {
+                const unsigned long long away = add_f32x2(pack_f32x2(pos[c], pos[c + 1]), own2);
+                unpack_f32x2(add_f32x2(pack_f32x2(x[c], x[c + 1]), fma_f32x2(per2, away, add2)), x[c], x[c + 1]);
+            }
         }
         const int wi = cc0 >> 5, sh = cc0 & 31;              // arithmetic shift: -1 for cc0 in (-32, 0)
         const uint32_t lo = wi < 0 ? 0xFFFFFFFFu : (wi < tk.words ? tk.anc[wi * kRows] : 0u);

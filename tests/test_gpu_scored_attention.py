@@ -241,3 +241,19 @@ def test_binding_refuses_what_it_cannot_pass_on(hb):
         hb.tree_attention_scored(q, k, v, lens, parent, slopes=slopes, pos=pos[:, :2])
     with pytest.raises(hb.HtError):
         hb.tree_attention_scored(q, k, v, lens, parent, cap=-1.0)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("shape", [(2, 18, 4, 4, 128, [130, 0]), (2, 91, 4, 4, 128, [1000, 64]), (1, 67, 16, 2, 128, [515])],
+                         ids=lambda s: "N%dHq%dHkv%d" % s[1:4])
+@pytest.mark.parametrize("away", [1000000, 70000, -1000000], ids=["far_behind", "behind", "far_ahead"])
+def test_trees_placed_far_from_their_cache_rows(hb, dtype, shape, away):
+    """Positions are given, and need not follow the cache rows: a cache that dropped rows has its tree far behind them, where
+    only the tree's own keys weigh anything (positive slopes) and their distances are small differences of large positions.
+    Far ahead (negative distances, a slope of 2^-20) every context key gains about as much."""
+    q, k, v, lens, parent, slopes, pos = case(37, dtype, *shape)
+    if away < 0:
+        slopes = torch.full_like(slopes, 2.0 ** -20)      # the biases stay below two: their rounding is that of a score
+    pos = pos + away
+    check(hb, (q, k, v, lens, parent, slopes, pos), 0.0, True)
+    check(hb, (q, k, v, lens, parent, slopes, pos), 20.0, True)

@@ -1,5 +1,7 @@
 // C ABI of the tree-verify library: argument checks and dispatch.  Declarations and the
 // meaning of every argument are in include/ht.h.
+#include <float.h>
+#include <math.h>
 #include <stdarg.h>
 #include <stdio.h>
 #include <stdlib.h>
@@ -145,10 +147,16 @@ int ht_tree_attention_launches(const ht_attn_desc *user_desc) {
 }
 
 // A call's score descriptor, or null where nothing is to be shaped.
-static int check_score(const ht_score_desc **score) {
+static int check_score(const ht_score_desc **score, const ht_attn_desc *desc) {
     const ht_score_desc *s = *score;
     if (!s) return HT_OK;
-    if (!(s->cap >= 0.f) || s->cap > 1e30f) return fail(HT_ERR_INVALID_ARG, "cap must be finite and not negative");
+    if (!(s->cap >= 0.f) || s->cap > FLT_MAX) return fail(HT_ERR_INVALID_ARG, "cap must be finite and not negative");
+    if (s->cap > 0.f && desc && desc->D > 0) {
+        // squares of products up to cap / scale and of capped scores are formed in 32 bits, and powers of scale / cap up to the tenth
+        const double scale = desc->scale > 0.f ? desc->scale : 1.0 / sqrt((double)desc->D);
+        if (s->cap > 1e18 || s->cap > 1e18 * scale) return fail(HT_ERR_INVALID_ARG, "cap and cap / scale must not exceed 1e18 (0: no cap)");
+        if (scale > 1e4) return fail(HT_ERR_INVALID_ARG, "scale must not exceed 1e4 with a cap");
+    }
     if (s->slopes && !s->pos) return fail(HT_ERR_INVALID_ARG, "slopes need pos");
     if (s->cap == 0.f && !s->slopes) *score = nullptr;
     return HT_OK;
@@ -191,7 +199,7 @@ int ht_tree_attention_scored(const ht_attn_desc *user_desc, const ht_score_desc 
                              const void *v_cache, const int32_t *kv_len, const int32_t *parent, void *out, void *workspace,
                              size_t workspace_bytes, int32_t *status, void *stream) {
     Range range("ht_tree_attention_scored");
-    const int rc = check_score(&score);
+    const int rc = check_score(&score, user_desc);
     if (rc != HT_OK) return rc;
     return tree_attention("ht_tree_attention_scored", user_desc, score, q, k_cache, v_cache, kv_len, parent, out, workspace,
                           workspace_bytes, status, stream);
@@ -247,7 +255,7 @@ int ht_tree_attention_scored_paged(const ht_attn_desc *desc, const ht_paged_desc
                                    const int32_t *parent, void *out, void *workspace, size_t workspace_bytes, int32_t *status,
                                    void *stream) {
     Range range("ht_tree_attention_scored_paged");
-    const int rc = check_score(&score);
+    const int rc = check_score(&score, desc);
     if (rc != HT_OK) return rc;
     return tree_attention_paged("ht_tree_attention_scored_paged", desc, pages, score, q, k_pages, v_pages, block_table, kv_len, parent,
                                 out, workspace, workspace_bytes, status, stream);

@@ -128,3 +128,27 @@ def test_binding_refuses_broadcast_rows_and_caches(hb):
     for B, H in ((2, 1), (1, 2), (2, 2)):
         with pytest.raises(ValueError, match="broadcast"):
             pair(c.expand(B, H, 16, 64))
+
+
+def test_caps_beyond_the_arithmetic_are_refused(hb, ptr):
+    """A capped score is squared in 32 bits on its way, and so is a product up to cap / scale: beyond 1.8e19 that gave NaN."""
+    inv = hb.HT_ERR_INVALID_ARG
+    paged, plain = hb.load().ht_tree_attention_scored_paged, hb.load().ht_tree_attention_scored
+    pages = hb.PagedDesc(16, 4, 8, 0, 0)
+
+    def both(cap, scale, D=128):
+        d = hb.AttnDesc(1, 4, 4, 4, D, 64, hb.HT_BF16, scale, 0, 0, 0, 0)
+        s = hb.ScoreDesc(cap, None, None)
+        # (a call that passes the check stops at the NULL q)
+        a = plain(ctypes.byref(d), ctypes.byref(s), None, ptr, ptr, ptr, ptr, ptr, None, 0, ptr, None), hb.load().ht_last_error_string()
+        b = paged(ctypes.byref(d), ctypes.byref(pages), ctypes.byref(s), None, *[ptr] * 6, ptr, 0, ptr, None), hb.load().ht_last_error_string()
+        assert a[0] == b[0] == inv and (b"NULL" in a[1]) == (b"NULL" in b[1])
+        return b"NULL" in a[1]
+    for cap, scale in ((1.3e19, 0.0), (1e30, 0.0), (1e20, 1e4), (1e17, 1e-2), (1.0, 1e-20), (30.0, 1e5), (30.0, float("inf"))):
+        assert not both(cap, scale), (cap, scale)
+    for cap, scale in ((8e16, 0.0), (1e18, 1.0), (1e8, 0.0), (50.0, 1e-10), (30.0, 1e4), (1e-6, 0.0)):
+        assert both(cap, scale), (cap, scale)
+    d = hb.AttnDesc(1, 4, 4, 4, 128, 64, hb.HT_BF16, 1e6, 0, 0, 0, 0)                  # without a cap any scale passes
+    s = hb.ScoreDesc(0.0, ptr, ptr)
+    assert plain(ctypes.byref(d), ctypes.byref(s), None, ptr, ptr, ptr, ptr, ptr, None, 0, ptr, None) == inv
+    assert b"NULL" in hb.load().ht_last_error_string()

@@ -1057,11 +1057,18 @@ int launch_attn_tc(const ht_attn_desc &d, const void *q, const void *kc, const v
             sp.score_mul = (float)mul;
             sp.cap_log2 = (float)(score->cap * log2e);
             if (mul <= 1000.0) {                     // (beyond, the coefficients leave the range of 32 bits)
-                // Taylor series of tanh
+                // Taylor series of tanh, and how far it is taken: to half the cap, less where a coefficient is so small that its own
+                // rounding (half a step of 2^-149; at most all of it) would move the sum by more than 1e-7 -- at scale 0.088
+                // from caps of 900 on (0.47 of the cap at 1000, 0.2 at 20000).
                 const double a[6] = {1.0, -1.0 / 3.0, 2.0 / 15.0, -17.0 / 315.0, 62.0 / 2835.0, -1382.0 / 155925.0};
-                double power = score->cap * log2e * mul;
-                for (int i = 0; i < 6; ++i, power *= mul * mul) sp.series[i] = (float)(a[i] * power);
-                sp.series_lim = 0.5f;
+                double power = score->cap * log2e * mul, lim = 0.5;
+                for (int i = 0; i < 6; ++i, power *= mul * mul) {
+                    sp.series[i] = (float)(a[i] * power);
+                    const double off = fabs(a[i]) * fmin(1.0, ldexp(1.0, -150) / fmax(fabs(a[i] * power), 1e-300));
+                    if (i > 0) lim = fmin(lim, pow(1e-7 / off, 0.5 / i));
+                    else if (off > 1e-7) lim = -1.0;
+                }
+                sp.series_lim = (float)lim;
             }
         }
         if (score->slopes) {

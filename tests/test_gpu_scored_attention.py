@@ -257,3 +257,26 @@ def test_trees_placed_far_from_their_cache_rows(hb, dtype, shape, away):
     pos = pos + away
     check(hb, (q, k, v, lens, parent, slopes, pos), 0.0, True)
     check(hb, (q, k, v, lens, parent, slopes, pos), 20.0, True)
+
+
+@pytest.mark.parametrize("q0", [87.0, 442.0, 1768.0, 17680.0])
+def test_large_caps_shape_scores_on_either_side_of_half_of_them_alike(hb, q0):
+    """One tile of scores a little above half the cap, one of scores a little below it: their forms must agree to the rounding
+    of 32 bits.  Values of +1 and -1 weigh the two tiles against one another."""
+    L, D = 256, 128
+    cap = 2.0 * 64 * q0 / D ** 0.5                        # 64 products of q0 are half of it: 984 to 200026
+    q, k, v = torch.zeros(1, 1, 1, D), torch.zeros(1, 1, L + 7, D), torch.ones(1, 1, L + 7, D)
+    k[..., :64] = 1.0
+    k[..., :128, 64], k[..., 128:, 64] = 0.002, -0.002
+    v[..., 128:, :] = -1.0
+    q[..., :65] = q0
+    q, k, v = (t.half().cuda() for t in (q, k, v))
+    lens, parent = torch.tensor([L], dtype=torch.int32, device="cuda"), torch.full((1, 1), -1, dtype=torch.int32, device="cuda")
+    out, st = hb.tree_attention_scored(q, k, v, lens, parent, cap=cap)
+    ref, size = so.tree_attention(f64(q), f64(k), f64(v), [L], parent.cpu().numpy(), cap, spread=True)
+    # Beside the bound of `close`: the capped score of a tile is cap - 2 cap / (1 + e^(2t)) with the exponential off by 2^-22 and the
+    # quotient by 2^-23 of themselves, which at t = 1/2 moves it by 2 * 0.27 * (0.73 * 2^-22 + 2^-23) = 1.6e-7 of the cap at most, or by
+    # the rounding of its products, less than 0.4 * 2^-23 = 5e-8 of it; the difference of two scores moves the output by half as much.
+    tol = 2.0 ** -11 * (size + np.abs(ref)) + 2e-5 * size + 2.0 ** -17 + 2.1e-7 * cap
+    got = f64(out)
+    assert (st == 0).all() and (np.abs(got - ref) <= tol).all(), (got[0, 0, 0, 0], ref[0, 0, 0, 0], tol[0, 0, 0, 0])

@@ -542,15 +542,18 @@ struct Sampler {
         return tie_cut(in, prefix, goal - above);
     }
 
-    // Elements ahead of the cut of a running weight, by halving the range of the keys: exact for every distribution, one
-    // pass over the row per step.  For rows whose zone does not fit the list: very many equal tokens, or a cut among
-    // tokens below 2^-32 of the largest.
-    __device__ __noinline__ Cut slow_cut(const Cut in, double goal) {
+    // Cut behind the elements before which less than top_p of the kept weight has come, by halving the range of the keys: exact
+    // for every distribution, one pass over the row per step.  For rows whose zone does not fit the list: very many equal
+    // tokens, or a cut among tokens below 2^-32 of the largest.  The goal is formed from the same 64-bit sum as what it is
+    // compared with (sums of the same terms in the same order, which only grow as terms are added): all of the weight
+    // reaches it.  The total of the passes before has its far tail from 32 bits and may exceed that sum.
+    __device__ __noinline__ Cut slow_cut(const Cut in, float top_p) {
         auto weight_from = [&](unsigned int key) {
             double w = 0.0;
             row.each([&](float x, int i) { if (in.keeps(x, i) && order_key(x) >= key) w += wt(x); });
             return team.sum(block_sum(sm, w));
         };
+        const double goal = (double)top_p * weight_from(0u);
         unsigned int lo = 0, hi = order_key(m);              // the answer: the largest key whose elements at or above it reach the goal
         while (lo < hi) {
             const unsigned int mid = lo + (hi - lo) / 2 + 1;
@@ -559,10 +562,12 @@ struct Sampler {
         }
         const double above = weight_from(lo + 1), each_w = wt(key_value(lo));        // (lo is the key of a finite value)
         // elements equal to it, in index order, are kept while the weight before them is below the goal
-        const double n = each_w > 0.0 ? ceil((goal - above) / each_w) : 1.0;
-        unsigned int ties = n < 1.0 ? 1u : (n > 2.0e9 ? 2000000000u : (unsigned int)n);
-        while (ties > 1 && !(above + (double)(ties - 1) * each_w < goal)) --ties;
-        while (above + (double)ties * each_w < goal && ties < 2000000000u) ++ties;
+        unsigned int ties = 1, most = (unsigned int)row.V;
+        while (ties < most) {
+            const unsigned int mid = ties + (most - ties) / 2;
+            if (above + (double)mid * each_w >= goal) most = mid;
+            else ties = mid + 1;
+        }
         return tie_cut(in, lo, ties);
     }
 
@@ -1167,7 +1172,7 @@ struct Sampler {
                     done = true;
                 }
             }
-            if (!done) cut = slow_cut(cut, goal);
+            if (!done) cut = slow_cut(cut, top_p);
         }
         sum_kept(cut, floor, u == 0.0);
         return locate(cut, floor, u);

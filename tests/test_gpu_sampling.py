@@ -1,4 +1,6 @@
 """Sampling and sampled verification on the GPU against the fp64 oracle: tokens are whole numbers and have to be equal."""
+import math
+
 import numpy as np
 import pytest
 import torch
@@ -345,3 +347,20 @@ def test_binding_refuses_what_it_cannot_pass_on(hb):
     for kw in (dict(u=dev(u)[:1]), dict(u=dev(u).double()), dict(T=torch.ones(3, device="cuda")), dict(k=torch.ones(2, device="cuda")), dict(T=torch.ones(2))):
         with pytest.raises(ValueError):
             hb.sample(x, kw.get("u", dev(u)), kw.get("T"), kw.get("k"))
+
+
+@pytest.mark.parametrize("V,gap", [(1 << 24, 22.22), (1 << 24, 22.7), (1 << 25, 22.5), (1 << 25, 22.67)])
+def test_nuclei_that_end_in_a_far_tail_of_very_many_equal_tokens(hb, V, gap):
+    """One token, and V - 1 equal ones below 2^-32 of it that together weigh as much as 0.2 to 0.8 % of it; the nucleus leaves
+    2^-24 of the whole out.  Where the whole is a 32-bit sum, its rounding is more than that: no token would end the nucleus.
+    The last kept token (uniform = 1) is known in closed form."""
+    x = torch.full((1, 1, V), -gap, device="cuda")
+    x[0, 0, V // 2] = 0.0
+    p = 1.0 - 2.0 ** -24
+    w = math.exp(float(x[0, 0, 0]))
+    n = (p * (1.0 + (V - 1) * w) - 1.0) / w              # equal tokens before which less than the goal has come: this rounded up
+    assert 0.05 < n % 1 < 0.95                           # (the kernel's weights are good to 1e-12: 0.01 of a token here)
+    last = math.ceil(n) - 1                              # as the index among the equal tokens
+    got, st = hb.sample(x, dev([[1.0]]), None, None, dev([p]))
+    assert st.tolist() == [0] and got.item() == last + (last >= V // 2), (got.item(), last)
+    assert hb.sample(x, dev([[0.5]]), None, None, dev([p]))[0].item() == V // 2

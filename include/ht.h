@@ -454,7 +454,8 @@ int ht_norm_rope_kv_append_paged(const ht_attn_desc *desc /* host */, const ht_h
  *   token        [B, N] int32 out
  *   status       [B] out: HT_STATUS_BAD_PARAM where the temperature is negative, infinite or NaN, top_p or min_p NaN, min_p
  *                above 1 or a uniform number outside [0, 1]; the sequence's tokens are then -1.
- * Weights and their sums are held in 64 bits (weights below 2^-31 of the largest are added up in 32).
+ * Weights and their sums are held in 64 bits (in rows of up to 2^20, weights below 2^-31 of the largest are added up in
+ * 32, which is off by less than 1e-8 of the whole).
  * N is the rows per sequence (1 for plain decoding); V <= 2^30.
  */
 int ht_sample(const void *logits, int dtype, int B, int N, int V, const float *uniform, const float *temperature,

@@ -10,8 +10,10 @@
 // Every filter keeps a prefix of the order, so a kept set is one pair (x, index): the first element left out.
 //
 // The token is a whole number, and the cut of a flat distribution moves all that follows it, so weights and sums are
-// held in 64 bits (relative error about 1e-13; tokens below 2^-31 of the largest, whose sum is below 1e-4 of the whole,
-// are added up in 32): a row's answer does not depend on how its sum was split.  Nothing is added by atomics but counts.
+// held in 64 bits (relative error about 1e-12), whatever the order of a sum.  The tokens below 2^-31 of the largest are
+// added up in 32 in rows of up to 2^20 (kLongTail): all of them weigh V 2^-31 of the whole at most, their sum is off by 2e-5
+// of that (weights 1e-5, as many roundings of 2^-25 as a thread has tokens), and so by 2e-5 V 2^-31 < 1e-8 of the whole: a
+// sixth of the step of a uniform number or a top_p.  Longer rows add them up in 64.  Nothing is added by atomics but counts.
 //
 // A row is split over the blocks of a cluster (one block where the rows fill the GPU by themselves), its slices in
 // shared memory; one read of the logits.  A histogram of the tokens over the logarithm of their weight (1/64 octave per
@@ -36,6 +38,7 @@ constexpr int kBinsPerOctave = 64;
 constexpr int kList = 1024;               // tokens that are sorted at most
 constexpr unsigned int kShort = 128;      // kept sets up to this are sorted whole instead of cut in their zone and walked
 constexpr int kMaxTeam = 8;               // blocks per row
+constexpr int kLongTail = 1 << 20;        // longer rows sum the tokens below 2^-31 of the largest in 64 bits
 
 struct SampleSmem {
     union {
@@ -106,7 +109,8 @@ struct Weights {
         split(x, q, s);
         return ((double)x - m) * c >= -64000.0 ? q * s : 0.0;
     }
-    // the weight of a logit below `low` (under 2^-31 of the largest): their sum is below 1e-4 of the whole, 32 bits are enough
+    // the weight of a logit below `low` (under 2^-31 of the largest) to 1e-5 where it counts: the exponent, -31 to about -60, is
+    // formed from three roundings of 2^-24
     __device__ __forceinline__ float small(float x) const {
         float y;
         asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"((x - m32) * c32));
@@ -792,6 +796,16 @@ struct Sampler {
         return true;
     }
 
+    __device__ __forceinline__ bool long_row() const { return !kStaged && row.V > kLongTail; }     // (rows in shared memory are shorter)
+
+    // Weight of this thread's kept elements below `low`, in 64 bits (for rows longer than kLongTail; out of line: the code of
+    // the pass that all rows take is what has to be short).
+    __device__ __noinline__ double deep_weight(const Cut &in) const {
+        double w = 0.0;
+        row.each([&](float x, int i) { if (x < wt.low && in.keeps(x, i)) w += wt(x); });
+        return w;
+    }
+
     // Counts of the kept elements by bin, summed over the row's blocks in the first one, and (kWeight) their weight.
     // The histogram shares its memory with the list: a barrier of the row lies between the uses.
     // kAll: nothing is cut off yet.
@@ -820,8 +834,15 @@ struct Sampler {
         low = __reduce_add_sync(0xffffffffu, low);
         if ((threadIdx.x & 31) == 0) atomicAdd(&sm.hist[kBins - 1], low);
         double sum = 0.0;
-        if (kWeight) sum = team.sum(block_sum(sm, w + (double)w_low));
-        else team.barrier();
+        if (kWeight) {
+            if (long_row()) {
+                w_low = 0.f;
+                w += deep_weight(in);
+            }
+            sum = team.sum(block_sum(sm, w + (double)w_low));
+        } else {
+            team.barrier();
+        }
         merge_counts();
         return sum;
     }
@@ -924,7 +945,7 @@ struct Sampler {
     __device__ __forceinline__ void sum_kept(const Cut &cut, double floor, bool exact) {
         double mine = 0.0;
         float low = 0.f;
-        if (floor > 0.0 || exact) {
+        if (floor > 0.0 || exact || long_row()) {
             row.each([&](float x, int i) { mine += kept_weight(cut, floor, x, i); });
         } else {
             const float top = fmaxf(wt.low, cut.x);
@@ -1423,6 +1444,7 @@ sample_kernel(const SampleArgs a) {
 
 // Shared memory a block may take beyond its static part (227 KB per SM in all).
 constexpr size_t kSampleDynMax = 227 * 1024 - sizeof(SampleSmem) - 1024;
+static_assert(kSampleDynMax / sizeof(__nv_bfloat16) * kMaxTeam <= kLongTail, "rows in shared memory sum the far tail in 32 bits");
 
 template <typename T, bool kStaged, bool kTeam, bool kVerify>
 static cudaError_t launch_shape(const SampleArgs &a, int team, size_t smem, cudaStream_t s) {

@@ -364,3 +364,28 @@ def test_nuclei_that_end_in_a_far_tail_of_very_many_equal_tokens(hb, V, gap):
     got, st = hb.sample(x, dev([[1.0]]), None, None, dev([p]))
     assert st.tolist() == [0] and got.item() == last + (last >= V // 2), (got.item(), last)
     assert hb.sample(x, dev([[0.5]]), None, None, dev([p]))[0].item() == V // 2
+
+
+@pytest.mark.parametrize("kw", [dict(), dict(p=0.9999), dict(k=1 << 20, p=0.99995), dict(k=(1 << 20) + 7)], ids=lambda k: "_".join(k) or "none")
+@pytest.mark.parametrize("dtype,V,gap", [("f32", 1 << 24, 22.31), ("f16", (1 << 23) + 1, 22.0), ("bf16", (1 << 21) + 3, 21.625)])
+def test_draws_from_a_far_tail_of_very_many_equal_tokens(hb, dtype, V, gap, kw):
+    """As above: the token that a uniform number meets within the tail is known in closed form, and a 32-bit sum of the tail
+    would move it by some tens of tokens or more."""
+    x = torch.full((1, 1, V), -gap, device="cuda").to(DT[dtype])
+    x[0, 0, 0] = 0.0
+    w = math.exp(float(x[0, 0, 1]))
+    n = min(kw.get("k", V), V) - 1                       # equal tokens kept
+    if "p" in kw:
+        p = float(np.float32(kw["p"]))
+        n_p = (p * (1.0 + n * w) - 1.0) / w
+        assert 0.01 < n_p % 1 < 0.99
+        n = math.ceil(n_p)
+    whole = 1.0 + n * w
+    for f in (0.1, 0.5, 0.93):                            # how far into the tail
+        u = float(np.float32((1.0 + f * n * w) / whole))
+        at = (u * whole - 1.0) / w                       # tokens passed when the goal is met
+        while not 0.05 < at % 1 < 0.95:                  # (the kernel's sums are good to 0.01 of a token)
+            u = float(np.nextafter(np.float32(u), np.float32(0)))
+            at = (u * whole - 1.0) / w
+        got, st = hb.sample(x, dev([[u]]), None, dev([kw["k"]], torch.int32) if "k" in kw else None, dev([kw["p"]]) if "p" in kw else None)
+        assert st.tolist() == [0] and got.item() == math.floor(at) + 1, (f, got.item(), at)

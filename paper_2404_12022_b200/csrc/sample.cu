@@ -57,6 +57,7 @@ struct SampleSmem {
         float f;
         unsigned int u;
     } slot[2];                            // what the row's other blocks read, by turns
+    long long value_at;                   // value_cut: the cut's value (its bin; -1: none) and, in the low half, how many of it are kept
     int n_list, n_above, zone_lo, zone_hi, answer, first_thread;
     unsigned int total;
     float cut_x;
@@ -714,27 +715,28 @@ struct Sampler {
             }
             double all, before = block_scan(mine, sm.wsum, &all);
             const double goal = (double)top_p * (all + low);
-            if (threadIdx.x == 0) sm.zone_lo = -1;
+            if (threadIdx.x == 0) sm.value_at = -1;
             __syncthreads();
 #pragma unroll
             for (int q = 0; q < PER; ++q) {
                 const int b = threadIdx.x * PER + q;
+                // (two threads' running sums are rounded apart: both may claim the goal at their border, so the answer is one store)
                 if (b != kSide && before < goal && before + mass[q] >= goal) {
                     // of the equal tokens those before which less than the goal has come
                     const double each_w = value_weight[b], n = ceil((goal - before) / each_w);
                     unsigned int ties = n < 1.0 ? 1u : (n > (double)c[q] ? c[q] : (unsigned int)n);
                     while (ties > 1 && !(before + (double)(ties - 1) * each_w < goal)) --ties;
                     while (ties < c[q] && before + (double)ties * each_w < goal) ++ties;
-                    sm.total = ties;
-                    sm.zone_lo = b;
+                    sm.value_at = ((long long)b << 32) | ties;
                 }
                 before += mass[q];
             }
         }
         team.barrier();
-        const int at = *team.of(&sm.zone_lo, 0);
-        const unsigned int ties = *team.of(&sm.total, 0);
-        if (at < 0) return false;
+        const long long value_at = *team.of(&sm.value_at, 0);
+        if (value_at < 0) return false;
+        const int at = (int)(value_at >> 32);
+        const unsigned int ties = (unsigned int)value_at;
         // kept weights and equal tokens by warp
         double w = 0.0;
         unsigned int equal = 0;

@@ -138,6 +138,7 @@ struct SampleArgs {
     const int32_t *top_k;
     int B, N, R, V;                       // R rows of each sequence's N are sampled
     int32_t *token, *status;              // token [B, N]
+    bool checked;                         // status [B] already says which sequences' parameters and uniform numbers are in range
     // verification (tokens == nullptr: sampling alone)
     const int32_t *tokens, *parent, *root_pred;
     int T, max_path;

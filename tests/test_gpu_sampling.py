@@ -389,3 +389,32 @@ def test_draws_from_a_far_tail_of_very_many_equal_tokens(hb, dtype, V, gap, kw):
             at = (u * whole - 1.0) / w
         got, st = hb.sample(x, dev([[u]]), None, dev([kw["k"]], torch.int32) if "k" in kw else None, dev([kw["p"]]) if "p" in kw else None)
         assert st.tolist() == [0] and got.item() == math.floor(at) + 1, (f, got.item(), at)
+
+
+@pytest.mark.parametrize("N", [2048, 2049, 5000])
+def test_many_rows_and_their_bad_numbers(hb, oracle, N):
+    """Sequences of more rows than every block looks through itself: flagged all the same, by any parameter and by a uniform
+    number anywhere, and only they."""
+    B, V = 6, 24
+    x, u = logits(43, torch.float32, B, N, V)
+    u[1, N - 1], u[2, 0], u[3, N // 2] = 1.5, -1e-9, np.nan
+    T, p = np.full(B, 0.8, np.float32), np.full(B, 0.9, np.float32)
+    T[4] = -1.0
+    want = so.sample(x.double().cpu().numpy(), u.astype(np.float64), np.where(T < 0, 1, T).astype(np.float64), None, p.astype(np.float64))
+    want[1:5] = -1
+    for _ in range(2):
+        got, st = hb.sample(x, dev(u), dev(T), None, dev(p))
+        assert st.tolist() == [0, 7, 7, 7, 7, 0] and np.array_equal(got.cpu().numpy(), want)
+    # the verification looks at the rows of the tree alone
+    rows = N - 1
+    rng = np.random.default_rng(44)
+    tokens, parent = rng.integers(0, V, (B, rows)).astype(np.int32), trees(rng, B, rows, N)
+    pred, alen, path, nxt, st = hb.verify_sampled(x, dev(u), dev(tokens, torch.int32), dev(parent, torch.int32), None, dev(T), None, dev(p))
+    assert st.tolist() == [0, 0, 7, 7, 7, 0] and (pred[2:5] == -1).all() and alen[2:5].tolist() == [0, 0, 0] and nxt[2:5].tolist() == [-1] * 3
+    full = np.full((B, N), -1, np.int32)
+    u[1, N - 1] = 0.5
+    full[:, :rows] = so.sample(x.double().cpu().numpy(), u.astype(np.float64), np.where(T < 0, 1, T).astype(np.float64), None, p.astype(np.float64))[:, :rows]
+    good = [0, 1, 5]
+    ref = oracle.accept_scan(tokens[good], parent[good], full[good], None, 8)
+    for g, w in zip((pred, alen, path, nxt, st), (full[good], *ref)):
+        assert np.array_equal(g.cpu().numpy()[good], w)

@@ -14,7 +14,12 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libht.so")
-SOURCES = ["ht_api.cu", "transfer.cu", "transfer_tc.cu", "attn_simt.cu", "attn_tc.cu", "attn_tc_pair.cu", "verify.cu", "compact.cu", "draft.cu", "rope.cu", "norm_rope.cu", "sample.cu", "attn_static.cu"]
+SOURCES = ["ht_api.cu", "transfer.cu", "transfer_tc.cu", "attn_simt.cu", "verify.cu", "compact.cu", "draft.cu", "rope.cu", "norm_rope.cu", "attn_static.cu"]
+# compiled once per shape of the attention scores (plain, capped, biased, both) or per type of the logits: (source, macro, its values)
+SPLIT = [("sample.cu", "HT_SAMPLE_DTYPE", (2, 1, 0)), ("attn_tc_pair.cu", "HT_ATTN_SHAPE", (3, 2, 1, 0)), ("attn_tc.cu", "HT_ATTN_SHAPE", (3, 2, 1, 0))]
+# (source, object, flags), what takes longest first
+UNITS = ([(src, "%s_%d.o" % (src[:-3], i), ["-D%s=%d" % (macro, i)]) for src, macro, values in SPLIT for i in values]
+         + [(src, src[:-3] + ".o", []) for src in SOURCES])
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC", "--expt-relaxed-constexpr"]
 
@@ -30,12 +35,13 @@ def _newest_header() -> float:
     return max(times)
 
 
-def _compile(src: str, verbose: bool) -> str:
-    obj = os.path.join(OBJ, src.replace(".cu", ".o"))
+def _compile(unit, verbose: bool) -> str:
+    src, name, flags = unit
+    obj = os.path.join(OBJ, name)
     path = os.path.join(CSRC, src)
     if os.path.exists(obj) and os.path.getmtime(obj) > max(os.path.getmtime(path), _newest_header()):
         return obj
-    cmd = [_nvcc(), *NVCC_FLAGS, "-c", path, "-o", obj]
+    cmd = [_nvcc(), *NVCC_FLAGS, *flags, "-c", path, "-o", obj]
     if verbose:
         cmd.insert(1, "-Xptxas=-v")
     res = subprocess.run(cmd, capture_output=True, text=True)
@@ -51,8 +57,8 @@ def build(force: bool = False, verbose: bool = False) -> str:
     if force:
         for f in os.listdir(OBJ):
             os.remove(os.path.join(OBJ, f))
-    with concurrent.futures.ThreadPoolExecutor(max_workers=len(SOURCES)) as pool:
-        objs = list(pool.map(lambda s: _compile(s, verbose), SOURCES))
+    with concurrent.futures.ThreadPoolExecutor(max_workers=len(UNITS)) as pool:
+        objs = list(pool.map(lambda u: _compile(u, verbose), UNITS))
     if (not os.path.exists(LIB)) or any(os.path.getmtime(o) > os.path.getmtime(LIB) for o in objs):
         tmp = LIB + ".tmp%d" % os.getpid()
         subprocess.run([_nvcc(), "-shared", "-o", tmp, *objs, "-gencode", "arch=compute_100a,code=sm_100a"],

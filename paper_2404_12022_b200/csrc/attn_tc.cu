@@ -779,6 +779,22 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
     }
 }
 
+}  // namespace tc
+
+template <>
+AttnKernelFn attn_tc_form<HT_ATTN_SHAPE>(int form) {
+    constexpr int kShape = HT_ATTN_SHAPE;
+    static const AttnKernelFn fns[kAttnForms] = {
+        tc::attn_tc_kernel<false, false, false, kShape>, tc::attn_tc_kernel<true, false, false, kShape>,
+        tc::attn_tc_kernel<false, true, false, kShape>,  tc::attn_tc_kernel<true, true, false, kShape>,
+        tc::attn_tc_kernel<false, false, true, kShape>,  tc::attn_tc_kernel<true, false, true, kShape>,
+        tc::attn_tc_kernel<false, true, true, kShape>,   tc::attn_tc_kernel<true, true, true, kShape>};
+    return fns[form];
+}
+
+#if HT_ATTN_SHAPE == 0
+namespace tc {
+
 // What must be zero when the attention kernel starts: the units' arrival counters (and, for a paged cache, the
 // status words).  A kernel rather than a memset node so that the launches can be chained by programmatic stream
 // serialization: this one is in place, waiting, before the previous kernel of the stream has finished, and the
@@ -905,17 +921,6 @@ size_t attn_tc_workspace(const ht_attn_desc &d) {
     return ticket_bytes(d) + (size_t)2 * sm_count() * (pair_mode(d) ? 2 : 1) * tc::kSlotFloats * sizeof(float);
 }
 
-typedef void (*AttnKernelFn)(const CUtensorMap, const CUtensorMap, const CUtensorMap, const tc::Params, const tc::PagedParams, const tc::ScoreParams);
-constexpr int kAttnForms = 32;             // bf16, paged, clustered, then the shape of the scores
-template <int kShape>
-static AttnKernelFn attn_tc_form(int form) {
-    static const AttnKernelFn fns[8] = {
-        tc::attn_tc_kernel<false, false, false, kShape>, tc::attn_tc_kernel<true, false, false, kShape>,
-        tc::attn_tc_kernel<false, true, false, kShape>,  tc::attn_tc_kernel<true, true, false, kShape>,
-        tc::attn_tc_kernel<false, false, true, kShape>,  tc::attn_tc_kernel<true, false, true, kShape>,
-        tc::attn_tc_kernel<false, true, true, kShape>,   tc::attn_tc_kernel<true, true, true, kShape>};
-    return fns[form];
-}
 static AttnKernelFn attn_tc_fn(bool bf16, bool paged, bool clustered, int shape = 0) {
     const int form = (bf16 ? 1 : 0) + (paged ? 2 : 0) + (clustered ? 4 : 0);
     switch (shape) {
@@ -936,7 +941,7 @@ static cudaError_t ensure_smem_attr(size_t smem) {
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
     if (dev >= 0 && dev < 64 && done[dev]) return cudaSuccess;
-    for (int i = 0; i < kAttnForms; ++i) {
+    for (int i = 0; i < kAttnForms * kAttnShapes; ++i) {
         const AttnKernelFn fn = attn_tc_fn(i & 1, (i >> 1) & 1, (i >> 2) & 1, i >> 3);
         e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
         if (e != cudaSuccess) return e;
@@ -1159,4 +1164,5 @@ int launch_attn_tc(const ht_attn_desc &d, const void *q, const void *kc, const v
     return HT_OK;
 }
 
+#endif  // HT_ATTN_SHAPE == 0
 }  // namespace ht

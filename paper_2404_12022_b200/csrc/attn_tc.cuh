@@ -1181,4 +1181,24 @@ __device__ __noinline__ void cluster_merge(const Params &p, unsigned char *area,
 }
 
 }  // namespace tc
+
+// The kernels of one shape of the scores, by form: bf16, paged, clustered (pair: several clusters per unit) as bits 0, 1, 2.
+// attn_tc.cu and attn_tc_pair.cu are compiled once per shape, side by side, each time with that shape's kernels alone
+// (HT_ATTN_SHAPE); shape 0 brings the host side.
+#ifndef HT_ATTN_SHAPE
+#define HT_ATTN_SHAPE 0
+#endif
+typedef void (*AttnKernelFn)(const CUtensorMap, const CUtensorMap, const CUtensorMap, const tc::Params, const tc::PagedParams, const tc::ScoreParams);
+constexpr int kAttnForms = 8, kAttnShapes = 4;
+template <int kShape> AttnKernelFn attn_tc_form(int form);
+template <int kShape> AttnKernelFn attn_tc_pair_form(int form);
+template <> AttnKernelFn attn_tc_form<0>(int form);
+template <> AttnKernelFn attn_tc_form<1>(int form);
+template <> AttnKernelFn attn_tc_form<2>(int form);
+template <> AttnKernelFn attn_tc_form<3>(int form);
+template <> AttnKernelFn attn_tc_pair_form<0>(int form);
+template <> AttnKernelFn attn_tc_pair_form<1>(int form);
+template <> AttnKernelFn attn_tc_pair_form<2>(int form);
+template <> AttnKernelFn attn_tc_pair_form<3>(int form);
+
 }  // namespace ht

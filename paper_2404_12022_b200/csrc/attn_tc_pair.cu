@@ -875,22 +875,24 @@ attn_tc_pair_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
 
 }  // namespace tc
 
-typedef void (*PairKernelFn)(const CUtensorMap, const CUtensorMap, const CUtensorMap, const tc::Params, const tc::PagedParams, const tc::ScoreParams);
-template <int kShape>
-static PairKernelFn pair_form(int form) {
-    static const PairKernelFn fns[8] = {
+template <>
+AttnKernelFn attn_tc_pair_form<HT_ATTN_SHAPE>(int form) {
+    constexpr int kShape = HT_ATTN_SHAPE;
+    static const AttnKernelFn fns[kAttnForms] = {
         tc::attn_tc_pair_kernel<false, false, false, kShape>, tc::attn_tc_pair_kernel<true, false, false, kShape>,
         tc::attn_tc_pair_kernel<false, true, false, kShape>,  tc::attn_tc_pair_kernel<true, true, false, kShape>,
         tc::attn_tc_pair_kernel<false, false, true, kShape>,  tc::attn_tc_pair_kernel<true, false, true, kShape>,
         tc::attn_tc_pair_kernel<false, true, true, kShape>,   tc::attn_tc_pair_kernel<true, true, true, kShape>};
     return fns[form];
 }
-static PairKernelFn pair_fn(int form, int shape) {
+
+#if HT_ATTN_SHAPE == 0
+static AttnKernelFn pair_fn(int form, int shape) {
     switch (shape) {
-        case 0: return pair_form<0>(form);
-        case 1: return pair_form<1>(form);
-        case 2: return pair_form<2>(form);
-        default: return pair_form<3>(form);
+        case 0: return attn_tc_pair_form<0>(form);
+        case 1: return attn_tc_pair_form<1>(form);
+        case 2: return attn_tc_pair_form<2>(form);
+        default: return attn_tc_pair_form<3>(form);
     }
 }
 
@@ -898,7 +900,7 @@ static PairKernelFn pair_fn(int form, int shape) {
 int launch_attn_tc_pair_kernel(const CUtensorMap &tm_q, const CUtensorMap &tm_k, const CUtensorMap &tm_v, const tc::Params &p,
                                const tc::PagedParams &pp, const tc::ScoreParams &sp, bool bf16, bool paged, int shape, cudaStream_t s) {
     const int form = (bf16 ? 1 : 0) + (paged ? 2 : 0) + (p.cluster_split > 1 ? 4 : 0);
-    const PairKernelFn fn = pair_fn(form, shape);
+    const AttnKernelFn fn = pair_fn(form, shape);
     static bool done[64];
     const size_t smem_max = sizeof(tc::PSmem) + 1024;
     const size_t smem = offsetof(tc::PSmem, anc) + (size_t)2 * ((p.N + 31) / 32) * tc::kRows * sizeof(uint32_t) + 1024;
@@ -906,7 +908,7 @@ int launch_attn_tc_pair_kernel(const CUtensorMap &tm_q, const CUtensorMap &tm_k,
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return fail(HT_ERR_CUDA, "cudaGetDevice: %s", cudaGetErrorString(e));
     if (!(dev >= 0 && dev < 64 && done[dev])) {
-        for (int i = 0; i < 32 && e == cudaSuccess; ++i) {
+        for (int i = 0; i < kAttnForms * kAttnShapes && e == cudaSuccess; ++i) {
             e = cudaFuncSetAttribute(pair_fn(i & 7, i >> 3), cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_max);
             if (e == cudaSuccess) e = cudaFuncSetAttribute(pair_fn(i & 7, i >> 3), cudaFuncAttributeNonPortableClusterSizeAllowed, 1);   // clusters of 16
         }
@@ -936,4 +938,5 @@ int launch_attn_tc_pair_kernel(const CUtensorMap &tm_q, const CUtensorMap &tm_k,
     return HT_OK;
 }
 
+#endif  // HT_ATTN_SHAPE == 0
 }  // namespace ht

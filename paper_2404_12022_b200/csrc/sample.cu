@@ -24,6 +24,8 @@
 // Bound by instructions per token (30 to 50 per pass and token, a third of them 64-bit) and, for few long rows, by the
 // chain of a cluster's steps, not by HBM: 4 x 32000 in bf16 13 us, 256 x 32003 in fp16 26 us, 64 x 131072 in fp32 97 us
 // (top-p), 4096 x 32000 in bf16 439 us (top-p).
+//
+// Compiled once per type of the logits (HT_SAMPLE_DTYPE, the number of the type), side by side; fp32 brings the entry.
 #include <float.h>
 #include <limits.h>
 
@@ -76,9 +78,9 @@ __device__ __forceinline__ float key_value(unsigned int k) {
 // In constant memory, where an instruction reads them as operands (as literals each would be put together in two
 // registers first, for every token anew).
 constexpr double kLn2By64 = 0.693147180559945309417 / 64.0;
-__constant__ double kSeries[5] = {1.0, kLn2By64, kLn2By64 *kLn2By64 / 2.0, kLn2By64 *kLn2By64 *kLn2By64 / 6.0,
+static __constant__ double kSeries[5] = {1.0, kLn2By64, kLn2By64 *kLn2By64 / 2.0, kLn2By64 *kLn2By64 *kLn2By64 / 6.0,
                                   kLn2By64 *kLn2By64 *kLn2By64 *kLn2By64 / 24.0};
-__constant__ double kMagicC = 6755399441055744.0 + (1 << 30);      // 1.5 * 2^52 + the bias below: adding it rounds to a whole number
+static __constant__ double kMagicC = 6755399441055744.0 + (1 << 30);      // 1.5 * 2^52 + the bias below: adding it rounds to a whole number
 
 // Weight of a logit.  exp(d / T) = 2^(t / 64) with t = 64 log2(e) d / T.  k = t rounded is the token's bin (its distance
 // to the largest in 1/64 octaves) and leaves |r| <= 1/2: k = 64 n + i, a table of 2^(i / 64), the Taylor series of
@@ -1298,18 +1300,6 @@ __device__ __forceinline__ bool bad_sequence(const SampleArgs &a, int b, float T
     return bad;
 }
 
-// The status words ahead of a call with more than kManyRows rows per sequence, where every block's own look at all of its
-// sequence's uniform numbers would add up to the square of the rows.  One sequence of 1000 tokens in bf16, top-p, by the
-// blocks' own looks / with this kernel: 256 rows 17.3 / 19.2 us, 2048 rows 99.9 / 99.7 us, 32768 rows 1731 / 1484 us.
-constexpr int kManyRows = 2048, kCheckThreads = 1024;
-__global__ void __launch_bounds__(kCheckThreads)
-check_sequences_kernel(const SampleArgs a) {
-    const int b = blockIdx.x;
-    const bool bad = __syncthreads_or(bad_sequence<kCheckThreads>(a, b, a.temperature ? a.temperature[b] : 1.f, a.top_p ? a.top_p[b] : 1.f,
-                                                                  a.min_p ? a.min_p[b] : 0.f));
-    if (threadIdx.x == 0) a.status[blockIdx.x] = bad ? HT_STATUS_BAD_PARAM : HT_STATUS_OK;
-}
-
 template <typename T, bool kStaged, bool kTeam, bool kVerify>
 __global__ void __launch_bounds__(kSampleThreads, 2)
 sample_kernel(const SampleArgs a) {
@@ -1497,7 +1487,7 @@ static cudaError_t launch_shape(const SampleArgs &a, int team, size_t smem, cuda
 }
 
 template <typename T>
-static cudaError_t launch_t(const SampleArgs &a, const char *what, cudaStream_t s) {
+cudaError_t launch_sample_t(const SampleArgs &a, const char *what, cudaStream_t s) {
     // Blocks per row: as many as rows are too few to fill the GPU with, and as many as it takes for the slices to fit
     // shared memory two to an SM.
     const long long rows = (long long)a.B * a.R;
@@ -1517,6 +1507,30 @@ static cudaError_t launch_t(const SampleArgs &a, const char *what, cudaStream_t 
     return team > 1 ? launch_shape<T, true, true, false>(a, team, smem, s) : launch_shape<T, true, false, false>(a, team, smem, s);
 }
 
+#ifndef HT_SAMPLE_DTYPE
+#define HT_SAMPLE_DTYPE 0
+#endif
+#if HT_SAMPLE_DTYPE == 1
+template cudaError_t launch_sample_t<__half>(const SampleArgs &, const char *, cudaStream_t);
+#elif HT_SAMPLE_DTYPE == 2
+template cudaError_t launch_sample_t<__nv_bfloat16>(const SampleArgs &, const char *, cudaStream_t);
+#else
+static_assert(HT_F32 == 0 && HT_F16 == 1 && HT_BF16 == 2, "the numbers of the types");
+extern template cudaError_t launch_sample_t<__half>(const SampleArgs &, const char *, cudaStream_t);
+extern template cudaError_t launch_sample_t<__nv_bfloat16>(const SampleArgs &, const char *, cudaStream_t);
+
+// The status words ahead of a call with more than kManyRows rows per sequence, where every block's own look at all of its
+// sequence's uniform numbers would add up to the square of the rows.  One sequence of 1000 tokens in bf16, top-p, by the
+// blocks' own looks / with this kernel: 256 rows 17.3 / 19.2 us, 2048 rows 99.9 / 99.7 us, 32768 rows 1731 / 1484 us.
+constexpr int kManyRows = 2048, kCheckThreads = 1024;
+__global__ void __launch_bounds__(kCheckThreads)
+check_sequences_kernel(const SampleArgs a) {
+    const int b = blockIdx.x;
+    const bool bad = __syncthreads_or(bad_sequence<kCheckThreads>(a, b, a.temperature ? a.temperature[b] : 1.f, a.top_p ? a.top_p[b] : 1.f,
+                                                                  a.min_p ? a.min_p[b] : 0.f));
+    if (threadIdx.x == 0) a.status[blockIdx.x] = bad ? HT_STATUS_BAD_PARAM : HT_STATUS_OK;
+}
+
 int launch_sample(const SampleArgs &args, int dtype, const char *what, cudaStream_t s) {
     SampleArgs a = args;
     a.checked = a.R > kManyRows;
@@ -1527,9 +1541,9 @@ int launch_sample(const SampleArgs &args, int dtype, const char *what, cudaStrea
     }
     cudaError_t e;
     switch (dtype) {
-        case HT_F32: e = launch_t<float>(a, what, s); break;
-        case HT_F16: e = launch_t<__half>(a, what, s); break;
-        default: e = launch_t<__nv_bfloat16>(a, what, s); break;
+        case HT_F32: e = launch_sample_t<float>(a, what, s); break;
+        case HT_F16: e = launch_sample_t<__half>(a, what, s); break;
+        default: e = launch_sample_t<__nv_bfloat16>(a, what, s); break;
     }
     if (e != cudaSuccess) {
         cudaGetLastError();
@@ -1537,5 +1551,6 @@ int launch_sample(const SampleArgs &args, int dtype, const char *what, cudaStrea
     }
     return HT_OK;
 }
+#endif  // HT_SAMPLE_DTYPE
 
 }  // namespace ht

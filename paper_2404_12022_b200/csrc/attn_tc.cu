@@ -934,15 +934,17 @@ static AttnKernelFn attn_tc_fn(bool bf16, bool paged, bool clustered, int shape 
 // Kernels per call: the attention kernel, and ahead of it the one that zeroes the arrival counters where it is needed.
 int attn_tc_launches(const ht_attn_desc &d) { return needs_prepare(d, false) ? 2 : 1; }
 
-// The kernels' dynamic shared memory limit is raised once per device.
-static cudaError_t ensure_smem_attr(size_t smem) {
-    static bool done[64];
+// The dynamic shared memory limit of the kernels of one shape is raised once per device, ahead of the shape's first launch
+// (which loads them: a program whose scores are plain never loads the others).
+static cudaError_t ensure_smem_attr(size_t smem, int shape) {
+    static bool done[64][kAttnShapes];
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
-    if (dev >= 0 && dev < 64 && done[dev]) return cudaSuccess;
-    for (int i = 0; i < kAttnForms * kAttnShapes; ++i) {
-        const AttnKernelFn fn = attn_tc_fn(i & 1, (i >> 1) & 1, (i >> 2) & 1, i >> 3);
+    if (dev >= 0 && dev < 64 && done[dev][shape]) return cudaSuccess;
+    trace("one-tile attention kernels set up: scores %s", shape_name(shape));
+    for (int i = 0; i < kAttnForms; ++i) {
+        const AttnKernelFn fn = attn_tc_fn(i & 1, (i >> 1) & 1, (i >> 2) & 1, shape);
         e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
         if (e != cudaSuccess) return e;
         if ((i >> 2) & 1) {                  // the cluster form may be launched in clusters of 16
@@ -950,7 +952,7 @@ static cudaError_t ensure_smem_attr(size_t smem) {
             if (e != cudaSuccess) return e;
         }
     }
-    if (dev >= 0 && dev < 64) done[dev] = true;
+    if (dev >= 0 && dev < 64) done[dev][shape] = true;
     return cudaSuccess;
 }
 
@@ -977,7 +979,7 @@ static int clusters_fit(int k) {
         attr[0].val.clusterDim.z = 1;
         cfg.attrs = attr;
         cfg.numAttrs = 1;
-        if (ensure_smem_attr(sizeof(tc::Smem) + 1024) != cudaSuccess ||
+        if (ensure_smem_attr(sizeof(tc::Smem) + 1024, 0) != cudaSuccess ||
             cudaOccupancyMaxActiveClusters(&n, attn_tc_fn(true, false, true), &cfg) != cudaSuccess) {
             cudaGetLastError();
             n = 0;
@@ -1137,7 +1139,7 @@ int launch_attn_tc(const ht_attn_desc &d, const void *q, const void *kc, const v
           k > 1 ? (k == 16 ? "clusters of 16" : (k == 8 ? (split == 2 ? "two clusters of 8 per unit" : "clusters of 8") : (k == 4 ? (split == 4 ? "four clusters of 4 per unit" : "clusters of 4") : "clusters of 2"))) : "persistent",
           p.grid, p.early ? ", early start" : "", needs_prepare(d, pages != nullptr) ? ", counters cleared by a kernel" : "");
     if (pair_mode(d)) return launch_attn_tc_pair_kernel(tm_q, tm_k, tm_v, p, pp, sp, d.dtype == HT_BF16, pages != nullptr, shape, s);
-    e = ensure_smem_attr(sizeof(tc::Smem) + 1024);
+    e = ensure_smem_attr(sizeof(tc::Smem) + 1024, shape);
     if (e != cudaSuccess) return fail(HT_ERR_CUDA, "cudaFuncSetAttribute: %s", cudaGetErrorString(e));
     // Few (sequence, KV head) units: one cluster of 16, 8, 4 or 2 CTAs per unit, parts reduced through
     // distributed shared memory; otherwise one persistent CTA per SM.  Either way the launch is serialized

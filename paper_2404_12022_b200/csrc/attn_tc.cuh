@@ -1190,6 +1190,7 @@ __device__ __noinline__ void cluster_merge(const Params &p, unsigned char *area,
 #endif
 typedef void (*AttnKernelFn)(const CUtensorMap, const CUtensorMap, const CUtensorMap, const tc::Params, const tc::PagedParams, const tc::ScoreParams);
 constexpr int kAttnForms = 8, kAttnShapes = 4;
+inline const char *shape_name(int shape) { return shape == 0 ? "plain" : (shape == 1 ? "capped" : (shape == 2 ? "biased" : "capped and biased")); }
 template <int kShape> AttnKernelFn attn_tc_form(int form);
 template <int kShape> AttnKernelFn attn_tc_pair_form(int form);
 template <> AttnKernelFn attn_tc_form<0>(int form);

@@ -896,24 +896,25 @@ static AttnKernelFn pair_fn(int form, int shape) {
     }
 }
 
-// Raises the kernels' dynamic shared memory limit (once per device) and launches.
+// Raises the dynamic shared memory limit of the shape's kernels (once per device) and launches.
 int launch_attn_tc_pair_kernel(const CUtensorMap &tm_q, const CUtensorMap &tm_k, const CUtensorMap &tm_v, const tc::Params &p,
                                const tc::PagedParams &pp, const tc::ScoreParams &sp, bool bf16, bool paged, int shape, cudaStream_t s) {
     const int form = (bf16 ? 1 : 0) + (paged ? 2 : 0) + (p.cluster_split > 1 ? 4 : 0);
     const AttnKernelFn fn = pair_fn(form, shape);
-    static bool done[64];
+    static bool done[64][kAttnShapes];
     const size_t smem_max = sizeof(tc::PSmem) + 1024;
     const size_t smem = offsetof(tc::PSmem, anc) + (size_t)2 * ((p.N + 31) / 32) * tc::kRows * sizeof(uint32_t) + 1024;
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return fail(HT_ERR_CUDA, "cudaGetDevice: %s", cudaGetErrorString(e));
-    if (!(dev >= 0 && dev < 64 && done[dev])) {
-        for (int i = 0; i < kAttnForms * kAttnShapes && e == cudaSuccess; ++i) {
-            e = cudaFuncSetAttribute(pair_fn(i & 7, i >> 3), cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_max);
-            if (e == cudaSuccess) e = cudaFuncSetAttribute(pair_fn(i & 7, i >> 3), cudaFuncAttributeNonPortableClusterSizeAllowed, 1);   // clusters of 16
+    if (!(dev >= 0 && dev < 64 && done[dev][shape])) {
+        trace("tile-pair attention kernels set up: scores %s", shape_name(shape));
+        for (int i = 0; i < kAttnForms && e == cudaSuccess; ++i) {
+            e = cudaFuncSetAttribute(pair_fn(i, shape), cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_max);
+            if (e == cudaSuccess) e = cudaFuncSetAttribute(pair_fn(i, shape), cudaFuncAttributeNonPortableClusterSizeAllowed, 1);   // clusters of 16
         }
         if (e != cudaSuccess) return fail(HT_ERR_CUDA, "cudaFuncSetAttribute: %s", cudaGetErrorString(e));
-        if (dev >= 0 && dev < 64) done[dev] = true;
+        if (dev >= 0 && dev < 64) done[dev][shape] = true;
     }
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)p.grid);

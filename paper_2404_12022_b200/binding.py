@@ -35,7 +35,12 @@ EXPORTS = ("ht_version", "ht_last_error_string", "ht_transfer", "ht_tree_attenti
            "ht_tree_attention_scored", "ht_tree_attention_scored_paged")
 HT_STATIC_SCRATCH_BYTES = 16 << 20
 
-_DTYPES = {torch.float32: HT_F32, torch.float16: HT_F16, torch.bfloat16: HT_BF16}
+class _Dtypes(dict):
+    def __missing__(self, dtype):
+        raise ValueError("%s is not supported: float32, float16 or bfloat16" % (dtype,))
+
+
+_DTYPES = _Dtypes({torch.float32: HT_F32, torch.float16: HT_F16, torch.bfloat16: HT_BF16})
 
 
 class AttnDesc(ctypes.Structure):

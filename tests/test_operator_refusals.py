@@ -152,3 +152,11 @@ def test_caps_beyond_the_arithmetic_are_refused(hb, ptr):
     s = hb.ScoreDesc(0.0, ptr, ptr)
     assert plain(ctypes.byref(d), ctypes.byref(s), None, ptr, ptr, ptr, ptr, ptr, None, 0, ptr, None) == inv
     assert b"NULL" in hb.load().ht_last_error_string()
+
+
+def test_unsupported_types_are_refused_like_all_else(hb):
+    import torch
+    for dtype in (torch.float64, torch.int32, torch.float8_e4m3fn):
+        with pytest.raises(ValueError, match="not supported: float32, float16 or bfloat16"):
+            hb._DTYPES[dtype]
+    assert [hb._DTYPES[t] for t in (torch.float32, torch.float16, torch.bfloat16)] == [hb.HT_F32, hb.HT_F16, hb.HT_BF16]

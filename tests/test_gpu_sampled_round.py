@@ -99,3 +99,78 @@ def test_two_rounds(oracle, ps):
             rows = at[b] + want[1][b, :want[0][b]]
             assert np.array_equal(f64(view(kc))[b, :, at[b]:at[b] + want[0][b]], K[b][:, rows])
         kv_len, root = new_len, nxt
+
+
+@pytest.mark.parametrize("ps", [0, 16], ids=["contiguous", "paged"])
+def test_rounds_leave_every_row_where_it_belongs(ps):
+    """Keys and values alike, the rows ahead of the tree included, and attention held to the bound of its own tests."""
+    if not torch.cuda.is_available():
+        pytest.skip("no CUDA device")
+    from paper_2404_12022_b200 import binding as hb
+    from test_gpu_scored_attention import close
+    dt, B, T, N, Hq, Hkv, D, V, per = torch.float16, 3, 12, 14, 4, 2, 128, 50, 8
+    cap = per * 16
+    g = torch.Generator().manual_seed(78)
+    rnd = lambda *s: torch.randn(s, generator=g).to(dt).cuda()                          # noqa: E731
+    rng = np.random.default_rng(78)
+    parent = np.full((B, N), -1, np.int32)
+    depth = np.zeros((B, N), np.int32)
+    for b in range(B):
+        for r in range(1, N):
+            parent[b, r] = rng.integers(max(0, r - 3), r) if r < T else 2
+            depth[b, r] = depth[b, parent[b, r]] + 1
+    kc, vc = rnd(B, Hkv, cap, D), rnd(B, Hkv, cap, D)
+    table = None
+    if ps:
+        table = torch.randperm(B * per + 1, generator=g)[:B * per].int().view(B, per).cuda()
+        pools = []
+        for t in (kc, vc):
+            pool = torch.zeros((B * per + 1, Hkv, ps, D), dtype=dt, device="cuda")
+            pool[table.long().flatten()] = t.view(B, Hkv, per, ps, D).permute(0, 2, 1, 3, 4).reshape(-1, Hkv, ps, D)
+            pools.append(pool)
+        kc, vc = pools
+    view = (lambda t: t[table.long()].permute(0, 2, 1, 3, 4).reshape(B, Hkv, cap, D)) if ps else (lambda t: t)
+    head = hb.make_head_desc(D)
+    slopes = torch.tensor([0.5, 0.1, 0.02, 0.0], device="cuda")
+    par, kv_len = torch.from_numpy(parent).cuda(), torch.tensor([0, 17, 60], dtype=torch.int32, device="cuda")
+    accept_len = torch.zeros(B, dtype=torch.int32, device="cuda")
+    moved = 0
+    for _ in range(3):
+        at = kv_len.cpu().numpy()
+        pos = torch.from_numpy(at[:, None] + depth).int().cuda()
+        q, k, v = rnd(B, N, Hq, D), rnd(B, N, Hkv, D), rnd(B, N, Hkv, D)
+        before = f64(view(kc)), f64(view(vc))
+        if ps:
+            qo, st = hb.norm_rope_kv_append_paged(q, k, v, pos, kv_len, table, kc, vc, head)
+            out, st2 = hb.tree_attention_scored_paged(qo, kc, vc, table, kv_len, par, cap=25.0, slopes=slopes, pos=pos)
+        else:
+            qo, st = hb.norm_rope_kv_append(q, k, v, pos, kv_len, kc, vc, head)
+            out, st2 = hb.tree_attention_scored(qo, kc, vc, kv_len, par, cap=25.0, slopes=slopes, pos=pos)
+        assert (st == 0).all() and (st2 == 0).all()
+        placed = f64(view(kc)), f64(view(vc))
+        close(out, sc.tree_attention(f64(qo), *placed, at, parent, 25.0, f64(slopes), pos.cpu().numpy(), spread=True))
+        x, u = rnd(B, N, V), torch.rand((B, N), generator=g).cuda()
+        drawn = so.sample(f64(x)[:, :T], f64(u))
+        tokens = rng.integers(0, V, (B, T)).astype(np.int32)
+        for b in range(B):
+            for c in range(1, T):
+                if rng.random() < 0.9:
+                    tokens[b, c] = drawn[b, parent[b, c]]
+        _, alen, path, _, vst = hb.verify_sampled(x, u, torch.from_numpy(tokens).cuda(), par, max_path=12, accept_len=accept_len)
+        if ps:
+            new_len, cst = hb.kv_compact_paged(kc[None], vc[None], table, N, kv_len, alen, path)
+        else:
+            new_len, cst = hb.kv_compact(kc[None], vc[None], N, kv_len, alen, path)
+        assert (vst == 0).all() and (cst == 0).all()
+        n, p = alen.cpu().numpy(), path.cpu().numpy()
+        assert np.array_equal(new_len.cpu().numpy(), at + n)
+        for now, mid, old in zip((f64(view(kc)), f64(view(vc))), placed, before):
+            for b in range(B):
+                L = at[b]
+                moved += (p[b, :n[b]] != np.arange(n[b])).sum()
+                assert np.array_equal(now[b, :, :L], old[b, :, :L])                     # the context
+                assert np.array_equal(now[b, :, L:L + n[b]], mid[b][:, L + p[b, :n[b]]])      # the accepted path behind it
+                assert np.array_equal(now[b, :, L + N:], old[b, :, L + N:])             # rows behind the tree
+        assert np.array_equal(placed[1][0][:, at[0]:at[0] + N], f64(v)[0].swapaxes(0, 1))
+        kv_len = new_len
+    assert moved > 0                                          # (paths that skip nodes have been moved)

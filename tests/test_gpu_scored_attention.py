@@ -280,3 +280,40 @@ def test_large_caps_shape_scores_on_either_side_of_half_of_them_alike(hb, q0):
     tol = 2.0 ** -11 * (size + np.abs(ref)) + 2e-5 * size + 2.0 ** -17 + 2.1e-7 * cap
     got = f64(out)
     assert (st == 0).all() and (np.abs(got - ref) <= tol).all(), (got[0, 0, 0, 0], ref[0, 0, 0, 0], tol[0, 0, 0, 0])
+
+
+@pytest.mark.parametrize("shape", [(1, 18, 4, 4, 128, [40000]), (1, 67, 16, 2, 128, [36001])], ids=["one_tile", "tile_pair"])
+@pytest.mark.parametrize("slope", [2.0 ** -13, 0.01], ids=["flat", "steep"])
+def test_biased_rows_longer_than_two_to_the_fifteenth(hb, shape, slope):
+    """A tile below 2^-40 of the reference is left out: of a part of n keys that is n 2^-40 of the weight at most, 2^-24 here."""
+    c = case(38, "f16", *shape, slope=slope)
+    check(hb, c, 0.0, True)
+    check(hb, c, 20.0, True)
+
+
+@pytest.mark.parametrize("ps", [16, 256])
+@pytest.mark.parametrize("shape", [(2, 18, 4, 4, 128, [900, 0]), (2, 67, 16, 2, 128, [1300, 90]), (5, 19, 16, 16, 128, [600, 20, 900, 333, 128])],
+                         ids=["few", "tile_pair", "many_units"])
+def test_paged_with_the_two_promises(hb, ps, shape):
+    """A kept workspace whose counters reset themselves, and context rows that are final ahead of the call."""
+    c = case(39, "bf16", *shape)
+    q, k, v, lens, parent, slopes, pos = c
+    B, Hkv, cap, D = k.shape
+    per = -(-cap // ps)
+    table = torch.randperm(B * per + 2, generator=torch.Generator().manual_seed(4))[:B * per].int().view(B, per).cuda()
+    pools = []
+    for t in (k, v):
+        full = torch.full((B, Hkv, per * ps, D), float("nan"), dtype=t.dtype, device="cuda")
+        full[:, :, :cap] = t
+        pool = torch.full((B * per + 2, Hkv, ps, D), float("nan"), dtype=t.dtype, device="cuda")
+        pool[table.long().flatten()] = full.view(B, Hkv, per, ps, D).permute(0, 2, 1, 3, 4).reshape(-1, Hkv, ps, D)
+        pools.append(pool)
+    ws = torch.zeros(48 << 20, dtype=torch.uint8, device="cuda")
+    for cap_s, bias in ((30.0, False), (0.0, True), (10.0, True)):
+        ref = reference(c, cap_s, bias)
+        for _ in range(3):
+            out, st = hb.tree_attention_scored_paged(q, *pools, table, lens, parent, cap=cap_s, slopes=slopes if bias else None,
+                                                     pos=pos if bias else None, workspace=ws,
+                                                     flags=hb.HT_ATTN_WORKSPACE_CLEAN | hb.HT_ATTN_CONTEXT_FINAL)
+            assert (st == 0).all()
+            close(out, ref)

@@ -11,8 +11,6 @@ import math
 
 import numpy as np
 
-OK, BAD_LEN, BAD_PAGE = 0, 2, 5
-
 
 def frequencies(rot_dim, base=10000.0, scaling="plain", factor=1.0, low=1.0, high=4.0, orig_len=0.0):
     f = np.array([base ** (-2.0 * i / rot_dim) for i in range(rot_dim // 2)], dtype=np.float64)

@@ -21,7 +21,7 @@ SPLIT = [("sample.cu", "HT_SAMPLE_DTYPE", (2, 1, 0)), ("attn_tc_pair.cu", "HT_AT
 UNITS = ([(src, "%s_%d.o" % (src[:-3], i), ["-D%s=%d" % (macro, i)]) for src, macro, values in SPLIT for i in values]
          + [(src, src[:-3] + ".o", []) for src in SOURCES])
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-              "-Xcompiler", "-fPIC", "--expt-relaxed-constexpr"]
+              "-Xcompiler", "-fPIC", "--expt-relaxed-constexpr", "--compress-mode=size"]
 
 
 def _nvcc() -> str:

@@ -828,18 +828,6 @@ static EncodeTiledFn encode_fn() {
     return fn;
 }
 
-static int sm_count() {
-    static int cached[64];
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 148;
-    if (!cached[dev]) {
-        int n = 0;
-        if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n <= 0) n = 148;
-        cached[dev] = n;
-    }
-    return cached[dev];
-}
-
 bool attn_tc_applicable(const ht_attn_desc &d) {
     if (d.flags & HT_ATTN_FORCE_SIMT) return false;
     if (d.dtype != HT_F16 && d.dtype != HT_BF16) return false;

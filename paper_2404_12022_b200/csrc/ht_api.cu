@@ -70,6 +70,18 @@ int fail(int code, const char *fmt, ...) {
     return code;
 }
 
+int sm_count() {
+    static int cached[64];
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 148;
+    if (!cached[dev]) {
+        int n = 0;
+        if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n <= 0) n = 148;
+        cached[dev] = n;
+    }
+    return cached[dev];
+}
+
 int check_launch(const char *what) {
     const cudaError_t e = cudaPeekAtLastError();
     if (e != cudaSuccess) {

@@ -17,6 +17,7 @@ int check_attn_desc(const ht_attn_desc *d);
 
 // Checks the launch status of the kernel just enqueued.
 int check_launch(const char *what);
+int sm_count();                           // of the current device; asked once per device
 
 // Knobs read once from the environment, for cross-checks and bug reports (never needed for results):
 //   HT_LOG=1                       every entry point prints its arguments and the kernel it chose to stderr

@@ -218,6 +218,8 @@ int ht_tree_attention_paged(const ht_attn_desc *desc /* host */, const ht_paged_
  * where the position of context row j is j and that of tree row c is pos[b,c].
  *   cap      finite, >= 0; neither cap nor cap / scale above 1e18, and with a cap no scale above 1e4 (squares of what lies
  *            in between are held in 32 bits)
+ *            A score is held in 32 bits, its bias included; distances are exact up to 2^24.  Keys that weigh less than 2^-40 of
+ *            a row's largest may be left out.
  *   slopes   [Hq] float or NULL; any sign, 0 for a head without a bias
  *   pos      [B, N] int32 position ids of the query rows (ht_draft_tree's `pos`, followed by the pseudo rows'); needed with
  *            slopes.  HT_ATTN_CONTEXT_FINAL says nothing about slopes and pos: the kernel ahead may write them.

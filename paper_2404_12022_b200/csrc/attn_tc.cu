@@ -43,8 +43,9 @@
 //
 //   scored forms       : instantiations whose scores are capped or biased by distance ahead of the
 //                        softmax (ht_tree_attention_scored; the arithmetic and its reasons are at
-//                        shape_scores).  4 x 91 rows on 4096 keys, 54.5 us without: cap 65 us,
-//                        bias 61 us, both 80 us -- the softmax groups, not HBM, set the pace.
+//                        shape_scores).  4 x 91 rows on 4096 keys, 50.7 us without: cap 68 us (121 us
+//                        where scores pass half the cap in most tiles), bias 58 us, both 78 us -- the
+//                        softmax groups, not HBM, set the pace.
 //
 // Every wait on an mbarrier is bounded; when one runs out the CTA raises an abort flag,
 // reports HT_STATUS_TIMEOUT, runs to the end of its control flow without further waiting,
@@ -1071,7 +1072,8 @@ int launch_attn_tc(const ht_attn_desc &d, const void *q, const void *kc, const v
             sp.slopes = score->slopes;
             sp.pos = score->pos;
             // A steep slope leaves a row a handful of keys: the tree's and the context rows right ahead of it.  The rounding
-            // of their weights to 16 bits does not average away, as on tiles with tree keys.
+            // of their weights to 16 bits does not average away, as on tiles with tree keys.  (A cap alone flattens the weights:
+            // context tiles then send them as the plain kernels do, each rounded to 16 bits once.)
             sp.near_keys = tc::kTile;
             sp.from_end = 1;
         }

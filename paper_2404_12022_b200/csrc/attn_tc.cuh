@@ -320,8 +320,8 @@ __device__ __forceinline__ unsigned long long add_f32x2(unsigned long long a, un
 //   - The running maximum needs no shaped maximum: tanh is monotone, so without a bias the maximum is the shaped raw
 //     maximum; with one, the raw maximum and the bias's larger end bound it, and the exact maximum is only formed in tiles
 //     with tree keys and where that bound may raise the reference -- in the first tiles, since a segment's tiles are taken from the nearest keys to
-//     the farthest (p.from_end).  A tile whose bound lies 2^-40 below the reference adds nothing to the 32-bit sum of a
-//     part of up to 2^15 keys: its weights are zero.
+//     the farthest (p.from_end).  A tile whose bound lies 2^-40 below the reference has its weights taken as zero: n such
+//     keys of a part are n 2^-40 of its weight at most, less than the 32-bit sum holds up to 2^16 of them.
 constexpr int kShapeCap = 1, kShapeBias = 2;
 constexpr float kNegligibleLog2 = 40.f;
 // What a row's thread knows about its row, and the coefficients of the tile.

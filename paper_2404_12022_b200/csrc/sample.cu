@@ -21,9 +21,9 @@
 // the whole kept set, where it is small) are sorted by the cluster's first block and the cut is found exactly.  A small
 // top-k needs no weights at all: the k-th largest of the threads' maxima is a lower bound of the k-th largest token.
 // bf16 rows are counted by value instead, which needs no weights per token until the cut is known.
-// Bound by instructions per token (30 to 50 per pass and token, a third of them 64-bit) and, for few long rows, by the
-// chain of a cluster's steps, not by HBM: 4 x 32000 in bf16 13 us, 256 x 32003 in fp16 26 us, 64 x 131072 in fp32 97 us
-// (top-p), 4096 x 32000 in bf16 439 us (top-p).
+// Bound by instructions per token (30 to 50 per pass and token, a third of them 64-bit; at 64 registers, two blocks per SM, with
+// 24 to 126 bytes of spills) and, for few long rows, by the chain of a cluster's steps, not by HBM: 4 x 32000 in bf16 13 us,
+// 256 x 32003 in fp16 26 us, 64 x 131072 in fp32 98 us (top-p), 4096 x 32000 in bf16 436 us (top-p).
 //
 // Compiled once per type of the logits (HT_SAMPLE_DTYPE, the number of the type), side by side; fp32 brings the entry.
 #include <float.h>

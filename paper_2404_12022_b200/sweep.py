@@ -1,6 +1,7 @@
 """Timing sweeps of single entry points, one JSON line per point (the results tables are made from these).
 
   python -m paper_2404_12022_b200.sweep attention --set configs|c5|c5-quick [--paged P] [--only TEXT] [--reps R]
+      [--scores cap|bias|both [--cap C] [--spread S]]
   python -m paper_2404_12022_b200.sweep transfer [--only TEXT] [--reps R]
   python -m paper_2404_12022_b200.sweep step --layers L [--kv KV] [--steps K]      (a small step, for profiler captures)
   python -m paper_2404_12022_b200.sweep peak                                        (copy and read-only streaming rates)
@@ -39,6 +40,21 @@ def sweep_points(which):
     return [wl.config_c5(*p) for p in pts]
 
 
+def shaped_scores(args, q, kv_len, parent):
+    """The scored entry points' arguments for --scores: the cap, and slopes 2^(-8 (h + 1) / heads) with the rows' positions."""
+    import torch
+    kw = {"cap": args.cap if args.scores in ("cap", "both") else 0.0}
+    if args.scores in ("bias", "both"):
+        par = parent.cpu().tolist()
+        depth = [[0] * len(row) for row in par]
+        for b, row in enumerate(par):
+            for r, p in enumerate(row):
+                depth[b][r] = depth[b][p] + 1 if p >= 0 else 0
+        kw["pos"] = (kv_len[:, None] + torch.tensor(depth, device=kv_len.device)).int()
+        kw["slopes"] = torch.tensor([2.0 ** (-8.0 * (h + 1) / q.shape[2]) for h in range(q.shape[2])], device=q.device)
+    return kw
+
+
 def run_attention(args):
     """CUDA-event time of ht_tree_attention per call, replayed from a CUDA graph of `reps` calls
     that rotate over enough copies of the cache to exceed twice the L2 (cold-L2 protocol)."""
@@ -50,7 +66,10 @@ def run_attention(args):
     l2 = torch.cuda.get_device_properties(0).L2_cache_size
     for w in [x for x in sweep_points(args.set) if args.only in x.name]:
         inp = wl.make_inputs(w, "cuda", with_logits=False, with_transfer=False, layers=[w.layers - 1])
-        q, kv_len, parent = inp.q[0], inp.kv_len, inp.parent
+        q, kv_len, parent = (inp.q[0] * args.spread).to(inp.q[0].dtype), inp.kv_len, inp.parent
+        plain = args.scores == "plain"
+        kw = {} if plain else shaped_scores(args, q, kv_len, parent)
+        attend, attend_paged = (hb.tree_attention, hb.tree_attention_paged) if plain else (hb.tree_attention_scored, hb.tree_attention_scored_paged)
         e = w.elem_bytes()
         cache_bytes = 2 * inp.k_cache[0].numel() * e
         nbuf = int(min(64, max(2, -(-2 * l2 // cache_bytes))))
@@ -66,8 +85,7 @@ def run_attention(args):
         # decoding loop can promise
         clean = hb.HT_ATTN_WORKSPACE_CLEAN | hb.HT_ATTN_CONTEXT_FINAL
         reps = args.reps or max(nbuf, 16)
-        call = lambda i: hb.tree_attention(q, ks[i % nbuf], vs[i % nbuf], kv_len, parent, out=out, workspace=ws, status=st,
-                                           flags=clean)
+        call = lambda i: attend(q, ks[i % nbuf], vs[i % nbuf], kv_len, parent, out=out, workspace=ws, status=st, flags=clean, **kw)
         if args.paged:
             ps = args.paged
             B, Hkv, cap, D = ks[0].shape
@@ -82,8 +100,8 @@ def run_attention(args):
                 return pool
             ks = [to_pool(c) for c in ks]
             vs = [to_pool(c) for c in vs]
-            call = lambda i: hb.tree_attention_paged(q, ks[i % nbuf], vs[i % nbuf], table, kv_len, parent, out=out,
-                                                     workspace=ws, status=st, flags=hb.HT_ATTN_CONTEXT_FINAL)
+            call = lambda i: attend_paged(q, ks[i % nbuf], vs[i % nbuf], table, kv_len, parent, out=out, workspace=ws, status=st,
+                                          flags=hb.HT_ATTN_CONTEXT_FINAL, **kw)
         for i in range(3):
             call(i)
         torch.cuda.synchronize()
@@ -109,7 +127,8 @@ def run_attention(args):
                           "hbm_gbs": round(byts / us / 1e3, 1), "frac_of_measured_hbm": round(byts / us / 1e3 / peak, 3),
                           "frac_of_8tbs": round(byts / us / 1e3 / 8000.0, 3), "tflops": round(flops / us / 1e6, 1),
                           "flop_per_byte": round(flops / byts, 1), "cold_l2_copies": nbuf,
-                          "cache": ("pages of %d rows" % args.paged) if args.paged else "contiguous"}), flush=True)
+                          "cache": ("pages of %d rows" % args.paged) if args.paged else "contiguous", "scores": args.scores,
+                          **({"cap": kw["cap"], "query_std": args.spread} if not plain else {})}), flush=True)
         del ks, vs, inp, ws, graph
 
 
@@ -222,6 +241,9 @@ def main():
     a.add_argument("--set", default="configs", choices=["configs", "c5", "c5-quick"])
     a.add_argument("--paged", type=int, default=0, help="the cache cut into pages of this many rows, placed in a seeded random "
                    "order in a pool (ht_tree_attention_paged)")
+    a.add_argument("--scores", default="plain", choices=["plain", "cap", "bias", "both"], help="scores capped or biased by distance (the scored entry points)")
+    a.add_argument("--cap", type=float, default=30.0)
+    a.add_argument("--spread", type=float, default=1.0, help="factor on the queries: the scores' standard deviation")
     a.add_argument("--only", default="", help="keep the workloads whose name contains this text")
     a.add_argument("--reps", type=int, default=0, help="calls per graph (small captures)")
     t = sub.add_parser("transfer")

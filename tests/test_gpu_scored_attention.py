@@ -317,3 +317,32 @@ def test_paged_with_the_two_promises(hb, ps, shape):
                                                      flags=hb.HT_ATTN_WORKSPACE_CLEAN | hb.HT_ATTN_CONTEXT_FINAL)
             assert (st == 0).all()
             close(out, ref)
+
+
+@pytest.mark.parametrize("shape", [(3, 18, 4, 4, 128, [130, 200, 90]), (3, 67, 16, 2, 128, [515, 300, 90])], ids=["one_tile", "tile_pair"])
+def test_paged_bad_pages_and_lengths_are_flagged_alone(hb, shape):
+    c = case(40, "bf16", *shape)
+    q, k, v, lens, parent, slopes, pos = c
+    B, Hkv, cap, D = k.shape
+    ps = 16
+    per = -(-cap // ps)
+    table = torch.arange(B * per, dtype=torch.int32, device="cuda").view(B, per).contiguous()
+    pools = []
+    for t in (k, v):
+        full = torch.zeros((B, Hkv, per * ps, D), dtype=t.dtype, device="cuda")
+        full[:, :, :cap] = t
+        pools.append(full.view(B, Hkv, per, ps, D).permute(0, 2, 1, 3, 4).reshape(-1, Hkv, ps, D).contiguous())
+    for kw in (dict(cap=10.0), dict(slopes=slopes, pos=pos), dict(cap=10.0, slopes=slopes, pos=pos)):
+        ref = reference(c, kw.get("cap", 0.0), "slopes" in kw)
+        for page in (-1, B * per, 2 ** 30):
+            bad = table.clone()
+            bad[1, 3] = page
+            bad[2, -1] = page                                  # behind the sequence's last row: not needed
+            out, st = hb.tree_attention_scored_paged(q, *pools, bad, lens, parent, **kw)
+            assert st.tolist() == [0, hb.HT_STATUS_BAD_PAGE, 0]
+            close(out[::2], [a[::2] for a in ref])
+        wrong = lens.clone()
+        wrong[0] = per * ps
+        out, st = hb.tree_attention_scored_paged(q, *pools, table, wrong, parent, **kw)
+        assert st.tolist() == [2, 0, 0]
+        close(out[1:], [a[1:] for a in ref])

@@ -219,7 +219,9 @@ int ht_tree_attention_paged(const ht_attn_desc *desc /* host */, const ht_paged_
  *   cap      finite, >= 0; neither cap nor cap / scale above 1e18, and with a cap no scale above 1e4 (squares of what lies
  *            in between are held in 32 bits)
  *            A score is held in 32 bits, its bias included; distances are exact up to 2^24.  Keys that weigh less than 2^-40 of
- *            a row's largest may be left out.
+ *            a row's largest may be left out.  As in the two entry points, a 16-bit call's weights are rounded to its type for
+ *            the product with V, but as a pair of two such values where a row may see few keys: in tiles with tree rows and,
+ *            with slopes, in those of the last 128 context rows.
  *   slopes   [Hq] float or NULL; any sign, 0 for a head without a bias
  *   pos      [B, N] int32 position ids of the query rows (ht_draft_tree's `pos`, followed by the pseudo rows'); needed with
  *            slopes.  HT_ATTN_CONTEXT_FINAL says nothing about slopes and pos: the kernel ahead may write them.

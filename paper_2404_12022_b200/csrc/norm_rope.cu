@@ -14,9 +14,9 @@
 // fraction to 32 (a position of a hundred thousand leaves a 32-bit product no low bits); products and sums in 32 bits,
 // one rounding to the type.
 //
-// 8 x 2048 rows of 80 heads in bf16 (671 MB): 141 us = 4.8 TB/s, 0.72 of the measured copy rate; the instructions of 16
+// 8 x 2048 rows of 80 heads in bf16 (671 MB): 142 us = 4.7 TB/s, 0.72 of the measured copy rate; the instructions of 16
 // values per lane and head (about 250 per warp and head group) are what is left.  One row per block took 203 us (the
-// chain position -> angle -> table -> heads once per row), one barrier per row 157 us.  1 x 91 rows of 96 heads: 4.2 us.
+// chain position -> angle -> table -> heads once per row), one barrier per row 157 us.  1 x 91 rows of 96 heads: 4.3 us.
 #include <math.h>
 
 #include "ht_common.cuh"

@@ -542,6 +542,11 @@ def _pair(k: torch.Tensor, v: torch.Tensor, dev: int, dtype, name: str):
     return shape, strides
 
 
+def _new_status(B: int, N: int, device) -> torch.Tensor:
+    """Status words for a call of N rows per sequence; one without rows writes none, and leaves nothing to report."""
+    return (torch.empty if N else torch.zeros)(B, dtype=torch.int32, device=device)
+
+
 def _place_args(q_in, k_in, v_in, pos, kv_len, head, q_weight, k_weight, q_out):
     B, N, Hq, D = q_in.shape
     dtype, dev = q_in.dtype, _device_of(q_in, "q_in")
@@ -560,7 +565,7 @@ def _place_args(q_in, k_in, v_in, pos, kv_len, head, q_weight, k_weight, q_out):
     if q_out is None:
         q_out = torch.empty((B, N, Hq, D), dtype=dtype, device=q_in.device)
     _dense(q_out, dev, dtype, (B, N, Hq, D), "q_out")
-    return head, q_out, torch.empty(B, dtype=torch.int32, device=q_in.device), Hkv, dev
+    return head, q_out, _new_status(B, N, q_in.device), Hkv, dev
 
 
 def norm_rope_kv_append(q_in, k_in, v_in, pos, kv_len, k_cache, v_cache, head: HeadDesc, q_weight=None, k_weight=None, q_out=None):
@@ -627,7 +632,7 @@ def sample(logits, uniform, temperature=None, top_k=None, top_p=None, min_p=None
         token = torch.empty((B, N), dtype=torch.int32, device=device)
     else:
         _dense(token, dev, torch.int32, (B, N), "token")
-    status = torch.empty(B, dtype=torch.int32, device=device)
+    status = _new_status(B, N, device)
     _check(load().ht_sample(logits.data_ptr(), _DTYPES[logits.dtype], B, N, V, uniform.data_ptr(), _ptr(temperature), _ptr(top_k),
                             _ptr(top_p), _ptr(min_p), token.data_ptr(), status.data_ptr(), _stream()))
     return token, status
@@ -694,7 +699,7 @@ def _attn_buffers(q, dev, desc, out, workspace, status):
             raise ValueError("workspace must be a contiguous CUDA tensor of device %d" % dev)
         ws, ws_bytes = workspace, workspace.numel() * workspace.element_size()
     if status is None:
-        status = torch.empty(q.shape[0], dtype=torch.int32, device=q.device)
+        status = _new_status(q.shape[0], q.shape[1], q.device)
     else:
         _dense(status, dev, torch.int32, q.shape[:1], "status")
     return out, ws, ws_bytes, status

@@ -447,6 +447,8 @@ __device__ __forceinline__ float scores_weights(uint32_t addr, const float *fact
 
 // Merge of the parts of a cut unit by the 512 softmax threads of the CTA that delivered the last part: four threads to a row, 32
 // features each, 16 at a time, so that the loads of several parts are on their way together within the kernel's 80 registers.
+// Which CTA comes last, and whether the last of two finishes the unit from its accumulators instead, is a matter of timing: the
+// arithmetic is the same, product by product, so that the result is not.
 template <bool kBf16>
 __device__ __noinline__ void merge_parts_q8(const Params &p, const CutUnit &cu, int per, int tid) {
     const int row = tid & 127, quarter = tid >> 7;
@@ -462,7 +464,7 @@ __device__ __noinline__ void merge_parts_q8(const Params &p, const CutUnit &cu, 
         const float *at = part(c) + kRows * kD + row;
         const float m = __ldcg(at), lp = __ldcg(at + kRows), Mn = fmaxf(M, m);
         const float fa = (M == -INFINITY) ? 0.f : exp2f(M - Mn), fb = (m == -INFINITY) ? 0.f : exp2f(m - Mn);
-        l = l * fa + lp * fb;
+        l = fmaf(l, fa, lp * fb);
         M = Mn;
     }
     const float inv = 1.f / l;
@@ -965,8 +967,9 @@ attn_q8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__
             const int xk_sh = clustered ? 5 - __ffs(p.cluster_k) + 1 : 0;
             const uint32_t xrecv = smem_u32(&sm.q[0][0]) + kXchgRecvOffset;
             const float *oslot = pslot;
-            float g0 = f0, g1 = f1, gb = 0.f;
-            if (direct) {
+            float g0 = f0, g1 = f1, w_own = 0.f, w_other = 0.f, inv_two = 0.f;
+            bool own_first = false;
+            if (direct) {                              // merge_parts_q8's arithmetic, this CTA's part straight from the accumulators
                 const CutUnit &cu = cut[cut_k];
                 const int oc = (cu.c_lo == my_pos) ? cu.c_hi : cu.c_lo;
                 oslot = p.part + (size_t)(2 * (oc * group + my_rt) + ((max(cu.t0, oc * per) == oc * per) ? 0 : 1)) * kSlotFloats;
@@ -975,10 +978,10 @@ attn_q8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__
                 const float Mn = fmaxf(M, m_o);
                 const float fa = (M == -INFINITY) ? 0.f : exp2f(M - Mn);
                 const float fb = (m_o == -INFINITY) ? 0.f : exp2f(m_o - Mn);
-                const float inv = 1.f / (l_tot * fa + l_o * fb);
-                g0 *= fa * inv;
-                g1 *= fa * inv;
-                gb = fb * inv;
+                own_first = oc == cu.c_hi;
+                inv_two = 1.f / (own_first ? fmaf(l_tot, fa, l_o * fb) : fmaf(l_o, fb, l_tot * fa));
+                w_own = fa;
+                w_other = fb;
             } else if (complete && !clustered) {
                 const float inv = 1.f / l_tot;
                 g0 *= inv;
@@ -1015,10 +1018,12 @@ attn_q8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__
 #pragma unroll
                         for (int c = 0; c < 4; ++c) {
                             const float4 v = __ldcg(reinterpret_cast<const float4 *>(oslot) + (col0 / 4 + c) * kRows + row);
-                            x[4 * c] = fmaf(gb, v.x, x[4 * c]);
-                            x[4 * c + 1] = fmaf(gb, v.y, x[4 * c + 1]);
-                            x[4 * c + 2] = fmaf(gb, v.z, x[4 * c + 2]);
-                            x[4 * c + 3] = fmaf(gb, v.w, x[4 * c + 3]);
+                            const float other[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                float &mine = x[4 * c + i];
+                                mine = (own_first ? fmaf(other[i], w_other, fmaf(mine, w_own, 0.f)) : fmaf(mine, w_own, fmaf(other[i], w_other, 0.f))) * inv_two;
+                            }
                         }
                     }
                     if (final) {

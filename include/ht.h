@@ -529,7 +529,8 @@ int ht_norm_rope_kv_append_q8_paged(const ht_attn_desc *desc /* host */, const h
  * otherwise off by 2^-17 of that at most), K's codes as they are, their powers of two in fp32; V in fp16 relative to the largest
  * scale among 128 rows, exactly where a row's is not 2^22 times smaller; the weights rounded to fp16 (as a pair of two such
  * values in tiles with tree rows and, with a window, in those of the last 128 context rows).
- * Paged: entries of pages that no row sees (ahead of the window and behind the first tokens) may hold anything, too.
+ * Rows that no row sees (ahead of every row's window and behind the first tokens) may hold anything; paged: so may the entries of
+ * pages of such rows alone.
  */
 typedef struct {
     int32_t window, sinks;

@@ -72,6 +72,7 @@ struct __align__(1024) SmemQ8 {
     float ref_row[2][kRows];                   // the streams' references
     int32_t len[kMaxB], nkt[kMaxB], pre[kMaxB + 1];
     int32_t len_listed[kMaxB];                 // context rows less those of tiles that are not in the list
+    int32_t seen[kMaxB];                       // where the farthest window begins (0: no window)
     int32_t gap_at[kMaxB], gap[kMaxB];         // tiles [gap_at, gap_at + gap) of the sequence are not in the list
     int32_t plan[kPlanWords];
     int32_t row_lo[kRows];                     // first context row that the window shows the row
@@ -130,16 +131,29 @@ __device__ __forceinline__ uint32_t mul_f16x2(uint32_t a, uint32_t b) {
 // 2^e, e in [-126, 127].
 __device__ __forceinline__ float pow2(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
 
-// The exponent that a tile's values are taken relative to, from the scale bytes of its rows (first 4 * lane of this lane's;
-// rows at and behind `valid`, and those marked as no numbers, do not count): `below` less than the largest.  Alike in all lanes
-// of the warp.
-__device__ __forceinline__ int tile_exponent(const unsigned char *scale, int lane, int valid, int below) {
-    const uint32_t w = *reinterpret_cast<const uint32_t *>(scale + 4 * lane);
+// Rows of a tile that hold data: below `valid`, and not in [hide_lo, hide_hi), behind the first tokens and ahead of the farthest
+// window: no row of the sequence sees those, and whatever a spare page holds may lie there.
+struct TileRows {
+    int valid, hide_lo, hide_hi;
+    __device__ __forceinline__ bool all() const { return valid >= kTile && (hide_hi <= 0 || hide_lo >= kTile); }
+    __device__ __forceinline__ bool data(int row) const { return row < valid && !(row >= hide_lo && row < hide_hi); }
+};
+// The bytes of the lane's four rows, 4 * lane and on, that are data.
+__device__ __forceinline__ uint32_t data_bytes(const TileRows &rows, int lane) {
+    uint32_t keep = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) keep |= rows.data(4 * lane + i) ? 255u << (8 * i) : 0u;
+    return keep;
+}
+// The exponent that a tile's values are taken relative to, from the scale bytes of its rows (of this lane's, those in `keep`;
+// rows marked as no numbers do not count): `below` less than the largest.  Alike in all lanes of the warp.
+__device__ __forceinline__ int tile_exponent(const unsigned char *scale, int lane, uint32_t keep, int below) {
+    const uint32_t w = *reinterpret_cast<const uint32_t *>(scale + 4 * lane) & keep;
     uint32_t top = 0;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const uint32_t byte = w >> (8 * i) & 255u;
-        top = max(top, byte != 255u && 4 * lane + i < valid ? byte : 0u);
+        top = max(top, byte != 255u ? byte : 0u);
     }
     top = __reduce_max_sync(0xFFFFFFFFu, top);
     return max((int)top - 127 - below, -100);
@@ -312,13 +326,13 @@ __device__ __forceinline__ void plan_q8(const Params &p, const Q8Params &qp, Sme
         int code = HT_STATUS_OK;
         if (saw_bad) code = HT_STATUS_BAD_TREE;
         if (L < 0 || (long long)L + p.N > p.cap) code = HT_STATUS_BAD_LEN;
-        int n = 0, gap_at = 0, gap = 0;
+        int n = 0, gap_at = 0, gap = 0, seen = 0;
         if (code == HT_STATUS_OK) {
             n = (L + p.N + kTile - 1) / kTile;
             gap_at = n;
             if (qp.window > 0) {
-                // rows that hang off the context see the farthest: from L - window + 1 on
-                const int first = (int)max(0ll, (long long)L - qp.window + 1) / kTile, kept = (int)(((long long)min(qp.sinks, L) + kTile - 1) / kTile);
+                seen = max(L - qp.window + 1, 0);            // rows that hang off the context see the farthest
+                const int first = seen / kTile, kept = (int)(((long long)min(qp.sinks, L) + kTile - 1) / kTile);
                 if (first > kept) {
                     gap_at = kept;
                     gap = first - kept;
@@ -327,6 +341,7 @@ __device__ __forceinline__ void plan_q8(const Params &p, const Q8Params &qp, Sme
             n -= gap;
         }
         sm.len[my_b] = L;
+        sm.seen[my_b] = seen;
         sm.len_listed[my_b] = L - gap * kTile;
         sm.nkt[my_b] = n;
         sm.gap_at[my_b] = gap_at;
@@ -752,16 +767,23 @@ attn_q8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     mbar_arrive(&sm.q_ready[(seg_i - 1) & 3]);
                 }
-                const int valid = sm.len[b] + p.N - tile_of(sm, b, cur.kt()) * kTile;      // rows of the tile that hold keys
+                const int L = sm.len[b], tile0 = tile_of(sm, b, cur.kt()) * kTile;
+                const TileRows rows = {L + p.N - tile0, qp.sinks - tile0, sm.seen[b] - tile0};
                 if (!wait(&sm.k_full[k_slot], k_ph)) break;
+                uint32_t keep = 0xFFFFFFFFu;
+                bool data = true;
+                if (!rows.all()) {
+                    keep = data_bytes(rows, lane);
+                    data = rows.data(row);
+                }
                 const int ek = sm.scale[k_slot][0][row], ev = sm.scale[k_slot][1][row];
                 // K relative to the tile's largest; V seven below it, so that the largest code, 448 * 2^7, lies just within fp16
-                const int ref_k = tile_exponent(sm.scale[k_slot][0], lane, valid, 0), ref_v = tile_exponent(sm.scale[k_slot][1], lane, valid, 7);
+                const int ref_k = tile_exponent(sm.scale[k_slot][0], lane, keep, 0), ref_v = tile_exponent(sm.scale[k_slot][1], lane, keep, 7);
                 mbar_arrive(&sm.k_empty[k_slot]);
                 // A row that is not a number in K or V makes its score so, which reaches the query rows that see it and no other; V's
-                // row is zero then, as the rows behind the tree are (a weight of zero times anything there is zero).
+                // row is zero then, as the rows are that hold no data (a weight of zero times anything there is zero).
                 const bool nan = ek == 255 || ev == 255;
-                next_zero = row >= valid || nan;
+                next_zero = !data || nan;
                 sm.factor[j & 3][row] = nan ? __uint_as_float(0x7FC00000u) : pow2(min(max(ek - 127 - ref_k, -126), 0));
                 if (row == 0) {
                     sm.ref[j & 3][0] = ref_k;

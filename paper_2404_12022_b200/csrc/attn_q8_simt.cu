@@ -118,13 +118,11 @@ attn_q8_simt_kernel(const Params p) {
         constexpr int VPR = D / 16;                    // 16-byte pieces per row
         for (int t = threadIdx.x; t < kKeys * VPR; t += blockDim.x) {
             const int j = t / VPR, v = t - j * VPR, key = k0 + j;
-            if (key < k_end) {
+            if (key < k_end && (key >= first_seen || key < p.sinks)) {        // what no row sees is no data, whatever lies there
                 long long row = (long long)b * p.stride_b + (long long)hk * p.stride_h + (long long)key * D;
                 long long at = (long long)b * p.scale_b + (long long)hk * p.scale_h + key;
                 if (p.pm.table) {
-                    // (a page that no row sees may have no entry: page 0, masked)
-                    int page = p.pm.table[(size_t)b * p.pm.max_pages + (key >> p.pm.shift)];
-                    page = (unsigned)page < (unsigned)p.pm.n_pages ? page : 0;
+                    const int page = p.pm.table[(size_t)b * p.pm.max_pages + (key >> p.pm.shift)];       // inside the pool: looked at above
                     const int in = key & ((1 << p.pm.shift) - 1);
                     row = (long long)page * p.stride_b + (long long)hk * p.stride_h + (long long)in * D;
                     at = (long long)page * p.scale_b + (long long)hk * p.scale_h + in;

@@ -2,7 +2,7 @@
 import pytest
 import torch
 
-from test_gpu_q8_attention import Case, hb  # noqa: F401
+from test_gpu_q8_attention import Case, close, hb  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -19,3 +19,47 @@ def test_a_call_repeats_itself(hb, shape, kw):  # noqa: F811
         out, _ = hb.tree_attention_q8(c.q, c.k, c.v, c.ks, c.vs, lens, par, **more)
         other += (out.view(torch.int16) != first).sum()
     assert int(other) == 0
+
+
+def spare_page(c, unseen):
+    """Page 0 becomes the pool's spare page, full of codes that are no numbers under the largest scale; the entries of pages that
+    `unseen` (sequence, logical page) names point at it, by their number or by one outside the pool."""
+    n = c.k.shape[0]
+    free = sorted(set(range(1, n)) - set(c.table.reshape(-1).tolist()))
+    c.table[c.table == 0] = free[0]
+    c.upload()
+    for t, what in ((c.k, 0x7F), (c.v, 0xFF), (c.ks, 254), (c.vs, 254)):
+        t.view(torch.uint8)[0] = what
+    for i, (b, page) in enumerate(unseen):
+        c.table[b, page] = (0, -1, 1 << 30)[i % 3]
+
+
+@pytest.mark.parametrize("dtype,D", [("bf16", 128), ("f16", 128), ("f32", 64), ("f32", 128), ("bf16", 64)])
+@pytest.mark.parametrize("page", [16, 32, 64])
+@pytest.mark.parametrize("window,sinks", [(100, 5), (33, 0), (257, 130)])
+def test_pages_that_no_row_sees_may_hold_anything(hb, dtype, D, page, window, sinks):  # noqa: F811
+    c = Case(40 + page, dtype, 3, 10, 4, 2, D, (500, 700, 61), page=page)
+    want = c.want(window=window, sinks=sinks)
+    unseen = [(b, i) for b, L in enumerate(c.lens) for i in range(c.table.shape[1])
+              if i * page >= sinks and (i + 1) * page <= L - window + 1 or i * page >= L + 10]
+    assert len(unseen) >= 10
+    spare_page(c, unseen)
+    out, st = c.run(hb, window=window, sinks=sinks)
+    assert st.tolist() == [0] * 3
+    close(out, want)
+
+
+@pytest.mark.parametrize("dtype,D", [("bf16", 128), ("f16", 128), ("f32", 64)])
+def test_rows_that_no_row_sees_may_hold_anything(hb, dtype, D):  # noqa: F811
+    """The rows between the first tokens and the farthest that any window reaches, of pages and of tiles that others see."""
+    for page in (0, 16, 256):
+        for window, sinks in ((100, 5), (300, 0), (20, 140)):
+            c = Case(50 + page, dtype, 2, 20, 4, 2, D, (600, 333), page=page)
+            want = c.want(window=window, sinks=sinks)
+            for b, L in enumerate(c.lens):
+                for x, s in zip(c.codes, c.bytes):
+                    x[b, :, sinks:L - window + 1], s[b, :, sinks:L - window + 1] = 0x7F, 254
+            c.upload()
+            out, st = c.run(hb, window=window, sinks=sinks)
+            assert st.tolist() == [0, 0]
+            close(out, want, (page, window, sinks))

@@ -3,8 +3,8 @@
 //   block = 8 warps, a query row of one head each; 32 keys at a time are staged as fp32 values (code * 2^e), lane j scores
 //   key j, running maximum and sum by shuffles, each lane owns D / 32 output features; with several splits (m, l, O) parts
 //   go to the workspace and a second kernel merges them.
-// Bound by the ALUs: 2 x 32 x D products per row and step against 64 D bytes.  Steps that no row of the block sees (outside
-// the window and behind the first tokens) are jumped over.  1 x 91 rows of 32 heads of 128 on 1024 keys in fp32: 285 us = 5.4 TFLOP/s;
+// Bound by the ALUs: 2 x 32 x D products per row and step against 64 D bytes.  Steps of context rows that no row of the block sees
+// (outside the window and behind the first tokens) are jumped over.  1 x 91 rows of 32 heads of 128 on 1024 keys in fp32: 285 us = 5.4 TFLOP/s;
 // heads of 64 in bf16 151 us.
 #include "q8.cuh"
 
@@ -94,7 +94,7 @@ attn_q8_simt_kernel(const Params p) {
     const T *qrow = static_cast<const T *>(p.q) + (((size_t)b * N + (row_ok ? r : 0)) * p.Hq + h) * D;
     for (int x = lane; x < D; x += 32) Qs[warp][x] = to_float<T>(qrow[x]);
     __syncthreads();
-    const int block_lo = s_lo;
+    const int block_lo = min(s_lo, L);                 // (tree rows stand where their depth puts them: never jumped over)
 
     const int total = L + N;
     int chunk = (total + p.splits - 1) / p.splits;

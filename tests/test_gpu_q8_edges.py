@@ -1,4 +1,5 @@
 """What the 8-bit attention may be given at its edges, and what a call of it promises."""
+import numpy as np
 import pytest
 import torch
 
@@ -63,3 +64,16 @@ def test_rows_that_no_row_sees_may_hold_anything(hb, dtype, D):  # noqa: F811
             out, st = c.run(hb, window=window, sinks=sinks)
             assert st.tolist() == [0, 0]
             close(out, want, (page, window, sinks))
+
+
+@pytest.mark.parametrize("dtype,D", [("f32", 64), ("f32", 128), ("bf16", 64)])
+@pytest.mark.parametrize("roots,N,L,window,sinks", [(60, 200, 0, 4, 4), (40, 300, 0, 5, 9), (33, 100, 1, 1, 4), (130, 300, 20, 30, 50)])
+def test_first_tokens_within_a_tree(hb, dtype, D, roots, N, L, window, sinks):  # noqa: F811
+    """A row of the tree stands where its depth puts it: behind wide siblings, rows far down the cache are among the first tokens."""
+    parent = np.full((1, N), -1, np.int32)
+    parent[0, roots:] = np.arange(roots - 1, N - 1)                                     # a chain below the last root
+    for page in (0, 16):
+        for kw in (dict(), dict(num_splits=3)):
+            Case(N, dtype, 1, N, 2, 2, D, (L,), page=page, parent=parent).check(hb, "%s %s" % (page, kw), window=window, sinks=sinks, **kw)
+    if dtype == "bf16":                                                                 # the tensor cores
+        Case(N, dtype, 1, N, 2, 2, 128, (L,), parent=parent).check(hb, window=window, sinks=sinks)

@@ -64,8 +64,8 @@ enum {
 
 /* ht_attn_desc.flags */
 #define HT_ATTN_FORCE_SIMT 1u /* use the fp32-ALU kernel even where a tensor-core kernel applies */
-/* The caller vouches that the first 64 KiB of the workspace are as a cudaMemset to zero, or any earlier
- * ht_tree_attention / ht_tree_attention_paged call on this workspace that reported no HT_STATUS_TIMEOUT, left
+/* The caller vouches that the first 64 KiB of the workspace are as a cudaMemset to zero, or any earlier attention
+ * call on this workspace that reported no HT_STATUS_TIMEOUT (whatever its cache, its scores and the kernel it took), left
  * them: the call then leaves out the small kernel that clears the arrival counters kept there (every call
  * leaves the counters it used at zero).  Worth about a microsecond per call in a chain of calls; with the flag
  * set on a workspace that is not in that state, results of sequences whose work was split are undefined

@@ -137,13 +137,20 @@ int ht_transfer(const void *h_src, const void *W, void *out, int B, int k, int d
     return launch_transfer(h_src, W, out, B, k, d, dtype, static_cast<cudaStream_t>(stream));
 }
 
+// A workspace begins with the tensor-core kernels' arrival counters, which a caller may count on being left at zero
+// (HT_ATTN_WORKSPACE_CLEAN): what the ALU kernels keep there lies behind them.
+static const size_t kCounterArea = 64 * 1024;
+static size_t behind_counters(size_t parts) { return parts == 0 ? 0 : kCounterArea + parts; }
+static void *parts_of(void *workspace) { return workspace ? static_cast<unsigned char *>(workspace) + kCounterArea : nullptr; }
+static size_t parts_bytes(size_t workspace_bytes) { return workspace_bytes > kCounterArea ? workspace_bytes - kCounterArea : 0; }
+
 size_t ht_tree_attention_workspace(const ht_attn_desc *desc) {
     if (check_attn_desc(desc) != HT_OK) return 0;
     if (desc->B == 0 || desc->N == 0) return 0;
     // (the maximum over the kernels the descriptor may get, whatever the environment's knobs say)
-    size_t need = attn_simt_workspace(*desc, nullptr);
+    size_t need = behind_counters(attn_simt_workspace(*desc, nullptr));
     const ht_attn_desc k = with_knobs(*desc);
-    const size_t need_k = attn_simt_workspace(k, nullptr);
+    const size_t need_k = behind_counters(attn_simt_workspace(k, nullptr));
     need = need_k > need ? need_k : need;
     if (attn_tc_applicable(*desc)) need = attn_tc_workspace(*desc) > need ? attn_tc_workspace(*desc) : need;
     return (need + 255) / 256 * 256;
@@ -196,7 +203,7 @@ static int tree_attention(const char *what, const ht_attn_desc *user_desc, const
     if (attn_tc_applicable(*desc))
         return launch_attn_tc(*desc, q, k_cache, v_cache, kv_len, parent, out, workspace, workspace_bytes, status,
                               static_cast<cudaStream_t>(stream), nullptr, nullptr, score);
-    return launch_attn_simt(*desc, q, k_cache, v_cache, kv_len, parent, out, workspace, workspace_bytes,
+    return launch_attn_simt(*desc, q, k_cache, v_cache, kv_len, parent, out, parts_of(workspace), parts_bytes(workspace_bytes),
                             status, static_cast<cudaStream_t>(stream), score);
 }
 
@@ -698,8 +705,8 @@ int ht_norm_rope_kv_append_q8_paged(const ht_attn_desc *desc, const ht_head_desc
 static size_t q8_workspace(const ht_attn_desc &d) {
     if (d.B == 0 || d.N == 0) return 0;
     // (the maximum over the kernels the descriptor may get, whatever the environment's knobs say)
-    size_t need = attn_q8_simt_workspace(d, nullptr);
-    const size_t with = attn_q8_simt_workspace(with_knobs(d), nullptr);
+    size_t need = behind_counters(attn_q8_simt_workspace(d, nullptr));
+    const size_t with = behind_counters(attn_q8_simt_workspace(with_knobs(d), nullptr));
     need = with > need ? with : need;
     if (attn_q8_tc_applicable(d)) need = attn_q8_tc_workspace(d) > need ? attn_q8_tc_workspace(d) : need;
     return (need + 255) / 256 * 256;
@@ -727,8 +734,8 @@ static int tree_attention_q8(const char *what, const ht_attn_desc &user, const h
     if (attn_q8_tc_applicable(d))
         return launch_attn_q8_tc(d, w, q, kc, vc, scales, kv_len, parent, out, workspace, workspace_bytes, status, static_cast<cudaStream_t>(stream), pages,
                                  block_table);
-    return launch_attn_q8_simt(d, w, q, kc, vc, scales, kv_len, parent, out, workspace, workspace_bytes, status, static_cast<cudaStream_t>(stream),
-                               make_page_map(pages, block_table, d.Hkv, d.D));
+    return launch_attn_q8_simt(d, w, q, kc, vc, scales, kv_len, parent, out, parts_of(workspace), parts_bytes(workspace_bytes), status,
+                               static_cast<cudaStream_t>(stream), make_page_map(pages, block_table, d.Hkv, d.D));
 }
 
 int ht_tree_attention_q8(const ht_attn_desc *desc, const ht_window_desc *window, const ht_q8_scales *scales, const void *q, const void *k_cache,

@@ -77,3 +77,29 @@ def test_first_tokens_within_a_tree(hb, dtype, D, roots, N, L, window, sinks):  
             Case(N, dtype, 1, N, 2, 2, D, (L,), page=page, parent=parent).check(hb, "%s %s" % (page, kw), window=window, sinks=sinks, **kw)
     if dtype == "bf16":                                                                 # the tensor cores
         Case(N, dtype, 1, N, 2, 2, 128, (L,), parent=parent).check(hb, window=window, sinks=sinks)
+
+
+def test_split_calls_on_the_alus_leave_a_workspace_clean(hb):  # noqa: F811
+    """Calls with parts of their own, of the 8-bit and of the other caches, between calls that count on the counters' area."""
+    ws = torch.zeros(64 << 20, dtype=torch.uint8, device="cuda")
+    clean = [Case(20, "bf16", 3, 40, 40, 40, 128, (900, 1000, 1100)), Case(23, "f16", 6, 5, 16, 16, 128, (700, 1, 300, 900, 40, 6000))]
+    split = [Case(80, "f32", 2, 30, 4, 2, 64, (600, 90)), Case(81, "bf16", 1, 9, 8, 2, 64, (900,), page=16), Case(82, "bf16", 2, 20, 6, 2, 128, (500, 300))]
+    want = [c.want() for c in clean + split]
+    lens = lambda c: (torch.from_numpy(c.lens).cuda(), torch.from_numpy(c.parent).cuda())  # noqa: E731
+    k16 = torch.randn((2, 2, 700, 64), device="cuda")
+    def others():                                                                       # the call of 16- and 32-bit caches
+        _, st = hb.tree_attention(split[0].q, k16, k16, *lens(split[0]), workspace=ws, num_splits=5)
+        assert st.tolist() == [0, 0]
+    for between in [lambda c=c, w=w, kw=kw: (c, w, kw) for c, w in zip(split, want[2:]) for kw in (dict(), dict(num_splits=6))] + [others, None]:
+        if between is others:
+            others()
+        elif between:
+            c, w, kw = between()
+            out, st = c.run(hb, workspace=ws, **kw)
+            assert (st == 0).all()
+            close(out, w)
+        assert int(ws[:65536].view(torch.int32).abs().max()) == 0
+        for c, w in zip(clean, want):
+            out, st = c.run(hb, workspace=ws, flags=hb.HT_ATTN_WORKSPACE_CLEAN)
+            assert (st == 0).all()
+            close(out, w)

@@ -197,8 +197,9 @@ __device__ __forceinline__ uint32_t to_e4m3x2(float lo, float hi) {
 // A row of Q (128 values in global memory, or none) times 2^-e, which brings its largest value to 128 .. 256, as a sum of parts
 // in e4m3: each part takes four bits and leaves the rest, exactly, to the next, down to 2^-9.  bf16's eight bits are two
 // parts' wherever a value is not 2^9 times smaller than the row's largest, fp16's eleven three parts' down to 2^6 times
-// smaller; below, what is left over is at most 2^-10, 2^-17 of the largest value.  e is 0 for a row of zeros, or with an infinity
-// or a NaN.  Four lanes next to one another take a row; `quarter` is this one's, and all lanes of the warp are here.
+// smaller; below, what is left over is at most 2^-10, 2^-17 of the largest value.  e is 0 for a row of zeros.  A row with an
+// infinity or a NaN has no result that is a number (its scores are infinite or none, whatever the keys): all of it becomes NaN, as
+// the conversion would make 448 of an infinity.  Four lanes next to one another take a row; `quarter` is this one's, and all lanes of the warp are here.
 template <bool kBf16>
 struct QuarterRow {
     uint4 in[4];
@@ -220,7 +221,7 @@ struct QuarterRow {
         const float largest = kBf16 ? __uint_as_float(top << 16) : __half2float(__ushort_as_half((unsigned short)top));
         const uint32_t bits = __float_as_uint(largest);
         const int e = bits == 0u || bits >= 0x7F800000u ? 0 : max((int)(bits >> 23) - 134, -100);
-        const float factor = pow2(-e);
+        const float factor = bits >= 0x7F800000u ? __uint_as_float(0x7FC00000u) : pow2(-e);
 #pragma unroll
         for (int k = 0; k < 2; ++k) {                       // 16 values: 16 bytes of each part
             const int c = quarter + 4 * k;

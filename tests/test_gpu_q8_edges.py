@@ -103,3 +103,24 @@ def test_split_calls_on_the_alus_leave_a_workspace_clean(hb):  # noqa: F811
             out, st = c.run(hb, workspace=ws, flags=hb.HT_ATTN_WORKSPACE_CLEAN)
             assert (st == 0).all()
             close(out, w)
+
+
+@pytest.mark.parametrize("dtype,D", [("bf16", 128), ("f16", 128), ("f32", 64), ("f16", 64)])
+@pytest.mark.parametrize("shape", [(2, 7, 4, 2, (300, 5)), (1, 20, 8, 8, (1500,)), (4, 33, 40, 40, (500, 17, 260, 900))], ids=["few", "clusters", "list"])
+def test_queries_that_are_no_numbers(hb, dtype, D, shape):  # noqa: F811
+    """A query row with an infinity or a NaN gives NaN, whatever else it holds and whatever it sees; the rows next to it are what they were."""
+    B, N, Hq, Hkv, lens = shape
+    for kw in (dict(), dict(window=40, sinks=3)):
+        c = Case(60, dtype, B, N, Hq, Hkv, D, lens)
+        want = c.want(**kw)
+        rng = np.random.default_rng(N)
+        hit = np.zeros((B, N, Hq), bool)
+        for i in range(3 * B):
+            b, r, h = rng.integers(B), rng.integers(N), rng.integers(Hq)
+            c.q[b, r, h, int(rng.integers(D))] = (float("inf"), -float("inf"), float("nan"))[i % 3]
+            hit[b, r, h] = True
+        c.q[0, 0, 0], hit[0, 0, 0] = float("inf"), True
+        out, st = c.run(hb, **kw)
+        assert st.tolist() == [0] * B
+        assert np.array_equal(out.isnan().any(-1).cpu().numpy(), hit) and np.array_equal(out.isnan().all(-1).cpu().numpy(), hit)
+        close(out, tuple(np.where(hit[..., None], np.nan, w) for w in want), str(kw))

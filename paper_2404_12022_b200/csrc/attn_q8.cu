@@ -904,7 +904,8 @@ attn_q8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__
                 }
                 const int kt = sg.kt0 + i, tile_lo = (kt < gap_at ? kt : kt + gap) * kTile, key0 = tile_lo + h * 64;
                 ok = ok && mbar_wait_quick(smem_u32(&sm.ref_full[jj & 3]), (jj >> 2) & 1, abort_flag);
-                const float tile_scale = row_scale * pow2(sm.ref[jj & 3][0]), shift = (float)sm.ref[jj & 3][1];
+                // (never zero: a masked score is -inf, and zero times that is none; scores as small are below 2^-96)
+                const float tile_scale = fmaxf(row_scale * pow2(sm.ref[jj & 3][0]), 0x1p-120f), shift = (float)sm.ref[jj & 3][1];
                 const float *factor = &sm.factor[jj & 3][h * 64];
                 const uint32_t s_addr = tmem + lane_base + s * 128 + h * 64;
                 ok = ok && mbar_wait_quick(smem_u32(&sm.s_full[s]), (jj >> 1) & 1, abort_flag);

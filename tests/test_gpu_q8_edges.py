@@ -124,3 +124,16 @@ def test_queries_that_are_no_numbers(hb, dtype, D, shape):  # noqa: F811
         assert st.tolist() == [0] * B
         assert np.array_equal(out.isnan().any(-1).cpu().numpy(), hit) and np.array_equal(out.isnan().all(-1).cpu().numpy(), hit)
         close(out, tuple(np.where(hit[..., None], np.nan, w) for w in want), str(kw))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_small_queries_on_zero_keys(hb, dtype):  # noqa: F811
+    """Scores that vanish next to one another leave equal weights, whatever powers of two they are made of."""
+    for power in (-60, -110):
+        for zeros in (slice(None), slice(130, None), slice(0, 256)):
+            c = Case(70, dtype, 2, 9, 4, 2, 128, (300, 40))
+            c.q = (c.q.double() * 2.0 ** power).to(c.q.dtype)
+            c.codes[0][:, :, zeros], c.bytes[0][:, :, zeros] = 0, 1
+            c.upload()
+            c.check(hb, "%d %s" % (power, zeros))
+            c.check(hb, "%d %s" % (power, zeros), window=20, sinks=3)

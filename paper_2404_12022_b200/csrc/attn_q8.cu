@@ -933,7 +933,10 @@ attn_q8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__
                     mx = fmaf(mx, tile_scale, shift);                 // scale > 0: max commutes with scaling
                 }
                 // The reference rises, for the 32 rows together, only where some row's maximum leaves it 2^8 behind (or has none yet).
-                if (pair_any(pair_id, mx > m_ref + kRescaleThreshold || (m_ref == -INFINITY && mx != -INFINITY))) {
+                // Under values that are all but zero, with an exponent down to -100, the sum of the weights themselves holds up to 2^107
+                // for a key: there it rises at once, and a million such keys stay within 32 bits (2^15 did not, 2^8 behind).
+                const float behind = shift < -64.f ? 0.f : kRescaleThreshold;
+                if (pair_any(pair_id, mx > m_ref + behind || (m_ref == -INFINITY && mx != -INFINITY))) {
                     sm.mx[s][h][row] = mx;
                     pair_sync(pair_id);
                     const float m_new = fmaxf(m_ref, fmaxf(mx, sm.mx[s][h ^ 1][row]));

@@ -137,3 +137,33 @@ def test_small_queries_on_zero_keys(hb, dtype):  # noqa: F811
             c.upload()
             c.check(hb, "%d %s" % (power, zeros))
             c.check(hb, "%d %s" % (power, zeros), window=20, sinks=3)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_long_texts_of_zero_values(hb, dtype):  # noqa: F811
+    """The sum of the weights of tens of thousands of keys whose values are all zero: one key that is not has its share of the whole.
+
+    Every head holds the same: two tiles of zero keys, 2^15 and more rows that score 7.9 above them in powers of two and hold zeros, and one
+    last context row that scores 7.9 too and holds ones.  Result: 1 / (number of those rows + what the others add)."""
+    sms = torch.cuda.get_device_properties(0).multi_processor_count
+    N, D, H, L, cap = 1, 128, sms, 46000, 46016
+    a = 4.0
+    k = torch.zeros((1, H, cap, D), dtype=torch.uint8, device="cuda")
+    v, ks, vs = torch.zeros_like(k), torch.full((1, H, cap), 127, dtype=torch.uint8, device="cuda"), torch.ones((1, H, cap), dtype=torch.uint8, device="cuda")
+    k[:, :, 256:L, 0] = 0x38                                                            # 1.0 in the first feature
+    v[:, :, L - 1] = 0x38
+    vs[:, :, L - 1] = 127
+    q = torch.zeros((1, N, H, D), dtype=torch.bfloat16 if dtype == "bf16" else torch.float16, device="cuda")
+    q[..., 0] = a
+    scale = 7.9 * np.log(2.0) / a
+    ty = lambda t: t.view(torch.float8_e4m3fn if t.dim() == 4 else torch.float8_e8m0fnu)  # noqa: E731
+    out, st = hb.tree_attention_q8(q, ty(k), ty(v), ty(ks), ty(vs), torch.tensor([L], dtype=torch.int32, device="cuda"),
+                                   torch.full((1, N), -1, dtype=torch.int32, device="cuda"), scale=scale)
+    assert st.tolist() == [0]
+    rest = (256 + 1) * 2.0 ** -7.9                                                      # the two tiles, and the row itself (a zero key)
+    want = 1.0 / (L - 256 + rest)
+    got = out.double()
+    # the weight rounded to fp16, the result to the type (fp16: a step of 2^-24 at these sizes), 32-bit sums of 46000 terms by 256 at a time
+    half = torch.finfo(out.dtype).eps / 2
+    tol = want * (2.0 ** -11 + half + 1e-4) + (2.0 ** -25 if dtype == "f16" else 0.0)
+    assert (got - want).abs().max() <= tol, (got.min(), got.max(), want)

@@ -844,6 +844,8 @@ def _q8_attn_args(q, kv_len, parent, window, sinks):
         raise ValueError("q must be contiguous")
     _dense(kv_len, dev, torch.int32, (B,), "kv_len")
     _dense(parent, dev, torch.int32, (B, N), "parent")
+    if not all(-1 << 31 <= x < 1 << 31 for x in (window, sinks)):   # (ctypes would take what is left of them in 32 bits)
+        raise ValueError("window and sinks must be 32-bit integers")
     return B, N, Hq, D, dev, WindowDesc(window, sinks)
 
 

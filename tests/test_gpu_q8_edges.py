@@ -167,3 +167,13 @@ def test_long_texts_of_zero_values(hb, dtype):  # noqa: F811
     half = torch.finfo(out.dtype).eps / 2
     tol = want * (2.0 ** -11 + half + 1e-4) + (2.0 ** -25 if dtype == "f16" else 0.0)
     assert (got - want).abs().max() <= tol, (got.min(), got.max(), want)
+
+
+def test_windows_beyond_32_bits_are_refused(hb):  # noqa: F811
+    c = Case(90, "bf16", 1, 4, 2, 2, 128, (40,), page=16)
+    d = Case(91, "bf16", 1, 4, 2, 2, 128, (40,))
+    for case in (c, d):
+        for kw in (dict(window=1 << 32), dict(window=(1 << 32) + 5), dict(window=5, sinks=1 << 32), dict(window=5, sinks=(1 << 33) + 1)):
+            with pytest.raises(ValueError):
+                case.run(hb, **kw)
+        case.check(hb, window=(1 << 31) - 1, sinks=(1 << 31) - 1)

@@ -178,3 +178,13 @@ def test_counts_out_of_range_are_reported(hb):
     st = hb.count_tokens(tokens, counts, index=index)
     want, status = qo.count_tokens(host(tokens), host(start), index=host(index))
     assert st.tolist() == status.tolist() == [7, 7, 0, 0, 0] and np.array_equal(host(counts), want)
+
+
+@pytest.mark.parametrize("in_place", [False, True], ids=["apart", "in_place"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_many_rows_a_block(hb, dtype, in_place):
+    """Batches large enough for a warp to take several rows, one after the other: the next row's mask and logits are on their way
+    while one is worked on, in the same places."""
+    c = Case(9, dtype, 16, 128, 2, 20001, seen=900, n_bias=40, masked=True)
+    c.check(hb, in_place)
+    c.check(hb, in_place, allowed=None)

@@ -177,3 +177,21 @@ def test_windows_beyond_32_bits_are_refused(hb):  # noqa: F811
             with pytest.raises(ValueError):
                 case.run(hb, **kw)
         case.check(hb, window=(1 << 31) - 1, sinks=(1 << 31) - 1)
+
+
+@pytest.mark.parametrize("shape,page", [((2, 40, 40, 40, 128, (2000, 1500)), 0), ((2, 40, 40, 40, 128, (2000, 1500)), 16), ((1, 91, 8, 8, 128, (6000,)), 0),
+                                        ((1, 91, 8, 8, 128, (6000,)), 64), ((3, 67, 64, 8, 128, (3000, 2000, 900)), 128)],
+                         ids=["list", "list_paged", "clusters", "clusters_paged", "groups_paged"])
+def test_waits_that_run_out_are_reported_in_every_form(hb, shape, page):  # noqa: F811
+    """The hook that lets no wait last: the calls return, every sequence's status says so, and the next call on the same workspace and
+    output is right."""
+    c = Case(33, "bf16", *shape, page=page)
+    want = c.want()
+    ws, out = torch.zeros(48 << 20, dtype=torch.uint8, device="cuda"), torch.empty_like(c.q)
+    for _ in range(3):
+        _, st = c.run(hb, flags=hb.HT_ATTN_TEST_SHORT_WAITS, workspace=ws, out=out)
+        assert st.tolist() == [hb.HT_STATUS_TIMEOUT] * shape[0]
+    for kw in (dict(), dict(flags=hb.HT_ATTN_WORKSPACE_CLEAN)):
+        _, st = c.run(hb, workspace=ws, out=out, **kw)
+        assert st.tolist() == [0] * shape[0]
+        close(out, want, str(kw))

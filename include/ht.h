@@ -521,14 +521,16 @@ int ht_norm_rope_kv_append_q8_paged(const ht_attn_desc *desc /* host */, const h
  * ht_tree_attention shows a row, a window leaves those at most window - 1 positions ahead of it, and those at positions below
  * `sinks`.  Context row j is at position j, a tree row at kv_len plus the number of its ancestors in the tree.
  *   window  NULL or window 0: none.  window >= 1 (a row sees itself at least), sinks >= 0
- *   scale, num_splits, flags, statuses, workspace: as ht_tree_attention, with ht_tree_attention_q8_workspace(desc) bytes.
+ *   scale, num_splits, flags, statuses, workspace: as ht_tree_attention, with ht_tree_attention_q8_workspace(desc) bytes (paged:
+ *           of a desc whose cap is max_pages * page_size).
  *           HT_ATTN_CONTEXT_FINAL has no effect.  Workspaces may be shared with ht_tree_attention's calls.
  * Supported: what ht_tree_attention supports (fp16 / bf16 with D = 128 and Hq / Hkv a power of two on the tensor cores, B <= 256;
  * the rest on the fp32 ALUs), paged as well as contiguous.  On the tensor cores q goes as a sum of e4m3 parts relative to a
  * power of two of its row (bf16: two, fp16: three; exact where a value is not 2^9, fp16: 2^6, times smaller than the row's largest,
  * otherwise off by 2^-17 of that at most), K's codes as they are, their powers of two in fp32; V in fp16 relative to the largest
- * scale among 128 rows, exactly where a row's is not 2^22 times smaller; the weights rounded to fp16 (as a pair of two such
- * values in tiles with tree rows and, with a window, in those of the last 128 context rows).
+ * scale among the 128 rows of its tile that some query row of the sequence sees (not each of them need: rows of other branches
+ * count), exactly where a row's is not 2^22 times smaller; the weights rounded to fp16 (as a pair of two such values in tiles with
+ * tree rows and, with a window, in those of the last 128 context rows).
  * Rows that no row sees (ahead of every row's window and behind the first tokens) may hold anything; paged: so may the entries of
  * pages of such rows alone.
  */

@@ -11,9 +11,10 @@
 //               largest of their powers of two, which the softmax adds to its exponents, so that a weight is held as what multiplies V's
 //               fp16 values.
 // Widening K as well kept the converting warps busy longer than the softmax where keys are shared: 16 x 67 rows of 64 on 8 heads
-// on 8192 keys 763 us, and 569 as it stands (4 x 91 rows of 32 heads on 4096 keys 68 and 72 us, 1 x 91 on 1024 16 and 21: with
-// few tiles per CTA it is the chain ahead of the first product that counts).  No unit is saturated (issue slots 45 %, tensor pipe
-// 25 %, shared memory 28 %): a tile's chain of waits is what bounds it, widening V and the maxima a tenth of the time each.
+// on 8192 keys 763 us, and 580 as it stands (4 x 91 rows of 32 heads on 4096 keys 68 and 73.5 us, 1 x 91 on 1024 16 and 21: with
+// few tiles per CTA it is the chain ahead of the first product that counts).  No unit is saturated (4 x 91 on 4096: issue slots
+// 40 %, tensor pipe 20 %, shared memory 28 %): a tile's chain of waits is what bounds it, widening V and the maxima a tenth of the
+// time each.
 //
 // The roles of a CTA (768 threads, one CTA per SM):
 //   warp 20         copies: code tiles (16 KiB, 128-byte swizzle), and with K's the 256 scale bytes of K's and V's rows
@@ -1314,7 +1315,7 @@ int launch_attn_q8_tc(const ht_attn_desc &d, const ht_window_desc &w, const void
     const int sms = sm_count(), k = cluster_size_q8(d, w, form);
     if (k == 0) form -= 4;
     // Row tiles side by side on the same keys, where at least four such groups fit: 16 x 67 rows of 64 on 8 heads on 8192 keys take
-    // 569 us, and 587 with the row tiles one after the other in the list.
+    // 580 us, and 593 with the row tiles one after the other in the list.
     qp.group = k <= 1 && p.n_rt > 1 && p.n_rt * 4 <= sms ? p.n_rt : 1;
     p.grid = k > 1 ? (int)units * k : sms / qp.group * qp.group;
     p.cluster_k = k > 1 ? k : 0;

@@ -4,8 +4,8 @@
 //   key j, running maximum and sum by shuffles, each lane owns D / 32 output features; with several splits (m, l, O) parts
 //   go to the workspace and a second kernel merges them.
 // Bound by the ALUs: 2 x 32 x D products per row and step against 64 D bytes.  Steps of context rows that no row of the block sees
-// (outside the window and behind the first tokens) are jumped over.  1 x 91 rows of 32 heads of 128 on 1024 keys in fp32: 285 us = 5.4 TFLOP/s;
-// heads of 64 in bf16 151 us.
+// (outside the window and behind the first tokens) are jumped over.  1 x 91 rows of 32 heads of 128 on 1024 keys in fp32: 295 us = 5.4 TFLOP/s;
+// heads of 64 in bf16 161 us.
 #include "q8.cuh"
 
 namespace ht {
@@ -231,8 +231,8 @@ attn_q8_combine_kernel(const Params p) {
 
 }  // namespace q8simt
 
-// Blocks for eight per SM, with 256 keys at least per split (1 x 91 rows of 32 heads on 1024 keys in fp32: four splits 285 us, two 320,
-// none 323).
+// Blocks for eight per SM, with 256 keys at least per split (1 x 91 rows of 32 heads on 1024 keys in fp32: four splits 295 us, two 324,
+// none 323, eight 292; heads of 64 in bf16: 161, 176, 170 and 163).
 static int choose_splits_q8(const ht_attn_desc &d) {
     if (d.num_splits > 0) return d.num_splits;
     const long long blocks = (long long)((d.N + q8simt::kRows - 1) / q8simt::kRows) * d.Hq * d.B, target = 8ll * sm_count();
